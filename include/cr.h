@@ -45,6 +45,9 @@ typedef int32_t cr_status;
 #define CR_ERR_DEST_RANGE 2u  /* a destination >= R was seen by the replay        */
 #define CR_ERR_SPEC 4u        /* a plan spec disagrees with its counts row         */
 #define CR_ERR_KEYMAP_FULL 8u /* more distinct opaque ids than the directory holds  */
+#define CR_ERR_SEQ 16u        /* offsets, lengths or indices of sequences that do not fit */
+#define CR_ERR_PAGE 32u       /* a page id out of range, or a free page named or freed  */
+#define CR_ERR_PAGES_OUT 64u  /* fewer free pages than a call would take            */
 
 #define CR_EMPTY_SLOT 0xFFFFFFFFu /* unused LRU slot / unused key               */
 #define CR_NO_KEY 0xFFFFFFFFu     /* not an opaque id; dense index of an unknown id */
@@ -383,6 +386,170 @@ cr_status cr_keymap_lookup(const void* table, size_t table_bytes, uint32_t capac
  * other entries of out are left as they are. ids, values u32 [m]; out u32 [out_len]. */
 cr_status cr_keymap_scatter(const void* table, size_t table_bytes, uint32_t capacity, const uint32_t* ids,
                             const uint32_t* values, uint64_t m, uint32_t* out, uint32_t out_len, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * The destination's side: what a hit, a miss and an eviction of the replay stand for on a
+ * serving GPU (Section 3.2: admitted and cold prefixes share each destination's native
+ * prefix cache). A cache of keys and values in pages, the calls that share, copy, move and
+ * free its pages, attention over whole prompts (a miss) and attention of requests that share
+ * a cached prefix (a hit, and every decoded token).
+ *
+ * Element types: CR_BF16, CR_F16 (queries, keys, values and outputs of one call alike).
+ * Scores, softmax statistics and sums are fp32; the softmax weights are rounded to the
+ * element type for the second product, as are the outputs, once.
+ * ------------------------------------------------------------------------------------- */
+#define CR_BF16 0u
+#define CR_F16 1u
+#define CR_NO_PAGE 0xFFFFFFFFu       /* table entry behind a sequence's pages           */
+#define CR_MAX_PAGE_TOKENS 1024      /* tokens per page: a power of two up to this      */
+#define CR_MAX_HEADS 1024            /* heads of queries, or of keys and values         */
+#define CR_MAX_LAYERS 1024           /* layers of a cache                               */
+#define CR_MAX_PAGES (1u << 26)      /* pages of a cache                                */
+
+/* Rows of a packed tensor [tokens][heads][dim]: element (t, h, x) at p[t * token_stride +
+ * h * head_stride + x]. Strides count elements, are multiples of 8 and not negative; p is
+ * 16-byte aligned. */
+typedef struct {
+    void* p;
+    int64_t token_stride;
+    int64_t head_stride;
+} cr_rows;
+
+/* A paged cache of keys and values. Page g of layer l holds page_tokens tokens of every key
+ * head: element (l, g, h, t, x) of k and of v at [l * layer_stride + g * page_stride +
+ * h * head_stride + t * token_stride + x] (strides in elements, multiples of 8, not negative;
+ * heads before tokens or tokens before heads alike; k and v 16-byte aligned). Page ids and
+ * counts are the same for all layers. refs u32 [num_pages]: how many table entries name a
+ * page; 0 = free. Page tables are u32 [rows][width]; entry j of a row holds the page of
+ * tokens [j * page_tokens, (j + 1) * page_tokens) of its sequence. */
+typedef struct {
+    uint32_t dtype;       /* CR_BF16 or CR_F16                                          */
+    uint32_t heads;       /* key heads, 1..CR_MAX_HEADS                                 */
+    uint32_t dim;         /* 64 or 128                                                  */
+    uint32_t page_tokens; /* power of two, 1..CR_MAX_PAGE_TOKENS                        */
+    uint32_t num_pages;   /* 1..CR_MAX_PAGES                                            */
+    uint32_t layers;      /* 1..CR_MAX_LAYERS                                           */
+    void* k;
+    void* v;
+    int64_t layer_stride, page_stride, head_stride, token_stride;
+    uint32_t* refs;
+} cr_kv_cache;
+
+/* Workspace of cr_pages_extend, cr_pages_fork (n sequences) and cr_pages_compact (n = 0). */
+size_t cr_pages_workspace_bytes(uint32_t num_pages, uint32_t n);
+
+/* Pages for sequences that grow from len_old[i] to len_new[i] tokens: table[i][j] for
+ * ceil(len_old[i] / page_tokens) <= j < ceil(len_new[i] / page_tokens) become free pages, the
+ * lowest ids first in the order of (i, j), with refs 1. len_old, len_new u32 [n] (len_old
+ * NULL: all 0); table u32 [n][width]. A sequence that shrinks or passes the table's width
+ * sets CR_ERR_SEQ and takes none. Too few free pages set CR_ERR_PAGES_OUT, and then nothing
+ * is changed. */
+cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_old, const uint32_t* len_new, uint32_t n,
+                          uint32_t* table, uint32_t width, void* ws, size_t ws_bytes, uint32_t* err, void* stream);
+
+/* Children of cached sequences: child i continues the first length[i] tokens of row parent[i]
+ * of `table`. Its full pages are its parent's (refs + 1 each); where length[i] is not a
+ * multiple of page_tokens the tokens behind them are copied, in every layer, into a page of
+ * its own (refs 1; lowest free ids first in the order of children), so that both may go on
+ * writing. Entries of child behind its pages become CR_NO_PAGE. parent, length u32 [n]; table
+ * u32 [rows][width]; child u32 [n][child_width] (not `table` itself). A parent >= rows or a
+ * length beyond either width sets CR_ERR_SEQ and that child gets no pages; an entry that is out of
+ * range or names a free page sets CR_ERR_PAGE and becomes CR_NO_PAGE (a tail's is copied from
+ * nowhere). CR_ERR_PAGES_OUT as cr_pages_extend, and then no page is taken or shared and all
+ * children's entries are CR_NO_PAGE. */
+cr_status cr_pages_fork(const cr_kv_cache* c, const uint32_t* table, uint32_t rows, uint32_t width,
+                        const uint32_t* parent, const uint32_t* length, uint32_t n, uint32_t* child,
+                        uint32_t child_width, void* ws, size_t ws_bytes, uint32_t* err, void* stream);
+
+/* refs - 1 for every page of n sequences' first length[i] tokens. A length beyond the width
+ * sets CR_ERR_SEQ (the row is skipped); a page out of range, or freed more often than it is
+ * named, sets CR_ERR_PAGE (refs stay >= 0). */
+cr_status cr_pages_free(const cr_kv_cache* c, const uint32_t* table, uint32_t width, const uint32_t* length,
+                        uint32_t n, uint32_t* err, void* stream);
+
+/* Moves the live pages to the front: with L pages live, the i-th live page with an id >= L moves
+ * to the i-th free id < L, contents of all layers, and the tables' entries are renamed.
+ * table u32 [rows][width], length u32 [rows]: entries of a row's first length tokens are
+ * renamed into table_out (the same shape), the others copied; refs_out u32 [num_pages]
+ * receives the counts (table_out and refs_out may be table and c->refs). Pages that moved
+ * away keep their old contents. Several tables: rename them in one call by giving them as one
+ * array, or call with rows = 0 last. A length beyond the width sets CR_ERR_SEQ (the row is
+ * copied); an entry out of range or naming a free page sets CR_ERR_PAGE and is copied. */
+cr_status cr_pages_compact(const cr_kv_cache* c, const uint32_t* table, const uint32_t* length, uint32_t rows,
+                           uint32_t width, uint32_t* table_out, uint32_t* refs_out, void* ws, size_t ws_bytes,
+                           uint32_t* err, void* stream);
+
+/* Contents of page src[i] copied to page dst[i], i < n, all layers; refs are not touched. The
+ * dst are distinct and none of them is among the src (otherwise contents are unspecified). An
+ * id out of range sets CR_ERR_PAGE and that pair is skipped. */
+cr_status cr_pages_copy(const cr_kv_cache* c, const uint32_t* src, const uint32_t* dst, uint32_t n, uint32_t* err,
+                        void* stream);
+
+/* New keys and values of packed sequences into their pages of one layer: sequence i's tokens
+ * are rows off[i]..off[i+1] of k and v ([total][heads][dim], the cache's type) and the last of
+ * its length[i] tokens. off u32 [n+1], length u32 [n], table u32 [n][width]. A sequence whose
+ * rows or length do not fit sets CR_ERR_SEQ, a page out of range CR_ERR_PAGE; their tokens are
+ * skipped. Sequences must not name the same page for the tokens they write. */
+cr_status cr_kv_append(const cr_kv_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, uint32_t total,
+                       const uint32_t* off, const uint32_t* length, uint32_t n, const uint32_t* table, uint32_t width,
+                       uint32_t* err, void* stream);
+
+/* Attention over packed prompts with grouped heads. Sequence b has queries q_off[b]..q_off[b+1]
+ * (nq of them) and keys k_off[b]..k_off[b+1] (nk). Query head h reads key head
+ * h / (heads_q / heads_kv). With s_j = scale * q_i . k_j over the visible keys j,
+ *   out_i = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  lse_i = m + ln sum_j exp(s_j - m),
+ * m the largest s_j. causal = 1: row i sees keys j <= i + nk - nq (the last query sees all
+ * keys, so nk > nq continues earlier context); causal = 0: all keys. A row that sees no key
+ * gives out 0 and lse -inf. Keys and values of other sequences never reach a row, whatever
+ * bits they hold; within a sequence a value that is not finite may reach earlier rows of up to
+ * 127 tokens before its own. */
+typedef struct {
+    uint32_t dtype, heads_q, heads_kv, dim; /* dim 64 or 128; heads_q a multiple of heads_kv */
+    uint32_t batch, causal;
+    uint32_t total_q, total_k;              /* rows of q and out, rows of k and v           */
+    float scale;                            /* > 0, finite                                  */
+    cr_rows q, k, v, out;
+    float* lse;                             /* f32 [total_q][heads_q], or NULL              */
+    const uint32_t* q_off;                  /* u32 [batch + 1], 0 .. total_q, non-decreasing */
+    const uint32_t* k_off;                  /* u32 [batch + 1], 0 .. total_k                */
+} cr_attn_prompt_args;
+
+/* total_q * heads_q < 2^31 (CR_EINVAL otherwise). Offsets that do not fit set CR_ERR_SEQ; the
+ * rows of such a sequence are then unspecified. The workspace holds partial results where
+ * the keys of a call with few rows are split over more workgroups; its size follows from the
+ * args' scalars alone (pointers and strides are not read). */
+size_t cr_attn_prompt_workspace_bytes(const cr_attn_prompt_args* a);
+cr_status cr_attn_prompt(const cr_attn_prompt_args* a, void* ws, size_t ws_bytes, uint32_t* err, void* stream);
+
+/* Attention of requests that share prefixes in a paged cache. Requests group_off[g] ..
+ * group_off[g+1] form group g and share the prefix_len[g] tokens of row g of prefix_table; row
+ * r of own_table holds request r's own own_len[r] tokens behind the prefix, its q_off[r+1] -
+ * q_off[r] query tokens being the last of them (already appended). Query t of nq sees the
+ * whole prefix and own tokens j <= own_len - nq + t. A group's prefix is read once for all its
+ * requests' queries and query heads; the results over prefix and own tokens are joined by
+ * their log-sum-exp. Definitions of out, lse and empty rows as cr_attn_prompt. One query per
+ * request is a decode step, several are the suffix of a hit or drafted tokens. prefix_len and
+ * own_len may be 0, and a table of width 0 may be NULL. */
+typedef struct {
+    uint32_t heads_q, layer;
+    uint32_t batch, groups, total_q;
+    uint32_t prefix_width, own_width;       /* entries per table row                        */
+    float scale;
+    cr_rows q, out;                         /* [total_q][heads_q][dim], the cache's type    */
+    float* lse;                             /* f32 [total_q][heads_q], or NULL              */
+    const uint32_t* q_off;                  /* u32 [batch + 1], 0 .. total_q                */
+    const uint32_t* group_off;              /* u32 [groups + 1], 0 .. batch                 */
+    const uint32_t* prefix_table;           /* u32 [groups][prefix_width]                   */
+    const uint32_t* prefix_len;             /* u32 [groups]                                 */
+    const uint32_t* own_table;              /* u32 [batch][own_width]                       */
+    const uint32_t* own_len;                /* u32 [batch]                                  */
+} cr_attn_shared_args;
+
+/* Errors as cr_attn_prompt; lengths beyond a table's width set CR_ERR_SEQ, pages out of range
+ * CR_ERR_PAGE. The workspace size follows from the scalars of the cache and the args. */
+size_t cr_attn_shared_workspace_bytes(const cr_kv_cache* c, const cr_attn_shared_args* a);
+cr_status cr_attn_shared(const cr_kv_cache* c, const cr_attn_shared_args* a, void* ws, size_t ws_bytes, uint32_t* err,
+                         void* stream);
 
 /* Library version string. */
 const char* cr_version(void);

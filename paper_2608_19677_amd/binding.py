@@ -29,7 +29,9 @@ EXPORTS = ("cr_count_rates", "cr_count_slice_workspace_bytes", "cr_count_slice",
            "cr_route_live", "cr_plan_churn", "cr_keymap_bytes", "cr_keymap_workspace_bytes", "cr_keymap_build",
            "cr_keymap_lookup", "cr_keymap_scatter", "cr_replay_workspace_bytes", "cr_lru_state_bytes",
            "cr_lru_reset", "cr_replay", "cr_replay_partition", "cr_replay_lru", "cr_replay_set_group_min_records",
-           "cr_version")
+           "cr_pages_workspace_bytes", "cr_pages_extend", "cr_pages_fork", "cr_pages_free", "cr_pages_compact",
+           "cr_pages_copy", "cr_kv_append", "cr_attn_prompt_workspace_bytes", "cr_attn_prompt",
+           "cr_attn_shared_workspace_bytes", "cr_attn_shared", "cr_version")
 CR_WINDOW_SUM = 0xFFFFFFFFFFFFFFFF
 CR_PLAN_BUFFERS = 16
 CR_GROUP_MULTI, CR_GROUP_COLD = 0xFFFE, 0xFFFF
@@ -53,6 +55,36 @@ class CrPlanSet(ctypes.Structure):
                 ("num_admitted", _P), ("cold", _P), ("clamped", _P), ("member_off", _P), ("members", _P),
                 ("load", _P), ("key_index", _P), ("route", _P), ("window_rank", _P), ("group_dest", _P),
                 ("group_rank", _P), ("group_multi", _P)]
+
+
+CR_BF16, CR_F16 = 0, 1
+CR_NO_PAGE = 0xFFFFFFFF
+CR_ERR_SEQ, CR_ERR_PAGE, CR_ERR_PAGES_OUT = 16, 32, 64
+
+_i64, _f32 = ctypes.c_int64, ctypes.c_float
+
+
+class CrRows(ctypes.Structure):
+    _fields_ = [("p", _P), ("token_stride", _i64), ("head_stride", _i64)]
+
+
+class CrKvCache(ctypes.Structure):
+    _fields_ = [("dtype", _u32), ("heads", _u32), ("dim", _u32), ("page_tokens", _u32), ("num_pages", _u32),
+                ("layers", _u32), ("k", _P), ("v", _P), ("layer_stride", _i64), ("page_stride", _i64),
+                ("head_stride", _i64), ("token_stride", _i64), ("refs", _P)]
+
+
+class CrAttnPromptArgs(ctypes.Structure):
+    _fields_ = [("dtype", _u32), ("heads_q", _u32), ("heads_kv", _u32), ("dim", _u32), ("batch", _u32), ("causal", _u32),
+                ("total_q", _u32), ("total_k", _u32), ("scale", _f32), ("q", CrRows), ("k", CrRows), ("v", CrRows),
+                ("out", CrRows), ("lse", _P), ("q_off", _P), ("k_off", _P)]
+
+
+class CrAttnSharedArgs(ctypes.Structure):
+    _fields_ = [("heads_q", _u32), ("layer", _u32), ("batch", _u32), ("groups", _u32), ("total_q", _u32),
+                ("prefix_width", _u32), ("own_width", _u32), ("scale", _f32), ("q", CrRows), ("out", CrRows), ("lse", _P),
+                ("q_off", _P), ("group_off", _P), ("prefix_table", _P), ("prefix_len", _P), ("own_table", _P),
+                ("own_len", _P)]
 
 
 class CrError(RuntimeError):
@@ -108,10 +140,26 @@ def load(path: Optional[str] = None):
                                       ctypes.c_size_t, _P, _P]
     L.cr_replay_lru.argtypes = [_P, _u32, _u64, _u32, _u32, _u32, ctypes.POINTER(_u32), _u32, _P, _P, _P, _P,
                                 ctypes.c_size_t, _P, _P]
+    cache, size = ctypes.POINTER(CrKvCache), ctypes.c_size_t
+    L.cr_pages_workspace_bytes.argtypes = [_u32, _u32]
+    L.cr_pages_extend.argtypes = [cache, _P, _P, _u32, _P, _u32, _P, size, _P, _P]
+    L.cr_pages_fork.argtypes = [cache, _P, _u32, _u32, _P, _P, _u32, _P, _u32, _P, size, _P, _P]
+    L.cr_pages_free.argtypes = [cache, _P, _u32, _P, _u32, _P, _P]
+    L.cr_pages_compact.argtypes = [cache, _P, _P, _u32, _u32, _P, _P, _P, size, _P, _P]
+    L.cr_pages_copy.argtypes = [cache, _P, _P, _u32, _P, _P]
+    L.cr_kv_append.argtypes = [cache, _u32, ctypes.POINTER(CrRows), ctypes.POINTER(CrRows), _u32, _P, _P, _u32, _P, _u32,
+                               _P, _P]
+    L.cr_attn_prompt_workspace_bytes.argtypes = [ctypes.POINTER(CrAttnPromptArgs)]
+    L.cr_attn_prompt.argtypes = [ctypes.POINTER(CrAttnPromptArgs), _P, size, _P, _P]
+    L.cr_attn_shared_workspace_bytes.argtypes = [cache, ctypes.POINTER(CrAttnSharedArgs)]
+    L.cr_attn_shared.argtypes = [cache, ctypes.POINTER(CrAttnSharedArgs), _P, size, _P, _P]
+    for f in ("cr_pages_workspace_bytes", "cr_attn_prompt_workspace_bytes", "cr_attn_shared_workspace_bytes"):
+        getattr(L, f).restype = size
     L.cr_version.restype = ctypes.c_char_p
     for f in ("cr_count_rates", "cr_count_slice", "cr_lru_reset", "cr_admit", "cr_admit_noalloc", "cr_place_lpt", "cr_place_hash", "cr_route", "cr_route_live", "cr_plan_churn",
               "cr_keymap_build", "cr_keymap_lookup", "cr_keymap_scatter", "cr_replay",
-              "cr_replay_partition", "cr_replay_lru"):
+              "cr_replay_partition", "cr_replay_lru", "cr_pages_extend", "cr_pages_fork", "cr_pages_free",
+              "cr_pages_compact", "cr_pages_copy", "cr_kv_append", "cr_attn_prompt", "cr_attn_shared"):
         getattr(L, f).restype = ctypes.c_int32
     _lib = L
     return L
@@ -281,6 +329,69 @@ def cr_replay_lru(prefix_len, num_keys: int, n: int, J: int, P: int, R: int, W: 
     _check(load().cr_replay_lru(_ptr(prefix_len), num_keys, n, J, P, R, Wa, max_W, _ptr(lru_in), _ptr(lru_out),
                                 _ptr(stats), _ptr(ws), ws.numel() * ws.element_size(), _ptr(err), _stream(stream)),
            "cr_replay_lru")
+
+
+def cr_pages_workspace_bytes(num_pages: int, n: int) -> int:
+    return int(load().cr_pages_workspace_bytes(num_pages, n))
+
+
+def _table_width(t) -> int:
+    return 0 if t is None else t.shape[-1]
+
+
+def cr_pages_extend(cache: CrKvCache, len_old, len_new, table, ws, err, stream=None):
+    """len_old (or None), len_new: int32 [n]; table: int32 [n, width]."""
+    _check(load().cr_pages_extend(ctypes.byref(cache), _ptr(len_old), _ptr(len_new), len_new.numel(), _ptr(table),
+                                  _table_width(table), _ptr(ws), _nbytes(ws), _ptr(err), _stream(stream)),
+           "cr_pages_extend")
+
+
+def cr_pages_fork(cache: CrKvCache, table, parent, length, child, ws, err, stream=None):
+    """table: int32 [rows, width]; parent, length: int32 [n]; child: int32 [n, child_width]."""
+    _check(load().cr_pages_fork(ctypes.byref(cache), _ptr(table), table.shape[0], _table_width(table), _ptr(parent),
+                                _ptr(length), parent.numel(), _ptr(child), _table_width(child), _ptr(ws), _nbytes(ws),
+                                _ptr(err), _stream(stream)), "cr_pages_fork")
+
+
+def cr_pages_free(cache: CrKvCache, table, length, err, stream=None):
+    _check(load().cr_pages_free(ctypes.byref(cache), _ptr(table), _table_width(table), _ptr(length), length.numel(),
+                                _ptr(err), _stream(stream)), "cr_pages_free")
+
+
+def cr_pages_compact(cache: CrKvCache, table, length, table_out, refs_out, ws, err, stream=None):
+    """table, table_out: int32 [rows, width] (or None); length: int32 [rows]."""
+    rows = 0 if table is None else table.shape[0]
+    _check(load().cr_pages_compact(ctypes.byref(cache), _ptr(table), _ptr(length), rows, _table_width(table),
+                                   _ptr(table_out), _ptr(refs_out), _ptr(ws), _nbytes(ws), _ptr(err), _stream(stream)),
+           "cr_pages_compact")
+
+
+def cr_pages_copy(cache: CrKvCache, src, dst, err, stream=None):
+    _check(load().cr_pages_copy(ctypes.byref(cache), _ptr(src), _ptr(dst), src.numel(), _ptr(err), _stream(stream)),
+           "cr_pages_copy")
+
+
+def cr_kv_append(cache: CrKvCache, layer: int, k: CrRows, v: CrRows, total: int, off, length, table, err, stream=None):
+    _check(load().cr_kv_append(ctypes.byref(cache), layer, ctypes.byref(k), ctypes.byref(v), total, _ptr(off), _ptr(length),
+                               length.numel(), _ptr(table), _table_width(table), _ptr(err), _stream(stream)), "cr_kv_append")
+
+
+def cr_attn_prompt_workspace_bytes(args: CrAttnPromptArgs) -> int:
+    return int(load().cr_attn_prompt_workspace_bytes(ctypes.byref(args)))
+
+
+def cr_attn_prompt(args: CrAttnPromptArgs, ws, err, stream=None):
+    _check(load().cr_attn_prompt(ctypes.byref(args), _ptr(ws), 0 if ws is None else _nbytes(ws), _ptr(err), _stream(stream)),
+           "cr_attn_prompt")
+
+
+def cr_attn_shared_workspace_bytes(cache: CrKvCache, args: CrAttnSharedArgs) -> int:
+    return int(load().cr_attn_shared_workspace_bytes(ctypes.byref(cache), ctypes.byref(args)))
+
+
+def cr_attn_shared(cache: CrKvCache, args: CrAttnSharedArgs, ws, err, stream=None):
+    _check(load().cr_attn_shared(ctypes.byref(cache), ctypes.byref(args), _ptr(ws), 0 if ws is None else _nbytes(ws),
+                                 _ptr(err), _stream(stream)), "cr_attn_shared")
 
 
 class PlanSet:
