@@ -407,8 +407,8 @@ cr_status cr_keymap_scatter(const void* table, size_t table_bytes, uint32_t capa
 #define CR_MAX_PAGES (1u << 26)      /* pages of a cache                                */
 
 /* Rows of a packed tensor [tokens][heads][dim]: element (t, h, x) at p[t * token_stride +
- * h * head_stride + x]. Strides count elements, are multiples of 8 and not negative; p is
- * 16-byte aligned. */
+ * h * head_stride + x]. Strides count elements, are multiples of 8, not negative and below 2^31
+ * (offsets may pass that); p is 16-byte aligned. */
 typedef struct {
     void* p;
     int64_t token_stride;
@@ -417,8 +417,9 @@ typedef struct {
 
 /* A paged cache of keys and values. Page g of layer l holds page_tokens tokens of every key
  * head: element (l, g, h, t, x) of k and of v at [l * layer_stride + g * page_stride +
- * h * head_stride + t * token_stride + x] (strides in elements, multiples of 8, not negative;
- * heads before tokens or tokens before heads alike; k and v 16-byte aligned). Page ids and
+ * h * head_stride + t * token_stride + x] (strides in elements, multiples of 8, not negative,
+ * below 2^31 but for layer_stride; heads before tokens or tokens before heads alike; k and v
+ * 16-byte aligned). Page ids and
  * counts are the same for all layers. refs u32 [num_pages]: how many table entries name a
  * page; 0 = free. Page tables are u32 [rows][width]; entry j of a row holds the page of
  * tokens [j * page_tokens, (j + 1) * page_tokens) of its sequence. */

@@ -5,7 +5,10 @@ Flags:
   -ffp-contract=off            the planner's double arithmetic is one rounding per
                                operation, in the order of the definition;
   -target-feature -packed-fp32-ops
-                               no packed FP32 instructions are generated.
+                               no packed FP32 instructions are generated;
+  -amdgpu-mfma-vgpr-form=1     matrix instructions keep their results in vector registers, where
+                               the softmax reads them (attention of 256 rows a block copied 300
+                               registers per half tile otherwise, 30 with it).
 """
 from __future__ import annotations
 
@@ -23,6 +26,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-ffp-contract=off",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+    "-mllvm", "-amdgpu-mfma-vgpr-form=1",
     "-Wall", "-Wno-unused-function", "-Wno-unused-command-line-argument",
     "-I" + os.path.join(ROOT, "include"),
 ]

@@ -18,7 +18,7 @@ inline uint32_t log2_of(uint32_t p2) { return (uint32_t)__builtin_ctz(p2); }
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
-inline bool good_stride(int64_t s) { return s >= 0 && (s & 7) == 0; }
+inline bool good_stride(int64_t s) { return s >= 0 && (s & 7) == 0 && s < ((int64_t)1 << 31); }
 
 inline bool good_rows(const cr_rows& r)
 {
@@ -35,7 +35,7 @@ inline bool good_cache_sizes(const cr_kv_cache* c)
 
 inline bool good_cache(const cr_kv_cache* c)
 {
-    return good_cache_sizes(c) && c->k && c->v && aligned16(c->k) && aligned16(c->v) && good_stride(c->layer_stride) &&
+    return good_cache_sizes(c) && c->k && c->v && aligned16(c->k) && aligned16(c->v) && c->layer_stride >= 0 && (c->layer_stride & 7) == 0 &&
            good_stride(c->page_stride) && good_stride(c->head_stride) && good_stride(c->token_stride);
 }
 
