@@ -53,6 +53,14 @@ struct F16 {
     }
 };
 
+// The stretches of keys a call works on.
+enum Kind : uint32_t {
+    kPrompt,  // a sequence's keys
+    kGroup,   // a group's prefix, for all rows of its requests
+    kOwn,     // a request's own tokens
+    kWhole,   // a request's prefix and own tokens, one after the other
+};
+
 struct Attn {
     cr_rows q, k, v, out;  // k, v: prompt only
     float* lse;
@@ -67,96 +75,96 @@ struct Attn {
     uint32_t prefix_width, own_width;
     uint32_t heads_q, heads_kv, group, batch, groups, total_q, total_k, causal;
     float c;               // scale * log2(e)
-    uint32_t rows;                   // query rows (token, head of the group) per block
-    uint32_t tiles, splits;          // prompt: over sequences; shared: over groups
-    uint32_t own_tiles, own_splits;  // shared: over requests
-    float* part_o;         // f32 [splits + own_splits][total_q * heads_q][dim], NULL: results are final
-    float* part_lse;       // f32 [splits + own_splits][total_q * heads_q], base 2
+    // A sequence's keys are cut into chunks of at least `chunk` and at most as many as there are slots;
+    // chunk i's results go to slot i, of the own parts of a call that joins them with prefixes to slot
+    // `slots` + i.
+    uint32_t chunk, slots, own_chunk, own_slots;
+    uint32_t first;        // kind of the first slots (the others are kOwn's)
+    float* part_o;         // f32 [slots + own_slots][total_q * heads_q][dim], NULL: results are final
+    float* part_lse;       // f32 [slots + own_slots][total_q * heads_q], base 2
     uint32_t* err;
 };
 
-// What a block works on: rows row0 .. row0 + rows of a sequence's (token, head of the group) rows,
-// over keys begin .. end. Row m is query token tok0 + m / group and sees keys below
-// first_lim + m / group (causal) or all n.
-struct Item {
-    uint32_t row0, rows, tok0, begin, end, slot;
-    int32_t first_lim;
+// A stretch of keys with the rows that see it. Row m is query token tok0 + m / group and sees keys
+// below max(least, first_lim + m / group) (causal) or all n. In pages, keys 0 .. len0 are the first
+// table's and keys gap_end .. n the second's; gap_end is len0 rounded up to whole tiles, so that a
+// tile has keys of one table, and the keys between are seen by no row.
+struct Seq {
+    uint32_t tok0, nq, n;
+    int32_t first_lim, least;
     uint32_t causal;
-    uint32_t key0;                // prompt: first key row
-    const uint32_t* table;        // shared: the sequence's pages
+    uint32_t key0;             // prompt: first key row
+    uint32_t len0, gap_end;
+    const uint32_t* table0;
+    const uint32_t* table1;
 };
 
-__device__ __forceinline__ bool bad_seq(const Attn& a, uint32_t bit)
+__device__ __forceinline__ bool bad_seq(const Attn& a)
 {
-    if (threadIdx.x == 0) atomicOr(a.err, bit);
+    if (threadIdx.x == 0) atomicOr(a.err, CR_ERR_SEQ);
     return false;
 }
 
-// Tile t of sequence x starts at floor(first row / rows per block) + x: steps of at least
-// ceil(rows / rows per block), so that the tiles of all sequences fit into floor(all rows / rows per block) +
-// sequences without a pass that counts them; some are empty.
 template <bool kPaged>
-__device__ __forceinline__ bool find_item(const Attn& a, uint32_t id, Item* it)
+__device__ __forceinline__ bool get_seq(const Attn& a, uint32_t kind, uint32_t x, Seq* s)
 {
-    uint32_t tile, split, splits, x, t0, t1, n;
-    if (kPaged && id < a.tiles * a.splits) {
-        split = id % a.splits;
-        tile = id / a.splits;
-        splits = a.splits;
-        it->slot = split;
-        auto start = [&](uint32_t g) { return a.q_off[min(a.group_off[g], a.batch)] * a.group / a.rows + g; };
-        x = wave_find(a.groups, tile, start);
-        const uint32_t r0 = a.group_off[x], r1 = a.group_off[x + 1];
-        if (r0 > r1 || r1 > a.batch) return bad_seq(a, CR_ERR_SEQ);
-        t0 = a.q_off[r0];
-        t1 = a.q_off[r1];
-        n = a.prefix_len[x];
-        if (pages_of(n, a.pg.log_tokens) > a.prefix_width) return bad_seq(a, CR_ERR_SEQ);
-        it->table = a.prefix_table + (uint64_t)x * a.prefix_width;
-        it->causal = 0;
-        tile -= min(start(x), tile);
-    } else {
-        if (kPaged) {
-            id -= a.tiles * a.splits;
-            splits = a.own_splits;
-            tile = id / splits;
-        } else {
-            splits = a.splits;
-            tile = a.tiles - 1u - id / splits;  // a causal sequence's last rows, the longest, first
-        }
-        split = id % splits;
-        it->slot = (kPaged ? a.splits : 0u) + split;
-        auto start = [&](uint32_t r) { return a.q_off[r] * a.group / a.rows + r; };
-        x = wave_find(a.batch, tile, start);
-        t0 = a.q_off[x];
-        t1 = a.q_off[x + 1];
-        if (kPaged) {
-            n = a.own_len[x];
-            if (pages_of(n, a.pg.log_tokens) > a.own_width) return bad_seq(a, CR_ERR_SEQ);
-            it->table = a.own_table + (uint64_t)x * a.own_width;
-            it->causal = 1;
-        } else {
-            const uint32_t k0 = a.k_off[x], k1 = a.k_off[x + 1];
-            if (k0 > k1 || k1 > a.total_k) return bad_seq(a, CR_ERR_SEQ);
-            n = k1 - k0;
-            it->key0 = k0;
-            it->causal = a.causal;
-        }
-        tile -= min(start(x), tile);
+    uint32_t r0 = x, r1 = x + 1u;
+    if (kPaged && kind == kGroup) {
+        r0 = a.group_off[x];
+        r1 = a.group_off[x + 1u];
+        if (r0 > r1 || r1 > a.batch) return bad_seq(a);
     }
-    if (t0 > t1 || t1 > a.total_q) return bad_seq(a, CR_ERR_SEQ);
-    const uint32_t nq = t1 - t0, rows = nq * a.group;
-    it->row0 = tile * a.rows;
-    if (it->row0 >= rows) return false;
-    it->rows = min(a.rows, rows - it->row0);
-    it->tok0 = t0;
-    it->first_lim = it->causal ? (int32_t)n - (int32_t)nq + 1 : (int32_t)n;
-    uint32_t top = n;  // keys that the last row sees
-    if (it->causal) top = (uint32_t)max(0, it->first_lim + (int32_t)((it->row0 + it->rows - 1u) / a.group));
-    const uint32_t per = ((top + splits - 1u) / splits + kKeys - 1u) / kKeys * kKeys;
-    it->begin = min(top, split * per);
-    it->end = min(top, it->begin + per);
+    const uint32_t t0 = a.q_off[r0], t1 = a.q_off[r1];
+    if (t0 > t1 || t1 > a.total_q) return bad_seq(a);
+    s->tok0 = t0;
+    s->nq = t1 - t0;
+    s->least = 0;
+    if (!kPaged) {
+        const uint32_t k0 = a.k_off[x], k1 = a.k_off[x + 1u];
+        if (k0 > k1 || k1 > a.total_k) return bad_seq(a);
+        s->n = k1 - k0;
+        s->key0 = k0;
+        s->causal = a.causal;
+    } else {
+        uint32_t pre = 0, own = 0;
+        if (kind != kOwn) {
+            const uint32_t g = kind == kGroup ? x : wave_find(a.groups, x, [&](uint32_t i) { return a.group_off[i]; });
+            pre = a.prefix_len[g];
+            if (pages_of(pre, a.pg.log_tokens) > a.prefix_width) return bad_seq(a);
+            s->table0 = a.prefix_table + (uint64_t)g * a.prefix_width;
+        }
+        if (kind != kGroup) {
+            own = a.own_len[x];
+            if (pages_of(own, a.pg.log_tokens) > a.own_width) return bad_seq(a);
+            s->table1 = a.own_table + (uint64_t)x * a.own_width;
+        }
+        s->len0 = pre;
+        s->gap_end = (pre + kKeys - 1u) / kKeys * kKeys;
+        s->n = kind == kGroup ? pre : s->gap_end + own;
+        s->causal = kind != kGroup;
+        s->least = (int32_t)s->gap_end;
+    }
+    s->first_lim = s->causal ? (int32_t)s->n - (int32_t)s->nq + 1 : (int32_t)s->n;
     return true;
+}
+
+// Keys that row m of a sequence sees.
+__device__ __forceinline__ uint32_t row_limit(const Attn& a, const Seq& s, uint32_t m)
+{
+    return s.causal ? (uint32_t)max(s.least, s.first_lim + (int32_t)(m / a.group)) : s.n;
+}
+
+// Keys per chunk of a sequence of n keys, and the number of its chunks.
+constexpr uint32_t kChunkUnit = 128;
+__device__ __forceinline__ uint32_t chunk_of(uint32_t n, uint32_t chunk, uint32_t slots)
+{
+    return max(chunk, ((n + slots - 1u) / slots + kChunkUnit - 1u) / kChunkUnit * kChunkUnit);
+}
+
+__device__ __forceinline__ uint32_t chunks_of(uint32_t n, uint32_t chunk, uint32_t slots)
+{
+    const uint32_t c = chunk_of(n, chunk, slots);
+    return (n + c - 1u) / c;
 }
 
 // Tiles in LDS, in elements. Keys: pieces of 16 bytes, all rows of one piece together (a lane reads a
@@ -165,12 +173,10 @@ __device__ __forceinline__ bool find_item(const Attn& a, uint32_t id, Item* it)
 // shifted against the one before, so that the pieces of one row, which lie next to each other
 // in memory and are written together, fall on different banks. All reads of a tile are one lane
 // address and constants.
-constexpr uint32_t kKeyRun = kKeys * 8u + 8u;
-constexpr uint32_t kValRun = kKeys * 32u + 32u;
-template <int kDim>
-constexpr uint32_t kKeyTile = kDim / 8 * kKeyRun;
-template <int kDim>
-constexpr uint32_t kValTile = kDim / 32 * kValRun;
+constexpr uint32_t key_run(uint32_t keys) { return keys * 8u + 8u; }
+constexpr uint32_t val_run(uint32_t keys) { return keys * 32u + 32u; }
+constexpr uint32_t key_tile(uint32_t keys, uint32_t dim) { return dim / 8u * key_run(keys); }
+constexpr uint32_t val_tile(uint32_t keys, uint32_t dim) { return dim / 32u * val_run(keys); }
 
 __device__ __forceinline__ s16x4 read_tr(const uint16_t* p)
 {
@@ -191,68 +197,108 @@ __device__ __forceinline__ float both_sum(float x)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Tiles of keys and values on their way from memory to LDS: a thread moves one 16-byte piece of every
-// kStep-th row.
-template <int kDim, bool kPaged>
+// Tiles of kTile keys and values on their way from memory to LDS, moved by kMovers threads: each
+// moves one 16-byte piece of every kStep-th row.
+template <int kDim, bool kPaged, uint32_t kTile, uint32_t kMovers>
 struct Loader {
-    static constexpr uint32_t kPieces = kDim / 8, kStep = kThreads / kPieces, kPer = kKeys / kStep;
-    const uint16_t *kb, *vb;
-    uint32_t row, piece, end;
-    uint32_t page[kPer];  // of the next tile's rows
+    static constexpr uint32_t kPieces = kDim / 8, kStep = kMovers / kPieces, kPer = kTile / kStep;
+    static constexpr uint32_t kWaveRows = kWave / kPieces;  // rows that a wavefront moves at once
+    const uint16_t *kb, *vb;  // of the key head (prompt: at the sequence's first key)
+    uint32_t row, piece, end, lane_k, lane_v, bad;
+    uint32_t page[kPer];      // of the next tile's rows
     u32x4 rk[kPer], rv[kPer];
 
-    __device__ __forceinline__ void init(const Attn& a, const Item& it, uint32_t head_kv)
+    __device__ __forceinline__ void init(const Attn& a, const Seq& s, uint32_t head_kv, uint32_t last, uint32_t mover)
     {
-        piece = threadIdx.x % kPieces;
-        row = threadIdx.x / kPieces;
-        end = it.end;
+        piece = mover % kPieces;
+        row = mover / kPieces;
+        end = last;
+        bad = 0;
         if (kPaged) {
-            kb = a.pg.k + (int64_t)head_kv * a.pg.head_stride + piece * 8u;
-            vb = a.pg.v + (int64_t)head_kv * a.pg.head_stride + piece * 8u;
+            kb = a.pg.k + (int64_t)head_kv * a.pg.head_stride;
+            vb = a.pg.v + (int64_t)head_kv * a.pg.head_stride;
+            lane_k = lane_v = row % kWaveRows * (uint32_t)a.pg.token_stride + piece * 8u;
         } else {
-            kb = (const uint16_t*)a.k.p + (int64_t)head_kv * a.k.head_stride + (int64_t)it.key0 * a.k.token_stride + piece * 8u;
-            vb = (const uint16_t*)a.v.p + (int64_t)head_kv * a.v.head_stride + (int64_t)it.key0 * a.v.token_stride + piece * 8u;
+            kb = (const uint16_t*)a.k.p + (int64_t)head_kv * a.k.head_stride + (int64_t)s.key0 * a.k.token_stride;
+            vb = (const uint16_t*)a.v.p + (int64_t)head_kv * a.v.head_stride + (int64_t)s.key0 * a.v.token_stride;
+            lane_k = row % kWaveRows * (uint32_t)a.k.token_stride + piece * 8u;
+            lane_v = row % kWaveRows * (uint32_t)a.v.token_stride + piece * 8u;
         }
     }
-    // Rows behind the last key repeat it: their weights are 0, and nothing foreign is read.
-    __device__ __forceinline__ uint32_t key(uint32_t k0, uint32_t p) const { return min(k0 + p * kStep + row, end - 1u); }
-
-    __device__ __forceinline__ void pages(const Attn& a, const Item& it, uint32_t k0)
+    // The table of the tile at k0, its first key there, and the end of the keys in it.
+    __device__ __forceinline__ void place(const Seq& s, uint32_t k0, const uint32_t** table, uint32_t* first, uint32_t* last) const
+    {
+        const bool second = k0 >= s.gap_end && end > s.gap_end;
+        *table = second ? s.table1 : s.table0;
+        *first = second ? k0 - s.gap_end : k0;
+        *last = second ? end - s.gap_end : min(end, s.len0);
+    }
+    __device__ __forceinline__ void pages(const Attn& a, const Seq& s, uint32_t k0)
     {
         if (!kPaged) return;
+        const uint32_t* table;
+        uint32_t first, last;
+        place(s, k0, &table, &first, &last);
 #pragma unroll
-        for (uint32_t p = 0; p < kPer; ++p) page[p] = it.table[key(k0, p) >> a.pg.log_tokens];
+        for (uint32_t p = 0; p < kPer; ++p) page[p] = table[min(first + p * kStep + row, last - 1u) >> a.pg.log_tokens];
     }
-    __device__ __forceinline__ void load(const Attn& a, uint32_t k0)
+    // Whole tiles whose rows of one wavefront and pass lie in one page: scalar addresses. Otherwise an
+    // address per lane; rows behind the last key repeat it: their weights are 0, and nothing foreign is
+    // read.
+    __device__ __forceinline__ void load(const Attn& a, const Seq& s, uint32_t k0)
     {
+        const uint32_t mask = (1u << a.pg.log_tokens) - 1u;
+        const uint32_t* table = nullptr;
+        uint32_t first = k0, last = end;
+        if (kPaged) place(s, k0, &table, &first, &last);
+        if (first + kTile <= last && (!kPaged || mask >= kWaveRows - 1u)) {
+            const uint32_t r0 = __builtin_amdgcn_readfirstlane(row);
 #pragma unroll
-        for (uint32_t p = 0; p < kPer; ++p) {
-            const uint32_t j = key(k0, p);
-            int64_t ak, av;
-            if (kPaged) {
-                uint32_t g = page[p];
-                if (g >= a.pg.num_pages) {
-                    atomicOr(a.err, CR_ERR_PAGE);
-                    g = 0;
+            for (uint32_t p = 0; p < kPer; ++p) {
+                const uint32_t j = first + p * kStep + r0;
+                int64_t ak, av;
+                if (kPaged) {
+                    uint32_t g = __builtin_amdgcn_readfirstlane(page[p]);
+                    bad |= g >= a.pg.num_pages;
+                    g = min(g, a.pg.num_pages - 1u);
+                    ak = av = (int64_t)((uint64_t)g * (uint32_t)a.pg.page_stride + (uint64_t)(j & mask) * (uint32_t)a.pg.token_stride);
+                } else {
+                    ak = (int64_t)((uint64_t)j * (uint32_t)a.k.token_stride);
+                    av = (int64_t)((uint64_t)j * (uint32_t)a.v.token_stride);
                 }
-                ak = (int64_t)((uint64_t)g * (uint32_t)a.pg.page_stride) +
-                     (int64_t)((uint64_t)(j & ((1u << a.pg.log_tokens) - 1u)) * (uint32_t)a.pg.token_stride);
-                av = ak;
-            } else {
-                ak = (int64_t)((uint64_t)j * (uint32_t)a.k.token_stride);
-                av = (int64_t)((uint64_t)j * (uint32_t)a.v.token_stride);
+                rk[p] = *reinterpret_cast<const u32x4*>(kb + ak + lane_k);
+                rv[p] = *reinterpret_cast<const u32x4*>(vb + av + lane_v);
             }
-            rk[p] = *reinterpret_cast<const u32x4*>(kb + ak);
-            rv[p] = *reinterpret_cast<const u32x4*>(vb + av);
+        } else {
+#pragma unroll
+            for (uint32_t p = 0; p < kPer; ++p) {
+                const uint32_t j = min(first + p * kStep + row, last - 1u);
+                int64_t ak, av;
+                if (kPaged) {
+                    uint32_t g = page[p];
+                    bad |= g >= a.pg.num_pages;
+                    g = min(g, a.pg.num_pages - 1u);
+                    ak = av = (int64_t)((uint64_t)g * (uint32_t)a.pg.page_stride + (uint64_t)(j & mask) * (uint32_t)a.pg.token_stride);
+                } else {
+                    ak = (int64_t)((uint64_t)j * (uint32_t)a.k.token_stride);
+                    av = (int64_t)((uint64_t)j * (uint32_t)a.v.token_stride);
+                }
+                rk[p] = *reinterpret_cast<const u32x4*>(kb + ak + piece * 8u);
+                rv[p] = *reinterpret_cast<const u32x4*>(vb + av + piece * 8u);
+            }
         }
+    }
+    __device__ __forceinline__ void report(const Attn& a) const
+    {
+        if (kPaged && bad) atomicOr(a.err, CR_ERR_PAGE);
     }
     __device__ __forceinline__ void store(uint16_t* lk, uint16_t* lv) const
     {
 #pragma unroll
         for (uint32_t p = 0; p < kPer; ++p) {
             const uint32_t r = p * kStep + row;
-            *reinterpret_cast<u32x4*>(lk + piece * kKeyRun + r * 8u) = rk[p];
-            *reinterpret_cast<u32x4*>(lv + (piece >> 2) * kValRun + r * 32u + (piece & 3u) * 8u) = rv[p];
+            *reinterpret_cast<u32x4*>(lk + piece * key_run(kTile) + r * 8u) = rk[p];
+            *reinterpret_cast<u32x4*>(lv + (piece >> 2) * val_run(kTile) + r * 32u + (piece & 3u) * 8u) = rv[p];
         }
     }
 };
@@ -267,14 +313,30 @@ struct Loader {
 // next (matrix unit), then the values of the first beside the maximum of the next. The maximum is
 // moved, and what is summed rescaled, only when a score passes it by 2^kSlack.
 template <typename E, int kDim, bool kPaged, int kBlk>
-__global__ __launch_bounds__(kThreads, (kDim == 128 && kBlk == 2) ? 1 : 2) void k_attn(const Attn a)
+__global__ __launch_bounds__(kThreads, (kDim == 128 && kBlk == 2) ? 1 : 2) void k_attn(const Attn a, uint32_t kind, uint32_t tiles)
 {
-    __shared__ __align__(16) uint16_t lds_k[2][kKeyTile<kDim>];
-    __shared__ __align__(16) uint16_t lds_v[3][kValTile<kDim>];
+    constexpr uint32_t kRows = kWaves * 32u * kBlk;  // of the block
+    constexpr uint32_t kKeyRun = key_run(kKeys), kValRun = val_run(kKeys);
+    __shared__ __align__(16) uint16_t lds_k[2][key_tile(kKeys, kDim)];
+    __shared__ __align__(16) uint16_t lds_v[3][val_tile(kKeys, kDim)];
 
-    const uint32_t head_kv = blockIdx.x % a.heads_kv;
-    Item it;
-    if (!find_item<kPaged>(a, blockIdx.x / a.heads_kv, &it)) return;
+    // Tiles of sequence x start at floor(first row / kRows) + x: steps of at least ceil(rows / kRows),
+    // so the tiles of all sequences fit into floor(all rows / kRows) + sequences without a pass that
+    // counts them; some are empty. The last rows of causal sequences, the longest, come first.
+    const uint32_t head_kv = blockIdx.x % a.heads_kv, id = blockIdx.x / a.heads_kv;
+    const uint32_t slots = kind == kOwn ? a.own_slots : a.slots;
+    const uint32_t split = id / tiles, tile = tiles - 1u - id % tiles;  // tiles that read the same keys side by side
+    auto start = [&](uint32_t x) {
+        return a.q_off[kPaged && kind == kGroup ? min(a.group_off[x], a.batch) : x] * a.group / kRows + x;
+    };
+    const uint32_t x = wave_find(kPaged && kind == kGroup ? a.groups : a.batch, tile, start);
+    Seq it;
+    if (!get_seq<kPaged>(a, kind, x, &it)) return;
+    const uint32_t row0 = (tile - min(start(x), tile)) * kRows, seq_rows = it.nq * a.group;
+    if (row0 >= seq_rows) return;
+    const uint32_t rows = min(kRows, seq_rows - row0);
+    const uint32_t chunk = chunk_of(it.n, kind == kOwn ? a.own_chunk : a.chunk, slots), key_begin = split * chunk;
+    const uint32_t key_end = min(row_limit(a, it, row0 + rows - 1u), key_begin + chunk);
 
     const uint32_t lane = lane_id(), wv = wave_in_block(), half = lane >> 5, col = lane & 31u;
     const uint32_t wrow = wv * 32u * kBlk;  // the wave's first row
@@ -282,20 +344,16 @@ __global__ __launch_bounds__(kThreads, (kDim == 128 && kBlk == 2) ? 1 : 2) void 
     int32_t lim[kBlk];
 #pragma unroll
     for (int b = 0; b < kBlk; ++b) {
-        const uint32_t m = it.row0 + min(wrow + b * 32u + col, it.rows - 1u);
+        const uint32_t m = row0 + min(wrow + b * 32u + col, rows - 1u);
         tok[b] = it.tok0 + m / a.group;
         head[b] = head_kv * a.group + m % a.group;
-        lim[b] = it.causal ? min(it.first_lim + (int32_t)(m / a.group), (int32_t)it.end) : (int32_t)it.end;
+        lim[b] = (int32_t)min(row_limit(a, it, m), key_end);
     }
     // keys that the wave's last and first rows see
-    uint32_t w_end = 0, w_full = it.end;
-    if (wrow < it.rows) {
-        w_end = it.end;
-        if (it.causal) {
-            const uint32_t last = it.row0 + min(wrow + 32u * kBlk, it.rows) - 1u;
-            w_end = (uint32_t)min((int32_t)it.end, max(0, it.first_lim + (int32_t)(last / a.group)));
-            w_full = (uint32_t)min((int32_t)it.end, max(0, it.first_lim + (int32_t)((it.row0 + wrow) / a.group)));
-        }
+    uint32_t w_end = 0, w_full = key_end;
+    if (wrow < rows) {
+        w_end = min(row_limit(a, it, row0 + min(wrow + 32u * kBlk, rows) - 1u), key_end);
+        w_full = min(row_limit(a, it, row0 + wrow), key_end);
     }
 
     f32x16 o[kBlk][kDim / 32];
@@ -310,12 +368,12 @@ __global__ __launch_bounds__(kThreads, (kDim == 128 && kBlk == 2) ? 1 : 2) void 
             for (int i = 0; i < 16; ++i) o[b][d][i] = 0.f;
     }
 
-    if (it.begin < it.end) {
-        Loader<kDim, kPaged> ld;
-        ld.init(a, it, head_kv);
-        ld.pages(a, it, it.begin);
-        ld.load(a, it.begin);
-        ld.pages(a, it, it.begin + kKeys);
+    if (key_begin < key_end) {
+        Loader<kDim, kPaged, kKeys, kThreads> ld;
+        ld.init(a, it, head_kv, key_end, threadIdx.x);
+        ld.pages(a, it, key_begin);
+        ld.load(a, it, key_begin);
+        ld.pages(a, it, key_begin + kKeys);
         s16x8 qf[kBlk][kDim / 16];
 #pragma unroll
         for (int b = 0; b < kBlk; ++b) {
@@ -341,10 +399,18 @@ __global__ __launch_bounds__(kThreads, (kDim == 128 && kBlk == 2) ? 1 : 2) void 
         };
         auto mask = [&](uint32_t k0, int h) {
 #pragma unroll
-            for (int b = 0; b < kBlk; ++b)
+            for (int b = 0; b < kBlk; ++b) {
+                const int32_t l = kPaged && k0 < it.gap_end ? min(lim[b], (int32_t)it.len0) : lim[b];
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if ((int32_t)(k0 + h * 32u + 8u * (i / 4) + 4u * half + (i & 3)) >= lim[b]) s[h][b][i] = -INFINITY;
+                    if ((int32_t)(k0 + h * 32u + 8u * (i / 4) + 4u * half + (i & 3)) >= l) s[h][b][i] = -INFINITY;
+            }
+        };
+        // Whether every row of the wave sees the second half of the tile at k0 and the first of the next.
+        auto whole = [&](uint32_t k0) {
+            bool w = k0 + kKeys + 32u <= w_full;
+            if (kPaged) w = w && (k0 + kKeys + 32u <= it.len0 || k0 >= it.gap_end);
+            return w;
         };
         float top[kBlk];
         auto maxima = [&](int h) {
@@ -431,23 +497,22 @@ __global__ __launch_bounds__(kThreads, (kDim == 128 && kBlk == 2) ? 1 : 2) void 
             __builtin_amdgcn_sched_barrier(0);
         };
 
-        // Loads behind the last key repeat its row, so they need no branch.
         ld.store(lds_k[0], lds_v[0]);
-        ld.load(a, it.begin + kKeys);
-        ld.pages(a, it, it.begin + 2u * kKeys);
+        ld.load(a, it, key_begin + kKeys);
+        ld.pages(a, it, key_begin + 2u * kKeys);
         __syncthreads();
         scores(lds_k[0], 0);
-        mask(it.begin, 0);
+        mask(key_begin, 0);
         maxima(0);
         rescale();
-        uint32_t kbuf = 0, vbuf = 0, k0 = it.begin;
+        uint32_t kbuf = 0, vbuf = 0, k0 = key_begin;
         // The next tile into LDS, the one behind it into registers. The keys' buffer was last read before
         // the last barrier, the values' two tiles ago.
         auto stage = [&]() {
             kbuf ^= 1u;
             vbuf = vbuf == 2u ? 0u : vbuf + 1u;
-            if (k0 + kKeys < it.end) ld.store(lds_k[kbuf], lds_v[vbuf]);
-            ld.load(a, k0 + 2u * kKeys);
+            if (k0 + kKeys < key_end) ld.store(lds_k[kbuf], lds_v[vbuf]);
+            ld.load(a, it, k0 + 2u * kKeys);
             ld.pages(a, it, k0 + 3u * kKeys);
             __syncthreads();
         };
@@ -472,21 +537,29 @@ __global__ __launch_bounds__(kThreads, (kDim == 128 && kBlk == 2) ? 1 : 2) void 
             rescale();
             k0 += kKeys;
         };
-        while (k0 + 2u * kKeys <= w_full) tile(std::false_type{});
-        while (k0 < w_end) tile(std::true_type{});
-        for (; k0 < it.end; k0 += kKeys) stage();  // keys that only other waves' rows see
+        if (kPaged) {
+            while (k0 < w_end) {
+                while (whole(k0)) tile(std::false_type{});
+                tile(std::true_type{});
+            }
+        } else {
+            while (whole(k0)) tile(std::false_type{});
+            while (k0 < w_end) tile(std::true_type{});
+        }
+        for (; k0 < key_end; k0 += kKeys) stage();  // keys that only other waves' rows see
+        ld.report(a);
     }
 
 #pragma unroll
     for (int b = 0; b < kBlk; ++b) {
         const float total = both_sum(sum[b]);
-        if (wrow + b * 32u + col >= it.rows) continue;
+        if (wrow + b * 32u + col >= rows) continue;
         const bool none = total == 0.f;  // the largest weight of a row that sees a key is 1 or more
         const float inv = none ? 0.f : 1.f / total;
         const float lse2 = none ? -INFINITY : mc[b] + log2f(total);
         const uint64_t orow = (uint64_t)tok[b] * a.heads_q + head[b];
         if (a.part_o) {
-            const uint64_t at = (uint64_t)it.slot * a.total_q * a.heads_q + orow;
+            const uint64_t at = (uint64_t)(split + (kind == kOwn ? a.slots : 0u)) * a.total_q * a.heads_q + orow;
             if (half == 0) a.part_lse[at] = lse2;
             if (none) continue;
 #pragma unroll
@@ -508,47 +581,336 @@ __global__ __launch_bounds__(kThreads, (kDim == 128 && kBlk == 2) ? 1 : 2) void 
     }
 }
 
-// Joins the partial results of a row: 4 elements per thread.
-template <typename E, int kDim>
-__global__ __launch_bounds__(256) void k_attn_join(const Attn a)
+// Few rows: 32 rows a block, its wavefronts take tiles of 32 keys in turn, each with tiles of its
+// own in LDS and no barrier, and join their results at the end of an item. An item is one tile of
+// rows of one sequence over one chunk of its keys. The blocks stay and walk over the items of up to two
+// lists (prefixes of groups or prompts, own tokens of requests), which every wavefront finds by
+// counting the items of 64 sequences at a time.
+constexpr uint32_t kNarrowRows = 32, kNarrowKeys = 32;
+
+template <int kDim>
+constexpr uint32_t narrow_lds()  // elements per wavefront: tiles, then its sums [32][dim + 4] f32
 {
-    constexpr uint32_t kPer = kDim / 4;
-    const uint64_t rows = (uint64_t)a.total_q * a.heads_q;
-    const uint64_t x = (uint64_t)blockIdx.x * 256u + threadIdx.x, row = x / kPer;
-    if (row >= rows) return;
-    const uint32_t e = (uint32_t)(x % kPer) * 4u, slots = a.splits + a.own_splits;
-    float mx = -INFINITY;
-    for (uint32_t s = 0; s < slots; ++s) mx = fmaxf(mx, a.part_lse[s * rows + row]);
-    float sum = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    if (mx != -INFINITY) {
-        for (uint32_t s = 0; s < slots; ++s) {
-            const float l = a.part_lse[s * rows + row];
-            if (l == -INFINITY) continue;
-            const float w = __builtin_amdgcn_exp2f(l - mx);
-            const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + (s * rows + row) * kDim + e);
-            sum += w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(w, v[i], acc[i]);
-        }
-    }
-    const float inv = sum > 0.f ? 1.f / sum : (mx == -INFINITY ? 0.f : 1.f / sum);
-    const uint32_t tok = (uint32_t)(row / a.heads_q), head = (uint32_t)(row % a.heads_q);
-    uint16_t* op = (uint16_t*)a.out.p + (int64_t)tok * a.out.token_stride + (int64_t)head * a.out.head_stride + e;
-    *reinterpret_cast<uint2*>(op) = uint2{E::pack(acc[0] * inv, acc[1] * inv), E::pack(acc[2] * inv, acc[3] * inv)};
-    if (a.lse && e == 0) a.lse[row] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
+    const uint32_t tiles = key_tile(kNarrowKeys, kDim) + val_tile(kNarrowKeys, kDim), sums = kNarrowRows * (kDim + 4u) * 2u;
+    return tiles > sums ? tiles : sums;
 }
 
-// Keys a block should have at least where a call is split, and workgroups that fill the GPU.
-constexpr uint32_t kSplitKeys = 256, kSplitMax = 32;
-
-// Parts of `keys` so that `blocks` workgroups of one part each become enough to fill the GPU.
-inline uint32_t split_of(uint64_t blocks, uint64_t keys)
+template <typename E, int kDim, bool kPaged>
+__global__ __launch_bounds__(kThreads, 2) void k_attn_narrow(const Attn a, uint32_t lists)
 {
-    const uint64_t want = 512u / (blocks ? blocks : 1u), most = keys / kSplitKeys;
-    uint64_t s = want < most ? want : most;
-    s = s < kSplitMax ? s : kSplitMax;
-    return (uint32_t)(s ? s : 1u);
+    constexpr uint32_t kKeyRun = key_run(kNarrowKeys), kValRun = val_run(kNarrowKeys), kSumRow = kDim + 4u;
+    __shared__ __align__(16) uint16_t lds[kWaves][narrow_lds<kDim>()];
+    __shared__ float sh_max[kWaves][kNarrowRows], sh_sum[kWaves][kNarrowRows];
+
+    const uint32_t lane = lane_id(), wv = wave_in_block(), half = lane >> 5, col = lane & 31u;
+    const uint32_t head_kv = blockIdx.x % a.heads_kv;
+    uint16_t* lk = lds[wv];
+    uint16_t* lv = lk + key_tile(kNarrowKeys, kDim);
+    float* sums = reinterpret_cast<float*>(lk);
+
+    // Sequences 0 .. first_n of the first list, then those of the second. Items `base` and on belong to
+    // the 64 sequences from x0, of which a lane has one.
+    const uint32_t first_n = (lists & 1u) ? (kPaged ? a.groups : a.batch) : 0u;
+    const uint32_t all_n = first_n + ((lists & 2u) ? a.batch : 0u);
+    uint32_t x0 = 0, base = 0, count = 0, incl = 0, l_tok = 0, l_nq = 0, l_n = 0, l_key0 = 0;
+    auto counted = [&]() {
+        const uint32_t x = x0 + lane;
+        count = 0;
+        if (x < all_n) {
+            const bool own = x >= first_n;
+            const uint32_t y = own ? x - first_n : x;
+            uint32_t r0 = y, r1 = y + 1u;
+            if (kPaged && !own) {
+                r0 = a.group_off[y];
+                r1 = a.group_off[y + 1u];
+            }
+            bool ok = r0 <= r1 && r1 <= a.batch;
+            if (kPaged) {
+                l_n = own ? a.own_len[y] : a.prefix_len[y];
+                ok = ok && pages_of(l_n, a.pg.log_tokens) <= (own ? a.own_width : a.prefix_width);
+            } else {
+                const uint32_t k0 = a.k_off[y], k1 = a.k_off[y + 1u];
+                l_key0 = k0;
+                l_n = k1 - k0;
+                ok = ok && k0 <= k1 && k1 <= a.total_k;
+            }
+            if (ok) {
+                const uint32_t t0 = a.q_off[r0], t1 = a.q_off[r1];
+                l_tok = t0;
+                l_nq = t1 - t0;
+                ok = t0 <= t1 && t1 <= a.total_q;
+            }
+            // a sequence without keys has rows to write all the same
+            if (ok)
+                count = (l_nq * a.group + kNarrowRows - 1u) / kNarrowRows *
+                        max(1u, chunks_of(l_n, own ? a.own_chunk : a.chunk, own ? a.own_slots : a.slots));
+            else
+                atomicOr(a.err, CR_ERR_SEQ);
+        }
+        incl = wave_incl_scan_u32(count);
+    };
+    counted();
+    for (uint32_t id = blockIdx.x / a.heads_kv;; id += gridDim.x / a.heads_kv) {
+        while (id - base >= rdlane(incl, 63)) {
+            base += rdlane(incl, 63);
+            x0 += 64u;
+            if (x0 >= all_n) return;
+            counted();
+        }
+        const uint32_t l = (uint32_t)__builtin_ctzll(ballot(incl > id - base));
+        const uint32_t local = id - base - (rdlane(incl, l) - rdlane(count, l)), x = x0 + l;
+        const bool own = x >= first_n;
+        Seq it;
+        it.tok0 = rdlane(l_tok, l);
+        it.nq = rdlane(l_nq, l);
+        it.n = rdlane(l_n, l);
+        it.least = 0;
+        it.gap_end = 0;
+        it.len0 = 0;
+        if (kPaged) {
+            it.causal = own;
+            if (!own) it.len0 = it.gap_end = it.n;
+            it.table0 = a.prefix_table + (uint64_t)x * a.prefix_width;
+            it.table1 = a.own_table + (uint64_t)(x - first_n) * a.own_width;
+        } else {
+            it.causal = a.causal;
+            it.key0 = rdlane(l_key0, l);
+        }
+        it.first_lim = it.causal ? (int32_t)it.n - (int32_t)it.nq + 1 : (int32_t)it.n;
+        const uint32_t slots = own ? a.own_slots : a.slots;
+        const uint32_t chunk = chunk_of(it.n, own ? a.own_chunk : a.chunk, slots), chunks = max(1u, (it.n + chunk - 1u) / chunk);
+        const uint32_t split = local % chunks, row0 = local / chunks * kNarrowRows;
+        const uint32_t rows = min(kNarrowRows, it.nq * a.group - row0);
+        const uint32_t key_begin = split * chunk;
+        const uint32_t key_end = min(row_limit(a, it, row0 + rows - 1u), key_begin + chunk);
+        const uint32_t full = min(row_limit(a, it, row0), key_end);  // keys that every row sees
+        const uint32_t m = row0 + min(col, rows - 1u);
+        const uint32_t tok = it.tok0 + m / a.group, head = head_kv * a.group + m % a.group;
+        const int32_t lim = (int32_t)min(row_limit(a, it, m), key_end);
+
+        f32x16 o[kDim / 32];
+#pragma unroll
+        for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+        float mc = kNoMax, sum = 0.f;
+        uint32_t k0 = key_begin + wv * kNarrowKeys;
+        if (k0 < key_end) {
+            Loader<kDim, kPaged, kNarrowKeys, kWave> ld;
+            ld.init(a, it, head_kv, key_end, lane);
+            ld.pages(a, it, k0);
+            ld.load(a, it, k0);
+            ld.pages(a, it, k0 + kWaves * kNarrowKeys);
+            s16x8 qf[kDim / 16];
+            const uint16_t* qp = (const uint16_t*)a.q.p + (int64_t)tok * a.q.token_stride + (int64_t)head * a.q.head_stride;
+#pragma unroll
+            for (int s = 0; s < kDim / 16; ++s) qf[s] = *reinterpret_cast<const s16x8*>(qp + s * 16 + half * 8u);
+            const uint32_t k_lane = half * kKeyRun + col * 8u;
+            const uint32_t v_lane = (half * 4u + (lane & 15u) / 4u) * 32u + ((lane >> 4) & 1u) * 16u + (lane & 3u) * 4u;
+            for (; k0 < key_end; k0 += kWaves * kNarrowKeys) {
+                ld.store(lk, lv);
+                wave_lds_fence();
+                ld.load(a, it, k0 + kWaves * kNarrowKeys);
+                ld.pages(a, it, k0 + 2u * kWaves * kNarrowKeys);
+                f32x16 s;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+                for (int d = 0; d < kDim / 16; ++d)
+                    s = E::mfma(*reinterpret_cast<const s16x8*>(lk + k_lane + d * 2u * kKeyRun), qf[d], s);
+                if (k0 + kNarrowKeys > full) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if ((int32_t)(k0 + 8u * (i / 4) + 4u * half + (i & 3)) >= lim) s[i] = -INFINITY;
+                }
+                float top = __builtin_elementwise_maximum(s[0], s[1]);
+#pragma unroll
+                for (int i = 2; i < 16; i += 2)
+                    top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top, s[i]), s[i + 1]);
+                top = both_max(top) * a.c;
+                if (ballot(top > mc + kSlack)) {
+                    const float up = fmaxf(mc, top), f = __builtin_amdgcn_exp2f(mc - up);
+                    mc = up;
+                    sum *= f;
+#pragma unroll
+                    for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[d][i] *= f;
+                }
+                uint32_t pk[8];
+                float t[4];
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c, -mc));
+                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], a.c, -mc));
+                    t[i & 3] = i < 4 ? x : t[i & 3] + x;
+                    t[(i & 3) + 1] = i < 4 ? y : t[(i & 3) + 1] + y;
+                    pk[i / 2] = E::pack(x, y);
+                }
+                sum += (t[0] + t[1]) + (t[2] + t[3]);
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    const u32x4 w = {pk[ks * 4], pk[ks * 4 + 1], pk[ks * 4 + 2], pk[ks * 4 + 3]};
+#pragma unroll
+                    for (int d = 0; d < kDim / 32; ++d) {
+                        s16x4 vf[2];
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) vf[y] = read_tr(lv + v_lane + d * kValRun + (ks * 16u + y * 8u) * 32u);
+                        o[d] = E::mfma(__builtin_shufflevector(vf[0], vf[1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_bit_cast(s16x8, w), o[d]);
+                    }
+                }
+                wave_lds_fence();
+            }
+            ld.report(a);
+        }
+        sum = both_sum(sum);
+        if (half == 0) {
+            sh_max[wv][col] = mc;
+            sh_sum[wv][col] = sum;
+        }
+#pragma unroll
+        for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<f32x4*>(sums + col * kSumRow + d * 32 + 2 * i + half * 4u) = f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+        __syncthreads();
+        // 4 elements of a row per thread
+        for (uint32_t y = threadIdx.x; y < rows * (kDim / 4u); y += kThreads) {
+            const uint32_t r = y / (kDim / 4u), e = y % (kDim / 4u) * 4u, mm = row0 + r;
+            float mx = sh_max[0][r], total = 0.f;
+#pragma unroll
+            for (uint32_t w = 1; w < kWaves; ++w) mx = fmaxf(mx, sh_max[w][r]);
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (uint32_t w = 0; w < kWaves; ++w) {
+                const float f = __builtin_amdgcn_exp2f(sh_max[w][r] - mx);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds[w]) + r * kSumRow + e);
+                total = __builtin_fmaf(f, sh_sum[w][r], total);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(f, v[i], acc[i]);
+            }
+            const bool none = total == 0.f;
+            const float inv = none ? 0.f : 1.f / total, lse2 = none ? -INFINITY : mx + log2f(total);
+            const uint32_t ot = it.tok0 + mm / a.group, oh = head_kv * a.group + mm % a.group;
+            const uint64_t orow = (uint64_t)ot * a.heads_q + oh;
+            if (a.part_o) {
+                const uint64_t at = (uint64_t)(split + (own ? a.slots : 0u)) * a.total_q * a.heads_q + orow;
+                if (e == 0) {
+                    a.part_lse[at] = lse2;
+                    if (split == chunks - 1u)  // slots without a chunk
+                        for (uint32_t z = chunks; z < slots; ++z) a.part_lse[at + (uint64_t)(z - split) * a.total_q * a.heads_q] = -INFINITY;
+                }
+                *reinterpret_cast<f32x4*>(a.part_o + at * kDim + e) = acc * inv;
+            } else {
+                if (a.lse && e == 0) a.lse[orow] = lse2 * kLn2;
+                *reinterpret_cast<uint2*>((uint16_t*)a.out.p + (int64_t)ot * a.out.token_stride + (int64_t)oh * a.out.head_stride + e) =
+                    uint2{E::pack(acc[0] * inv, acc[1] * inv), E::pack(acc[2] * inv, acc[3] * inv)};
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Joins the partial results of a token's rows: 4 elements of a row per thread, kPar threads share the
+// slots of a row's elements.
+template <typename E, int kDim, uint32_t kPar>
+__global__ __launch_bounds__(kThreads) void k_attn_join(const Attn a)
+{
+    constexpr uint32_t kPer = kDim / 4, kGroup4 = kThreads / kPar;
+    __shared__ float sh[kPar > 1 ? kPar : 1][kPar > 1 ? kGroup4 : 1][6];
+    const uint32_t tok = blockIdx.x, slots = a.slots + a.own_slots;
+    const uint32_t x = blockIdx.y * kGroup4 + threadIdx.x % kGroup4, part = threadIdx.x / kGroup4;
+    const uint32_t head = x / kPer, e = x % kPer * 4u;
+    const bool ok = head < a.heads_q;
+    const uint64_t rows = (uint64_t)a.total_q * a.heads_q, row = (uint64_t)tok * a.heads_q + (ok ? head : 0u);
+    float mx = -INFINITY, sum = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (uint32_t i = part; i < slots; i += kPar) {
+        const uint64_t at = i * rows + row;
+        const float l = a.part_lse[at];
+        if (l == -INFINITY) continue;  // its elements may be unwritten
+        const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + at * kDim + e);
+        const float up = l > mx || l != l ? l : mx;
+        const float f = __builtin_amdgcn_exp2f(mx - up), w = __builtin_amdgcn_exp2f(l - up);
+        mx = up;
+        sum = __builtin_fmaf(sum, f, w);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) acc[y] = __builtin_fmaf(acc[y], f, w * v[y]);
+    }
+    if (kPar > 1) {
+        float* mine = sh[part][threadIdx.x % kGroup4];
+        mine[0] = mx;
+        mine[1] = sum;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) mine[2 + y] = acc[y];
+        __syncthreads();
+        if (part != 0) return;
+        for (uint32_t p = 1; p < kPar; ++p) {
+            const float* his = sh[p][threadIdx.x % kGroup4];
+            const float l = his[0];
+            if (l == -INFINITY) continue;
+            const float up = l > mx || l != l ? l : mx;
+            const float f = __builtin_amdgcn_exp2f(mx - up), w = __builtin_amdgcn_exp2f(l - up);
+            mx = up;
+            sum = __builtin_fmaf(sum, f, w * his[1]);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) acc[y] = __builtin_fmaf(acc[y], f, w * his[2 + y]);
+        }
+    }
+    if (!ok) return;
+    const bool none = mx == -INFINITY;
+    const float inv = none ? 0.f : 1.f / sum;
+    uint16_t* op = (uint16_t*)a.out.p + (int64_t)tok * a.out.token_stride + (int64_t)head * a.out.head_stride + e;
+    *reinterpret_cast<uint2*>(op) = uint2{E::pack(acc[0] * inv, acc[1] * inv), E::pack(acc[2] * inv, acc[3] * inv)};
+    if (a.lse && e == 0) a.lse[row] = none ? -INFINITY : (mx + log2f(sum)) * kLn2;
+}
+
+// How a call is cut: the wide kernels' launches, the lists of the narrow one, chunks and slots.
+struct Wide {
+    uint32_t kind, rows;  // rows per block
+};
+struct Shape {
+    Wide wide[2];
+    uint32_t wides, lists;  // lists of the narrow launch: 1 the first kind's, 2 own tokens
+    uint32_t first, chunk, slots, own_chunk, own_slots;
+    bool join;
+};
+
+constexpr uint32_t kFewRows = 64;        // mean rows of a sequence up to which the narrow kernel takes it
+constexpr uint32_t kWholeRows = 128;     // mean rows of a request from which its prefix is read again, not joined
+constexpr uint32_t kSplitKeys = 256;     // keys a workgroup should have at least where a call is split
+constexpr uint32_t kSplitMax = 32;
+constexpr uint32_t kNarrowItems = 1024;  // items of the narrow kernel that fill the GPU
+constexpr uint32_t kNarrowSlots = 128;
+
+inline uint32_t up_to(uint64_t x, uint32_t m) { return (uint32_t)((x + m - 1u) / m * m); }
+
+// Tiles that a call's rows make, about: whole ones, and one for each sequence's rest.
+inline uint64_t tiles_of(uint64_t rows, uint32_t per, uint32_t seqs) { return rows / per + (rows < (uint64_t)seqs * per ? seqs : 1u); }
+
+// Rows per block, and the chunks of sequences of about `keys` keys that make enough workgroups.
+inline Wide wide_shape(uint32_t kind, uint64_t rows, uint32_t seqs, uint32_t heads_kv, uint64_t keys, uint32_t* chunk, uint32_t* slots)
+{
+    uint64_t most = keys / kSplitKeys;
+    most = most < 1 ? 1 : (most < kSplitMax ? most : kSplitMax);
+    Wide w{kind, 128u};
+    if (rows >= 192ull * seqs && tiles_of(rows, 256, seqs) * heads_kv * most >= 256u) w.rows = 256u;
+    const uint64_t want = 512u / (tiles_of(rows, w.rows, seqs) * heads_kv);
+    *slots = (uint32_t)(want < 1 ? 1 : (want < most ? want : most));
+    *chunk = up_to(keys / *slots + 1u, kChunkUnit);
+    return w;
+}
+
+inline void narrow_shape(uint64_t rows, uint32_t seqs, uint32_t heads_kv, uint64_t keys, uint64_t most_keys, uint32_t* chunk,
+                         uint32_t* slots)
+{
+    const uint64_t total = tiles_of(rows, kNarrowRows, seqs) * heads_kv * keys;
+    uint64_t c = 256;
+    while (c < 4096 && c * 2u * kNarrowItems <= total) c *= 2u;
+    const uint64_t n = (most_keys + c - 1u) / c;
+    *chunk = (uint32_t)c;
+    *slots = (uint32_t)(n < 1 ? 1 : (n < kNarrowSlots ? n : kNarrowSlots));
 }
 
 inline bool good_scale(float s) { return s > 0.f && s <= 3.0e38f; }
@@ -566,63 +928,109 @@ inline bool good_shared_sizes(const cr_kv_cache* c, const cr_attn_shared_args* p
 {
     return good_cache_sizes(c) && p && good_heads(p->heads_q, c->heads) && p->layer < c->layers && good_scale(p->scale) &&
            (uint64_t)p->total_q * p->heads_q < (1ull << 31) && p->batch <= (1u << 24) && p->groups <= p->batch &&
-           (p->total_q == 0 || p->groups > 0) && ((uint64_t)p->prefix_width * c->page_tokens) < (1ull << 31) &&
-           ((uint64_t)p->own_width * c->page_tokens) < (1ull << 31);
+           (p->total_q == 0 || p->groups > 0) &&
+           ((uint64_t)p->prefix_width + p->own_width) * c->page_tokens < (1ull << 31);
 }
 
-// Query rows per block: 256 where the tiles of 256 fill the GPU by themselves, else 128.
-inline uint32_t rows_of(uint64_t rows, uint32_t heads_kv) { return rows * heads_kv >= 256ull * 256u ? 256u : 128u; }
-
-// Tiles that a call's rows make, about: whole ones, and one for each sequence's rest.
-inline uint64_t tiles_of(uint64_t rows, uint32_t per, uint32_t seqs) { return rows / per + (rows < (uint64_t)seqs * per ? seqs : 1u); }
-
-inline void prompt_shape(const cr_attn_prompt_args* p, uint32_t* per, uint32_t* splits)
+// Lengths are on the device: the mean stands for them, and a sequence's chunks grow where it is longer.
+inline Shape prompt_shape(const cr_attn_prompt_args* p)
 {
-    const uint64_t rows = (uint64_t)p->total_q * (p->heads_q / p->heads_kv);
-    *per = rows_of(rows, p->heads_kv);
-    *splits = p->total_q ? split_of(tiles_of(rows, *per, p->batch) * p->heads_kv, p->total_k / p->batch) : 1u;
+    Shape s{};
+    s.first = kPrompt;
+    const uint64_t rows = (uint64_t)p->total_q * (p->heads_q / p->heads_kv), keys = p->total_k / p->batch;
+    if (rows <= (uint64_t)kFewRows * p->batch) {
+        s.lists = 1;
+        narrow_shape(rows, p->batch, p->heads_kv, keys, p->batch > 1 ? 2 * keys : keys, &s.chunk, &s.slots);
+    } else {
+        s.wide[s.wides++] = wide_shape(kPrompt, rows, p->batch, p->heads_kv, keys, &s.chunk, &s.slots);
+    }
+    s.join = s.slots > 1;
+    return s;
 }
 
-inline void shared_shape(const cr_kv_cache* c, const cr_attn_shared_args* p, uint32_t* per, uint32_t* prefix, uint32_t* own)
+// Here the tables' widths stand for the lengths.
+inline Shape shared_shape(const cr_kv_cache* c, const cr_attn_shared_args* p)
 {
+    Shape s{};
     const uint64_t rows = (uint64_t)p->total_q * (p->heads_q / c->heads);
-    *per = rows_of(rows, c->heads);
-    *prefix = split_of(tiles_of(rows, *per, p->groups) * c->heads, (uint64_t)p->prefix_width * c->page_tokens);
-    *own = split_of(tiles_of(rows, *per, p->batch) * c->heads, (uint64_t)p->own_width * c->page_tokens);
+    const uint64_t prefix = (uint64_t)p->prefix_width * c->page_tokens, own = (uint64_t)p->own_width * c->page_tokens;
+    if (rows >= (uint64_t)kWholeRows * p->batch) {
+        s.first = kWhole;
+        s.wide[s.wides++] = wide_shape(kWhole, rows, p->batch, c->heads, prefix + own, &s.chunk, &s.slots);
+        s.join = s.slots > 1;
+        return s;
+    }
+    s.first = kGroup;
+    if (rows <= (uint64_t)kFewRows * p->groups) {
+        s.lists |= 1u;
+        narrow_shape(rows, p->groups, c->heads, prefix, prefix, &s.chunk, &s.slots);
+    } else {
+        s.wide[s.wides++] = wide_shape(kGroup, rows, p->groups, c->heads, prefix, &s.chunk, &s.slots);
+    }
+    if (rows <= (uint64_t)kFewRows * p->batch) {
+        s.lists |= 2u;
+        narrow_shape(rows, p->batch, c->heads, own, own, &s.own_chunk, &s.own_slots);
+    } else {
+        s.wide[s.wides++] = wide_shape(kOwn, rows, p->batch, c->heads, own, &s.own_chunk, &s.own_slots);
+    }
+    s.join = true;
+    return s;
 }
 
-inline size_t part_bytes(uint64_t slots, uint64_t rows, uint32_t dim) { return slots * rows * (dim + 4u) * sizeof(float); }
-
-inline void set_parts(Attn* a, void* ws, uint64_t slots, uint32_t dim)
+inline size_t part_bytes(const Shape& s, uint64_t rows, uint32_t dim)
 {
-    a->part_o = (float*)ws;
-    a->part_lse = a->part_o + slots * a->total_q * a->heads_q * dim;
+    return s.join ? ((uint64_t)s.slots + s.own_slots) * rows * (dim + 1u) * sizeof(float) : 0;
 }
 
 template <typename E, int kDim, bool kPaged>
-void launch(const Attn& a, hipStream_t st)
+void launch(const Attn& a, const Shape& s, hipStream_t st)
 {
-    const uint64_t items = (uint64_t)a.tiles * a.splits + (uint64_t)a.own_tiles * a.own_splits;
-    const dim3 grid((uint32_t)(items * a.heads_kv));
-    if (a.rows == 256u) hipLaunchKernelGGL((k_attn<E, kDim, kPaged, 2>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((k_attn<E, kDim, kPaged, 1>), grid, dim3(kThreads), 0, st, a);
-    if (a.part_o) {
-        const uint64_t threads = (uint64_t)a.total_q * a.heads_q * (kDim / 4);
-        hipLaunchKernelGGL((k_attn_join<E, kDim>), dim3((uint32_t)((threads + 255u) / 256u)), dim3(256), 0, st, a);
+    const uint64_t rows = (uint64_t)a.total_q * a.group;
+    for (uint32_t i = 0; i < s.wides; ++i) {
+        const Wide& w = s.wide[i];
+        const uint32_t tiles = (uint32_t)(rows / w.rows) + (w.kind == kGroup ? a.groups : a.batch);
+        const dim3 grid(tiles * (w.kind == kOwn ? a.own_slots : a.slots) * a.heads_kv);
+        if (w.rows == 256u) hipLaunchKernelGGL((k_attn<E, kDim, kPaged, 2>), grid, dim3(kThreads), 0, st, a, w.kind, tiles);
+        else hipLaunchKernelGGL((k_attn<E, kDim, kPaged, 1>), grid, dim3(kThreads), 0, st, a, w.kind, tiles);
+    }
+    if (s.lists) {
+        uint64_t items = 0;
+        if (s.lists & 1u) items += (rows / kNarrowRows + (kPaged ? a.groups : a.batch)) * a.slots;
+        if (s.lists & 2u) items += (rows / kNarrowRows + a.batch) * a.own_slots;
+        const uint64_t most = (2u * (uint64_t)device_cus() + a.heads_kv - 1u) / a.heads_kv;
+        const dim3 grid((uint32_t)(items < most ? items : most) * a.heads_kv);
+        hipLaunchKernelGGL((k_attn_narrow<E, kDim, kPaged>), grid, dim3(kThreads), 0, st, a, s.lists);
+    }
+    if (s.join) {
+        constexpr uint32_t kPer = kDim / 4;
+        if (s.slots + s.own_slots > 8u)
+            hipLaunchKernelGGL((k_attn_join<E, kDim, 8>), dim3(a.total_q, (a.heads_q * kPer + 31u) / 32u), dim3(kThreads), 0, st, a);
+        else
+            hipLaunchKernelGGL((k_attn_join<E, kDim, 1>), dim3(a.total_q, (a.heads_q * kPer + 255u) / 256u), dim3(kThreads), 0, st, a);
     }
 }
 
 template <bool kPaged>
-cr_status dispatch(const Attn& a, uint32_t dtype, uint32_t dim, void* stream)
+cr_status dispatch(Attn& a, const Shape& s, void* ws, uint32_t dtype, uint32_t dim, void* stream)
 {
     const hipStream_t st = as_stream(stream);
-    const uint64_t items = (uint64_t)a.tiles * a.splits + (uint64_t)a.own_tiles * a.own_splits;
-    if (items * a.heads_kv >= (1ull << 31)) return CR_EINVAL;
+    const uint64_t rows = (uint64_t)a.total_q * a.group;
+    for (uint32_t i = 0; i < s.wides; ++i)
+        if ((rows / s.wide[i].rows + a.batch) * (s.wide[i].kind == kOwn ? s.own_slots : s.slots) * a.heads_kv >= (1ull << 31)) return CR_EINVAL;
+    a.first = s.first;
+    a.chunk = s.chunk;
+    a.slots = s.slots;
+    a.own_chunk = s.own_chunk;
+    a.own_slots = s.own_slots;
+    if (s.join) {
+        a.part_o = (float*)ws;
+        a.part_lse = a.part_o + ((uint64_t)s.slots + s.own_slots) * a.total_q * a.heads_q * dim;
+    }
     (void)hipGetLastError();
-    if (dtype == CR_BF16 && dim == 128) launch<Bf16, 128, kPaged>(a, st);
-    else if (dtype == CR_BF16) launch<Bf16, 64, kPaged>(a, st);
-    else if (dim == 128) launch<F16, 128, kPaged>(a, st);
-    else launch<F16, 64, kPaged>(a, st);
+    if (dtype == CR_BF16 && dim == 128) launch<Bf16, 128, kPaged>(a, s, st);
+    else if (dtype == CR_BF16) launch<Bf16, 64, kPaged>(a, s, st);
+    else if (dim == 128) launch<F16, 128, kPaged>(a, s, st);
+    else launch<F16, 64, kPaged>(a, s, st);
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
 }
 
@@ -632,10 +1040,8 @@ cr_status dispatch(const Attn& a, uint32_t dtype, uint32_t dim, void* stream)
 extern "C" size_t cr_attn_prompt_workspace_bytes(const cr_attn_prompt_args* p)
 {
     using namespace cr;
-    if (!good_prompt_sizes(p)) return 0;
-    uint32_t per, s;
-    prompt_shape(p, &per, &s);
-    return s > 1 ? part_bytes(s, (uint64_t)p->total_q * p->heads_q, p->dim) : 0;
+    if (!good_prompt_sizes(p) || p->total_q == 0) return 0;
+    return part_bytes(prompt_shape(p), (uint64_t)p->total_q * p->heads_q, p->dim);
 }
 
 extern "C" cr_status cr_attn_prompt(const cr_attn_prompt_args* p, void* ws, size_t ws_bytes, uint32_t* err, void* stream)
@@ -646,7 +1052,8 @@ extern "C" cr_status cr_attn_prompt(const cr_attn_prompt_args* p, void* ws, size
     if (!good_rows(p->q) || !good_rows(p->out) || !p->q_off || !p->k_off ||
         (p->total_k > 0 && (!good_rows(p->k) || !good_rows(p->v))) || (p->lse && !aligned4(p->lse)))
         return CR_EINVAL;
-    const size_t need = cr_attn_prompt_workspace_bytes(p);
+    const Shape s = prompt_shape(p);
+    const size_t need = part_bytes(s, (uint64_t)p->total_q * p->heads_q, p->dim);
     if (need && (!ws || !aligned16(ws))) return CR_EINVAL;
     if (ws_bytes < need) return CR_ESIZE;
     Attn a{};
@@ -665,20 +1072,15 @@ extern "C" cr_status cr_attn_prompt(const cr_attn_prompt_args* p, void* ws, size
     a.total_k = p->total_k;
     a.causal = p->causal;
     a.c = p->scale * kLog2e;
-    prompt_shape(p, &a.rows, &a.splits);
-    a.tiles = (uint32_t)((uint64_t)p->total_q * a.group / a.rows) + p->batch;
-    if (a.splits > 1) set_parts(&a, ws, a.splits, p->dim);
     a.err = err;
-    return dispatch<false>(a, p->dtype, p->dim, stream);
+    return dispatch<false>(a, s, ws, p->dtype, p->dim, stream);
 }
 
 extern "C" size_t cr_attn_shared_workspace_bytes(const cr_kv_cache* c, const cr_attn_shared_args* p)
 {
     using namespace cr;
-    if (!good_shared_sizes(c, p)) return 0;
-    uint32_t per, s1, s2;
-    shared_shape(c, p, &per, &s1, &s2);
-    return part_bytes((uint64_t)s1 + s2, (uint64_t)p->total_q * p->heads_q, c->dim);
+    if (!good_shared_sizes(c, p) || p->total_q == 0) return 0;
+    return part_bytes(shared_shape(c, p), (uint64_t)p->total_q * p->heads_q, c->dim);
 }
 
 extern "C" cr_status cr_attn_shared(const cr_kv_cache* c, const cr_attn_shared_args* p, void* ws, size_t ws_bytes,
@@ -688,10 +1090,12 @@ extern "C" cr_status cr_attn_shared(const cr_kv_cache* c, const cr_attn_shared_a
     if (!good_cache(c) || !good_shared_sizes(c, p) || !err) return CR_EINVAL;
     if (p->total_q == 0) return CR_OK;
     if (!good_rows(p->q) || !good_rows(p->out) || !p->q_off || !p->group_off || !p->prefix_len || !p->own_len ||
-        (p->prefix_width && !p->prefix_table) || (p->own_width && !p->own_table) || (p->lse && !aligned4(p->lse)) || !ws ||
-        !aligned16(ws))
+        (p->prefix_width && !p->prefix_table) || (p->own_width && !p->own_table) || (p->lse && !aligned4(p->lse)))
         return CR_EINVAL;
-    if (ws_bytes < cr_attn_shared_workspace_bytes(c, p)) return CR_ESIZE;
+    const Shape s = shared_shape(c, p);
+    const size_t need = part_bytes(s, (uint64_t)p->total_q * p->heads_q, c->dim);
+    if (need && (!ws || !aligned16(ws))) return CR_EINVAL;
+    if (ws_bytes < need) return CR_ESIZE;
     Attn a{};
     a.q = p->q;
     a.out = p->out;
@@ -714,11 +1118,6 @@ extern "C" cr_status cr_attn_shared(const cr_kv_cache* c, const cr_attn_shared_a
     a.groups = p->groups;
     a.total_q = p->total_q;
     a.c = p->scale * kLog2e;
-    shared_shape(c, p, &a.rows, &a.splits, &a.own_splits);
-    const uint64_t rows = (uint64_t)p->total_q * a.group;
-    a.tiles = (uint32_t)(rows / a.rows) + p->groups;
-    a.own_tiles = (uint32_t)(rows / a.rows) + p->batch;
-    set_parts(&a, ws, (uint64_t)a.splits + a.own_splits, c->dim);
     a.err = err;
-    return dispatch<true>(a, c->dtype, c->dim, stream);
+    return dispatch<true>(a, s, ws, c->dtype, c->dim, stream);
 }
