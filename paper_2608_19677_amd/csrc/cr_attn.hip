@@ -9,6 +9,9 @@
 
 #include <type_traits>
 
+// Code of the tile loops is inlined whatever its size: its arrays live in registers only so.
+#define CR_INLINE __attribute__((always_inline))
+
 namespace cr {
 namespace {
 
@@ -184,11 +187,18 @@ __device__ __forceinline__ s16x4 read_tr(const uint16_t* p)
         (__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) void*)const_cast<uint16_t*>(p));
 }
 
+// Keeps the computation of x here: the compiler would move it past the next branch, to its first use.
+template <typename T>
+__device__ __forceinline__ void stay(T& x)
+{
+    asm volatile("" : "+v"(x));
+}
+
 // The larger of a column's values in the two half-waves, and their sum.
 __device__ __forceinline__ float both_max(float x)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    return __builtin_elementwise_maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 __device__ __forceinline__ float both_sum(float x)
@@ -303,22 +313,28 @@ struct Loader {
     }
 };
 
-// A wavefront keeps 32 kBlk rows, each in one column: S^T = K Q^T gives a lane its row's scores of 16
-// of 32 keys (the other half-wave has the other 16), so the row's maximum needs one exchange, and
-// the weights are the second operand of O^T = V^T P^T as they lie: the order of keys inside a
+// A wavefront keeps 32 rows, each in one column: S^T = K Q^T gives a lane its row's scores of 16 of 32
+// keys (the other half-wave has the other 16), so the row's maximum needs one exchange, and the
+// weights are the second operand of O^T = V^T P^T as they lie: the order of keys inside a
 // product is the same on both sides, 4 + 4 of 16 per half-wave, which is what two transposed LDS
 // reads of the values give.
 //
-// The wave works on half tiles of 32 keys: the weights of one (vector unit) beside the scores of the
-// next (matrix unit), then the values of the first beside the maximum of the next. The maximum is
-// moved, and what is summed rescaled, only when a score passes it by 2^kSlack.
-template <typename E, int kDim, bool kPaged, int kBlk>
-__global__ __launch_bounds__(kThreads, (kDim == 128 && kBlk == 2) ? 1 : 2) void k_attn(const Attn a, uint32_t kind, uint32_t tiles)
+// The wave works on half tiles of 32 keys, three of them at a time: the scores of the next and the
+// values of the last on the matrix unit, and between these products the weights of the one between
+// and the maximum of the next on the vector unit. The maximum is moved, and what is summed rescaled,
+// only when a score passes it by 2^kSlack.
+//
+// kW wavefronts share the tiles. Eight (256 rows) read a tile from memory for twice the rows that four
+// do; four are for sequences of fewer rows. Values have three buffers where a block has a compute
+// unit to itself (one barrier per tile), else two and a barrier more.
+template <typename E, int kDim, bool kPaged, uint32_t kW>
+__global__ __launch_bounds__(kW * kWave, 2) void k_attn(const Attn a, uint32_t kind, uint32_t tiles)
 {
-    constexpr uint32_t kRows = kWaves * 32u * kBlk;  // of the block
+    constexpr uint32_t kRows = kW * 32u;  // of the block
     constexpr uint32_t kKeyRun = key_run(kKeys), kValRun = val_run(kKeys);
+    constexpr uint32_t kValBufs = kW == 8u ? 3u : 2u;
     __shared__ __align__(16) uint16_t lds_k[2][key_tile(kKeys, kDim)];
-    __shared__ __align__(16) uint16_t lds_v[3][val_tile(kKeys, kDim)];
+    __shared__ __align__(16) uint16_t lds_v[kValBufs][val_tile(kKeys, kDim)];
 
     // Tiles of sequence x start at floor(first row / kRows) + x: steps of at least ceil(rows / kRows),
     // so the tiles of all sequences fit into floor(all rows / kRows) + sequences without a pass that
@@ -339,246 +355,224 @@ __global__ __launch_bounds__(kThreads, (kDim == 128 && kBlk == 2) ? 1 : 2) void 
     const uint32_t key_end = min(row_limit(a, it, row0 + rows - 1u), key_begin + chunk);
 
     const uint32_t lane = lane_id(), wv = wave_in_block(), half = lane >> 5, col = lane & 31u;
-    const uint32_t wrow = wv * 32u * kBlk;  // the wave's first row
-    uint32_t tok[kBlk], head[kBlk];
-    int32_t lim[kBlk];
-#pragma unroll
-    for (int b = 0; b < kBlk; ++b) {
-        const uint32_t m = row0 + min(wrow + b * 32u + col, rows - 1u);
-        tok[b] = it.tok0 + m / a.group;
-        head[b] = head_kv * a.group + m % a.group;
-        lim[b] = (int32_t)min(row_limit(a, it, m), key_end);
-    }
+    const uint32_t wrow = wv * 32u;  // the wave's first row
+    const uint32_t m = row0 + min(wrow + col, rows - 1u);
+    const uint32_t tok = it.tok0 + m / a.group, head = head_kv * a.group + m % a.group;
+    const int32_t lim = (int32_t)min(row_limit(a, it, m), key_end);
     // keys that the wave's last and first rows see
     uint32_t w_end = 0, w_full = key_end;
     if (wrow < rows) {
-        w_end = min(row_limit(a, it, row0 + min(wrow + 32u * kBlk, rows) - 1u), key_end);
+        w_end = min(row_limit(a, it, row0 + min(wrow + 32u, rows) - 1u), key_end);
         w_full = min(row_limit(a, it, row0 + wrow), key_end);
     }
 
-    f32x16 o[kBlk][kDim / 32];
-    float mc[kBlk], sum[kBlk];
+    f32x16 o[kDim / 32];
+    float mc = kNoMax, sum = 0.f;
 #pragma unroll
-    for (int b = 0; b < kBlk; ++b) {
-        mc[b] = kNoMax;
-        sum[b] = 0.f;
+    for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
-        for (int d = 0; d < kDim / 32; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[b][d][i] = 0.f;
-    }
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
     if (key_begin < key_end) {
-        Loader<kDim, kPaged, kKeys, kThreads> ld;
+        Loader<kDim, kPaged, kKeys, kW * kWave> ld;
         ld.init(a, it, head_kv, key_end, threadIdx.x);
         ld.pages(a, it, key_begin);
         ld.load(a, it, key_begin);
         ld.pages(a, it, key_begin + kKeys);
-        s16x8 qf[kBlk][kDim / 16];
+        constexpr int kSteps = kDim / 16;  // products of a half tile's scores, and of its values
+        s16x8 qf[kSteps];
+        const uint16_t* qp = (const uint16_t*)a.q.p + (int64_t)tok * a.q.token_stride + (int64_t)head * a.q.head_stride;
 #pragma unroll
-        for (int b = 0; b < kBlk; ++b) {
-            const uint16_t* qp = (const uint16_t*)a.q.p + (int64_t)tok[b] * a.q.token_stride + (int64_t)head[b] * a.q.head_stride;
-#pragma unroll
-            for (int s = 0; s < kDim / 16; ++s) qf[b][s] = *reinterpret_cast<const s16x8*>(qp + s * 16 + half * 8u);
-        }
-        f32x16 s[2][kBlk];
+        for (int s = 0; s < kSteps; ++s) qf[s] = *reinterpret_cast<const s16x8*>(qp + s * 16 + half * 8u);
 
-        // scores of half tile h (keys 32 h ..) of the tile in lk, into s[h]
-        const uint32_t k_lane = half * kKeyRun + col * 8u, v_lane = (half * 4u + (lane & 15u) / 4u) * 32u + ((lane >> 4) & 1u) * 16u + (lane & 3u) * 4u;
-        auto scores = [&](const uint16_t* lk, int h) {
-#pragma unroll
-            for (int b = 0; b < kBlk; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[h][b][i] = 0.f;
-#pragma unroll
-            for (int d = 0; d < kDim / 16; ++d) {
-                const s16x8 kf = *reinterpret_cast<const s16x8*>(lk + k_lane + d * 2u * kKeyRun + h * 32u * 8u);
-#pragma unroll
-                for (int b = 0; b < kBlk; ++b) s[h][b] = E::mfma(kf, qf[b][d], s[h][b]);
-            }
+        f32x16 s[2];            // scores of the two halves of a tile
+        uint32_t pk[2][8];      // their weights
+        float top, part[2];
+        float late = 1.f;       // factor that o lacks: its values come a half tile after their weights
+        bool is_late = false;
+        const uint32_t k_lane = half * kKeyRun + col * 8u;
+        const uint32_t v_lane = (half * 4u + (lane & 15u) / 4u) * 32u + ((lane >> 4) & 1u) * 16u + (lane & 3u) * 4u;
+
+        // Fragment d of half tile h of the keys in lk; fragment n of the values in lv: 16 keys
+        // n / (kDim / 32) by 32 elements n % (kDim / 32).
+        auto key_frag = [&](const uint16_t* lk, int h, int d) CR_INLINE {
+            return *reinterpret_cast<const s16x8*>(lk + k_lane + d * 2u * kKeyRun + h * 32u * 8u);
         };
-        auto mask = [&](uint32_t k0, int h) {
+        auto val_frag = [&](const uint16_t* lv, int h, int n) CR_INLINE {
+            const uint16_t* p = lv + v_lane + n % (kDim / 32) * kValRun + (h * 32u + n / (kDim / 32) * 16u) * 32u;
+            const s16x4 x = read_tr(p), y = read_tr(p + 8u * 32u);
+            return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        auto mask = [&](uint32_t k0, int h) CR_INLINE {
+            const int32_t l = kPaged && k0 < it.gap_end ? min(lim, (int32_t)it.len0) : lim;
 #pragma unroll
-            for (int b = 0; b < kBlk; ++b) {
-                const int32_t l = kPaged && k0 < it.gap_end ? min(lim[b], (int32_t)it.len0) : lim[b];
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if ((int32_t)(k0 + h * 32u + 8u * (i / 4) + 4u * half + (i & 3)) >= l) s[h][b][i] = -INFINITY;
-            }
+            for (int i = 0; i < 16; ++i)
+                if ((int32_t)(k0 + h * 32u + 8u * (i / 4) + 4u * half + (i & 3)) >= l) s[h][i] = -INFINITY;
         };
         // Whether every row of the wave sees the second half of the tile at k0 and the first of the next.
-        auto whole = [&](uint32_t k0) {
+        auto whole = [&](uint32_t k0) CR_INLINE {
             bool w = k0 + kKeys + 32u <= w_full;
             if (kPaged) w = w && (k0 + kKeys + 32u <= it.len0 || k0 >= it.gap_end);
             return w;
         };
-        float top[kBlk];
-        auto maxima = [&](int h) {
+        auto maximum = [&](int h, int i) CR_INLINE {  // over scores i and i + 1
+            top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(i ? top : s[h][i], s[h][i]), s[h][i + 1]);
+        };
+        auto scale_o = [&](float f) CR_INLINE {
 #pragma unroll
-            for (int b = 0; b < kBlk; ++b) {
-                float t = __builtin_elementwise_maximum(s[h][b][0], s[h][b][1]);
+            for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
-                for (int i = 2; i < 16; i += 2)
-                    t = __builtin_elementwise_maximum(__builtin_elementwise_maximum(t, s[h][b][i]), s[h][b][i + 1]);
-                top[b] = both_max(t) * a.c;
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        };
+        auto move_maximum = [&]() CR_INLINE {
+            top = both_max(top) * a.c;
+            stay(top);
+            if (is_late) {
+                scale_o(late);
+                is_late = false;
+            }
+            if (ballot(top > mc + kSlack)) {
+                const float up = fmaxf(mc, top);
+                late = __builtin_amdgcn_exp2f(mc - up);
+                is_late = true;
+                sum *= late;
+                mc = up;
             }
         };
-        auto rescale = [&]() {
-            bool up = false;
-#pragma unroll
-            for (int b = 0; b < kBlk; ++b) up |= top[b] > mc[b] + kSlack;
-            if (!ballot(up)) return;
-#pragma unroll
-            for (int b = 0; b < kBlk; ++b) {
-                const float m = fmaxf(mc[b], top[b]), f = __builtin_amdgcn_exp2f(mc[b] - m);
-                mc[b] = m;
-                sum[b] *= f;
-#pragma unroll
-                for (int d = 0; d < kDim / 32; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[b][d][i] *= f;
-            }
+        auto weight = [&](int h, int i) CR_INLINE {  // of scores i and i + 1
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i], a.c, -mc));
+            const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i + 1], a.c, -mc));
+            part[0] = i ? part[0] + x : x;
+            part[1] = i ? part[1] + y : y;
+            pk[h][i / 2] = E::pack(x, y);
+            stay(pk[h][i / 2]);
         };
-        uint32_t pk[kBlk][8];
-        auto weights = [&](int h) {
-#pragma unroll
-            for (int b = 0; b < kBlk; ++b) {
-                float t[4];
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][b][i], a.c, -mc[b]));
-                    const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][b][i + 1], a.c, -mc[b]));
-                    t[i & 3] = i < 4 ? x : t[i & 3] + x;
-                    t[(i & 3) + 1] = i < 4 ? y : t[(i & 3) + 1] + y;
-                    pk[b][i / 2] = E::pack(x, y);
-                }
-                sum[b] += (t[0] + t[1]) + (t[2] + t[3]);
-            }
+        auto value = [&](s16x8 vf, int h, int n) CR_INLINE {
+            const int ks = n / (kDim / 32), d = n % (kDim / 32);
+            const u32x4 w = {pk[h][ks * 4], pk[h][ks * 4 + 1], pk[h][ks * 4 + 2], pk[h][ks * 4 + 3]};
+            o[d] = E::mfma(vf, __builtin_bit_cast(s16x8, w), o[d]);
         };
-        auto values = [&](const uint16_t* lv, int h) {
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-                for (int d = 0; d < kDim / 32; ++d) {
-                    s16x4 vf[2];
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) vf[y] = read_tr(lv + v_lane + d * kValRun + (h * 32u + ks * 16u + y * 8u) * 32u);
-#pragma unroll
-                    for (int b = 0; b < kBlk; ++b) {
-                        const u32x4 w = {pk[b][ks * 4], pk[b][ks * 4 + 1], pk[b][ks * 4 + 2], pk[b][ks * 4 + 3]};
-                        o[b][d] = E::mfma(__builtin_shufflevector(vf[0], vf[1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_bit_cast(s16x8, w), o[b][d]);
-                    }
-                }
-        };
-
-        // Order of instructions: every matrix product with its share of vector work behind it, the
-        // fragments read two products ahead.
-        auto order_scores = [&]() {
-            constexpr int kSteps = kDim / 16, kTrans = 16 * kBlk / kSteps, kVec = 40 * kBlk / kSteps;
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        // Scores of half h of the keys in lk (of the tile at k0), weights of the other half, values (in lv) of
+        // half h before that. The order stands as written: fragments are read two products ahead, 5 of the 8
+        // pairs of weights lie between the products of scores, 3 and the maximum between those of values.
+        auto half_tile = [&](const uint16_t* lk, const uint16_t* lv, int h, uint32_t k0, auto masked, auto has_last) CR_INLINE {
+            constexpr int kEarly = 5;
+            s16x8 kf[kSteps + 2], vf[kSteps + 2];
+            kf[0] = key_frag(lk, h, 0);
+            kf[1] = key_frag(lk, h, 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int d = 0; d < kSteps; ++d) {
-                __builtin_amdgcn_sched_group_barrier(0x008, kBlk, 0);
-                __builtin_amdgcn_sched_group_barrier(0x400, kTrans, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, kVec, 0);
-                if (d + 2 < kSteps) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        auto order_values = [&]() {
-            constexpr int kSteps = kDim / 16;
-            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+                if (d + 2 < kSteps) kf[d + 2] = key_frag(lk, h, d + 2);
+                else if (has_last) vf[d + 2 - kSteps] = val_frag(lv, h, d + 2 - kSteps);
+                if (d == 0) {
 #pragma unroll
-            for (int d = 0; d < kSteps; ++d) {
-                __builtin_amdgcn_sched_group_barrier(0x008, kBlk, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 2 * kBlk, 0);
-                if (d + 2 < kSteps) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                    for (int i = 0; i < 16; ++i) s[h][i] = 0.f;
+                }
+                s[h] = E::mfma(kf[d], qf[d], s[h]);
+#pragma unroll
+                for (int i = d * kEarly / kSteps; i < (d + 1) * kEarly / kSteps; ++i) weight(h ^ 1, 2 * i);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < kSteps; ++n) {
+                if (has_last) {
+                    if (n + 2 < kSteps) vf[n + 2] = val_frag(lv, h, n + 2);
+                    value(vf[n], h, n);
+                }
+                if (n == 1 && masked) mask(k0, h);
+                if (n < kSteps / 2) {
+#pragma unroll
+                    for (int i = kEarly + n * (8 - kEarly) * 2 / kSteps; i < kEarly + (n + 1) * (8 - kEarly) * 2 / kSteps; ++i) weight(h ^ 1, 2 * i);
+                } else {
+#pragma unroll
+                    for (int i = (n - kSteps / 2) * 16 / kSteps; i < (n - kSteps / 2 + 1) * 16 / kSteps; ++i) maximum(h, 2 * i);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            sum += part[0] + part[1];
+            stay(sum);
+            move_maximum();
         };
 
         ld.store(lds_k[0], lds_v[0]);
         ld.load(a, it, key_begin + kKeys);
         ld.pages(a, it, key_begin + 2u * kKeys);
         __syncthreads();
-        scores(lds_k[0], 0);
-        mask(key_begin, 0);
-        maxima(0);
-        rescale();
         uint32_t kbuf = 0, vbuf = 0, k0 = key_begin;
+        const uint16_t* lv_last = lds_v[0];
         // The next tile into LDS, the one behind it into registers. The keys' buffer was last read before
-        // the last barrier, the values' two tiles ago.
-        auto stage = [&]() {
+        // the last barrier, the values' one barrier and a half tile earlier.
+        auto stage = [&]() CR_INLINE {
             kbuf ^= 1u;
-            vbuf = vbuf == 2u ? 0u : vbuf + 1u;
+            vbuf = vbuf + 1u == kValBufs ? 0u : vbuf + 1u;
+            if (kValBufs == 2u) __syncthreads();
             if (k0 + kKeys < key_end) ld.store(lds_k[kbuf], lds_v[vbuf]);
             ld.load(a, it, k0 + 2u * kKeys);
             ld.pages(a, it, k0 + 3u * kKeys);
             __syncthreads();
         };
-        auto tile = [&](auto masked) {
+        auto tile_of = [&](auto masked, auto has_last) CR_INLINE {
             const uint16_t* lv = lds_v[vbuf];
-            scores(lds_k[kbuf], 1);
-            weights(0);
-            order_scores();
-            if (masked) mask(k0, 1);
-            values(lv, 0);
-            maxima(1);
-            order_values();
-            rescale();
+            half_tile(lds_k[kbuf], lv_last, 1, k0, masked, has_last);
             stage();
-            scores(lds_k[kbuf], 0);  // behind the last tile: of whatever lies there, all masked
-            weights(1);
-            order_scores();
-            if (masked) mask(k0 + kKeys, 0);
-            values(lv, 1);
-            maxima(0);
-            order_values();
-            rescale();
+            half_tile(lds_k[kbuf], lv, 0, k0 + kKeys, masked, std::true_type{});  // behind the last tile: of what lies there, masked
+            lv_last = lv;
             k0 += kKeys;
         };
-        if (kPaged) {
-            while (k0 < w_end) {
-                while (whole(k0)) tile(std::false_type{});
-                tile(std::true_type{});
+        if (k0 < w_end) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
+#pragma unroll
+            for (int d = 0; d < kSteps; ++d) s[0] = E::mfma(key_frag(lds_k[0], 0, d), qf[d], s[0]);
+            mask(k0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) maximum(0, i);
+            move_maximum();
+            tile_of(std::true_type{}, std::false_type{});
+            if (kPaged) {
+                while (k0 < w_end) {
+                    while (whole(k0)) tile_of(std::false_type{}, std::true_type{});
+                    tile_of(std::true_type{}, std::true_type{});
+                }
+            } else {
+                while (whole(k0)) tile_of(std::false_type{}, std::true_type{});
+                while (k0 < w_end) tile_of(std::true_type{}, std::true_type{});
             }
-        } else {
-            while (whole(k0)) tile(std::false_type{});
-            while (k0 < w_end) tile(std::true_type{});
+#pragma unroll
+            for (int n = 0; n < kSteps; ++n) value(val_frag(lv_last, 1, n), 1, n);
+            if (is_late) scale_o(late);
         }
         for (; k0 < key_end; k0 += kKeys) stage();  // keys that only other waves' rows see
         ld.report(a);
     }
 
-#pragma unroll
-    for (int b = 0; b < kBlk; ++b) {
-        const float total = both_sum(sum[b]);
-        if (wrow + b * 32u + col >= rows) continue;
-        const bool none = total == 0.f;  // the largest weight of a row that sees a key is 1 or more
-        const float inv = none ? 0.f : 1.f / total;
-        const float lse2 = none ? -INFINITY : mc[b] + log2f(total);
-        const uint64_t orow = (uint64_t)tok[b] * a.heads_q + head[b];
-        if (a.part_o) {
-            const uint64_t at = (uint64_t)(split + (kind == kOwn ? a.slots : 0u)) * a.total_q * a.heads_q + orow;
-            if (half == 0) a.part_lse[at] = lse2;
-            if (none) continue;
-#pragma unroll
-            for (int d = 0; d < kDim / 32; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    *reinterpret_cast<f32x4*>(a.part_o + at * kDim + d * 32 + 2 * i + half * 4u) =
-                        f32x4{o[b][d][i] * inv, o[b][d][i + 1] * inv, o[b][d][i + 2] * inv, o[b][d][i + 3] * inv};
-            continue;
-        }
-        if (a.lse && half == 0) a.lse[orow] = lse2 * kLn2;
-        uint16_t* op = (uint16_t*)a.out.p + (int64_t)tok[b] * a.out.token_stride + (int64_t)head[b] * a.out.head_stride;
+    const float total = both_sum(sum);
+    if (wrow + col >= rows) return;
+    const bool none = total == 0.f;  // the largest weight of a row that sees a key is 2^-kSlack or more
+    const float inv = none ? 0.f : 1.f / total;
+    const float lse2 = none ? -INFINITY : mc + log2f(total);
+    const uint64_t orow = (uint64_t)tok * a.heads_q + head;
+    if (a.part_o) {
+        const uint64_t at = (uint64_t)(split + (kind == kOwn ? a.slots : 0u)) * a.total_q * a.heads_q + orow;
+        if (half == 0) a.part_lse[at] = lse2;
+        if (none) return;
 #pragma unroll
         for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<uint2*>(op + d * 32 + 2 * i + half * 4u) =
-                    uint2{E::pack(o[b][d][i] * inv, o[b][d][i + 1] * inv), E::pack(o[b][d][i + 2] * inv, o[b][d][i + 3] * inv)};
+                *reinterpret_cast<f32x4*>(a.part_o + at * kDim + d * 32 + 2 * i + half * 4u) =
+                    f32x4{o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
+        return;
     }
+    if (a.lse && half == 0) a.lse[orow] = lse2 * kLn2;
+    uint16_t* op = (uint16_t*)a.out.p + (int64_t)tok * a.out.token_stride + (int64_t)head * a.out.head_stride;
+#pragma unroll
+    for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<uint2*>(op + d * 32 + 2 * i + half * 4u) =
+                uint2{E::pack(o[d][i] * inv, o[d][i + 1] * inv), E::pack(o[d][i + 2] * inv, o[d][i + 3] * inv)};
 }
 
 // Few rows: 32 rows a block, its wavefronts take tiles of 32 keys in turn, each with tiles of its
@@ -990,8 +984,8 @@ void launch(const Attn& a, const Shape& s, hipStream_t st)
         const Wide& w = s.wide[i];
         const uint32_t tiles = (uint32_t)(rows / w.rows) + (w.kind == kGroup ? a.groups : a.batch);
         const dim3 grid(tiles * (w.kind == kOwn ? a.own_slots : a.slots) * a.heads_kv);
-        if (w.rows == 256u) hipLaunchKernelGGL((k_attn<E, kDim, kPaged, 2>), grid, dim3(kThreads), 0, st, a, w.kind, tiles);
-        else hipLaunchKernelGGL((k_attn<E, kDim, kPaged, 1>), grid, dim3(kThreads), 0, st, a, w.kind, tiles);
+        if (w.rows == 256u) hipLaunchKernelGGL((k_attn<E, kDim, kPaged, 8>), grid, dim3(8 * kWave), 0, st, a, w.kind, tiles);
+        else hipLaunchKernelGGL((k_attn<E, kDim, kPaged, 4>), grid, dim3(4 * kWave), 0, st, a, w.kind, tiles);
     }
     if (s.lists) {
         uint64_t items = 0;
