@@ -327,19 +327,29 @@ struct Loader {
 // kW wavefronts share the tiles. Eight (256 rows) read a tile from memory for twice the rows that four
 // do; four are for sequences of fewer rows. Values have three buffers where a block has a compute
 // unit to itself (one barrier per tile), else two and a barrier more.
+struct Part {
+    uint32_t kind, tiles, blocks;  // blocks: tiles x slots x key heads
+};
+
+constexpr uint32_t val_bufs(uint32_t waves) { return waves == 8u ? 3u : 2u; }
+constexpr uint32_t wide_lds(uint32_t waves, uint32_t dim)  // elements
+{
+    return 2u * key_tile(kKeys, dim) + val_bufs(waves) * val_tile(kKeys, dim);
+}
+
 template <typename E, int kDim, bool kPaged, uint32_t kW>
-__global__ __launch_bounds__(kW * kWave, 2) void k_attn(const Attn a, uint32_t kind, uint32_t tiles)
+__device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_t block, uint16_t* lds)
 {
     constexpr uint32_t kRows = kW * 32u;  // of the block
-    constexpr uint32_t kKeyRun = key_run(kKeys), kValRun = val_run(kKeys);
-    constexpr uint32_t kValBufs = kW == 8u ? 3u : 2u;
-    __shared__ __align__(16) uint16_t lds_k[2][key_tile(kKeys, kDim)];
-    __shared__ __align__(16) uint16_t lds_v[kValBufs][val_tile(kKeys, kDim)];
+    constexpr uint32_t kKeyRun = key_run(kKeys), kValRun = val_run(kKeys), kValBufs = val_bufs(kW);
+    auto lds_k = [&](uint32_t i) CR_INLINE { return lds + i * key_tile(kKeys, kDim); };
+    auto lds_v = [&](uint32_t i) CR_INLINE { return lds + 2u * key_tile(kKeys, kDim) + i * val_tile(kKeys, kDim); };
+    const uint32_t kind = part_of.kind, tiles = part_of.tiles;
 
     // Tiles of sequence x start at floor(first row / kRows) + x: steps of at least ceil(rows / kRows),
     // so the tiles of all sequences fit into floor(all rows / kRows) + sequences without a pass that
     // counts them; some are empty. The last rows of causal sequences, the longest, come first.
-    const uint32_t head_kv = blockIdx.x % a.heads_kv, id = blockIdx.x / a.heads_kv;
+    const uint32_t head_kv = block % a.heads_kv, id = block / a.heads_kv;
     const uint32_t slots = kind == kOwn ? a.own_slots : a.slots;
     const uint32_t split = id / tiles, tile = tiles - 1u - id % tiles;  // tiles that read the same keys side by side
     auto start = [&](uint32_t x) {
@@ -495,28 +505,28 @@ __global__ __launch_bounds__(kW * kWave, 2) void k_attn(const Attn a, uint32_t k
             move_maximum();
         };
 
-        ld.store(lds_k[0], lds_v[0]);
+        ld.store(lds_k(0), lds_v(0));
         ld.load(a, it, key_begin + kKeys);
         ld.pages(a, it, key_begin + 2u * kKeys);
         __syncthreads();
         uint32_t kbuf = 0, vbuf = 0, k0 = key_begin;
-        const uint16_t* lv_last = lds_v[0];
+        const uint16_t* lv_last = lds_v(0);
         // The next tile into LDS, the one behind it into registers. The keys' buffer was last read before
         // the last barrier, the values' one barrier and a half tile earlier.
         auto stage = [&]() CR_INLINE {
             kbuf ^= 1u;
             vbuf = vbuf + 1u == kValBufs ? 0u : vbuf + 1u;
             if (kValBufs == 2u) __syncthreads();
-            if (k0 + kKeys < key_end) ld.store(lds_k[kbuf], lds_v[vbuf]);
+            if (k0 + kKeys < key_end) ld.store(lds_k(kbuf), lds_v(vbuf));
             ld.load(a, it, k0 + 2u * kKeys);
             ld.pages(a, it, k0 + 3u * kKeys);
             __syncthreads();
         };
         auto tile_of = [&](auto masked, auto has_last) CR_INLINE {
-            const uint16_t* lv = lds_v[vbuf];
-            half_tile(lds_k[kbuf], lv_last, 1, k0, masked, has_last);
+            const uint16_t* lv = lds_v(vbuf);
+            half_tile(lds_k(kbuf), lv_last, 1, k0, masked, has_last);
             stage();
-            half_tile(lds_k[kbuf], lv, 0, k0 + kKeys, masked, std::true_type{});  // behind the last tile: of what lies there, masked
+            half_tile(lds_k(kbuf), lv, 0, k0 + kKeys, masked, std::true_type{});  // behind the last tile: of what lies there, masked
             lv_last = lv;
             k0 += kKeys;
         };
@@ -524,7 +534,7 @@ __global__ __launch_bounds__(kW * kWave, 2) void k_attn(const Attn a, uint32_t k
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
 #pragma unroll
-            for (int d = 0; d < kSteps; ++d) s[0] = E::mfma(key_frag(lds_k[0], 0, d), qf[d], s[0]);
+            for (int d = 0; d < kSteps; ++d) s[0] = E::mfma(key_frag(lds_k(0), 0, d), qf[d], s[0]);
             mask(k0, 0);
 #pragma unroll
             for (int i = 0; i < 16; i += 2) maximum(0, i);
@@ -575,6 +585,13 @@ __global__ __launch_bounds__(kW * kWave, 2) void k_attn(const Attn a, uint32_t k
                 uint2{E::pack(o[d][i] * inv, o[d][i + 1] * inv), E::pack(o[d][i + 2] * inv, o[d][i + 3] * inv)};
 }
 
+template <typename E, int kDim, bool kPaged>
+__global__ __launch_bounds__(8 * kWave, 2) void k_attn_wide(const Attn a, const Part p)
+{
+    __shared__ __align__(16) uint16_t lds[wide_lds(8, kDim)];
+    wide_block<E, kDim, kPaged, 8>(a, p, blockIdx.x, lds);
+}
+
 // Few rows: 32 rows a block, its wavefronts take tiles of 32 keys in turn, each with tiles of its
 // own in LDS and no barrier, and join their results at the end of an item. An item is one tile of
 // rows of one sequence over one chunk of its keys. The blocks stay and walk over the items of up to two
@@ -590,15 +607,14 @@ constexpr uint32_t narrow_lds()  // elements per wavefront: tiles, then its sums
 }
 
 template <typename E, int kDim, bool kPaged>
-__global__ __launch_bounds__(kThreads, 2) void k_attn_narrow(const Attn a, uint32_t lists)
+__device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t block, uint32_t blocks, uint16_t* lds,
+                                       float (*sh_max)[kNarrowRows], float (*sh_sum)[kNarrowRows])
 {
     constexpr uint32_t kKeyRun = key_run(kNarrowKeys), kValRun = val_run(kNarrowKeys), kSumRow = kDim + 4u;
-    __shared__ __align__(16) uint16_t lds[kWaves][narrow_lds<kDim>()];
-    __shared__ float sh_max[kWaves][kNarrowRows], sh_sum[kWaves][kNarrowRows];
 
     const uint32_t lane = lane_id(), wv = wave_in_block(), half = lane >> 5, col = lane & 31u;
-    const uint32_t head_kv = blockIdx.x % a.heads_kv;
-    uint16_t* lk = lds[wv];
+    const uint32_t head_kv = block % a.heads_kv;
+    uint16_t* lk = lds + wv * narrow_lds<kDim>();
     uint16_t* lv = lk + key_tile(kNarrowKeys, kDim);
     float* sums = reinterpret_cast<float*>(lk);
 
@@ -644,7 +660,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_narrow(const Attn a, uint3
         incl = wave_incl_scan_u32(count);
     };
     counted();
-    for (uint32_t id = blockIdx.x / a.heads_kv;; id += gridDim.x / a.heads_kv) {
+    for (uint32_t id = block / a.heads_kv;; id += blocks / a.heads_kv) {
         while (id - base >= rdlane(incl, 63)) {
             base += rdlane(incl, 63);
             x0 += 64u;
@@ -778,7 +794,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_narrow(const Attn a, uint3
 #pragma unroll
             for (uint32_t w = 0; w < kWaves; ++w) {
                 const float f = __builtin_amdgcn_exp2f(sh_max[w][r] - mx);
-                const f32x4 v = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds[w]) + r * kSumRow + e);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds + w * narrow_lds<kDim>()) + r * kSumRow + e);
                 total = __builtin_fmaf(f, sh_sum[w][r], total);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(f, v[i], acc[i]);
@@ -802,6 +818,23 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn_narrow(const Attn a, uint3
             }
         }
         __syncthreads();
+    }
+}
+
+// One launch of what is not wide: tiles of 128 rows (up to two parts) and the narrow lists' blocks,
+// so that neither waits for the other's last.
+template <typename E, int kDim, bool kPaged>
+__global__ __launch_bounds__(kThreads, 2) void k_attn_mixed(const Attn a, const Part p0, const Part p1, uint32_t lists)
+{
+    constexpr uint32_t kWide = wide_lds(kWaves, kDim), kNarrow = kWaves * narrow_lds<kDim>();
+    __shared__ __align__(16) uint16_t lds[kWide > kNarrow ? kWide : kNarrow];
+    __shared__ float sh_max[kWaves][kNarrowRows], sh_sum[kWaves][kNarrowRows];
+    const uint32_t wides = p0.blocks + p1.blocks;
+    if (blockIdx.x < wides) {
+        const bool second = blockIdx.x >= p0.blocks;
+        wide_block<E, kDim, kPaged, kWaves>(a, second ? p1 : p0, second ? blockIdx.x - p0.blocks : blockIdx.x, lds);
+    } else {
+        narrow_block<E, kDim, kPaged>(a, lists, blockIdx.x - wides, gridDim.x - wides, lds, sh_max, sh_sum);
     }
 }
 
@@ -873,7 +906,7 @@ struct Shape {
 
 constexpr uint32_t kFewRows = 64;        // mean rows of a sequence up to which the narrow kernel takes it
 constexpr uint32_t kWholeRows = 128;     // mean rows of a request from which its prefix is read again, not joined
-constexpr uint32_t kSplitKeys = 256;     // keys a workgroup should have at least where a call is split
+constexpr uint32_t kSplitKeys = 128;     // keys a workgroup should have at least where a call is split
 constexpr uint32_t kSplitMax = 32;
 constexpr uint32_t kNarrowItems = 1024;  // items of the narrow kernel that fill the GPU
 constexpr uint32_t kNarrowSlots = 128;
@@ -881,17 +914,33 @@ constexpr uint32_t kNarrowSlots = 128;
 inline uint32_t up_to(uint64_t x, uint32_t m) { return (uint32_t)((x + m - 1u) / m * m); }
 
 // Tiles that a call's rows make, about: whole ones, and one for each sequence's rest.
-inline uint64_t tiles_of(uint64_t rows, uint32_t per, uint32_t seqs) { return rows / per + (rows < (uint64_t)seqs * per ? seqs : 1u); }
+inline uint64_t tiles_of(uint64_t rows, uint32_t per, uint32_t seqs)
+{
+    return seqs == 1u ? (rows + per - 1u) / per : rows / per + (rows < (uint64_t)seqs * per ? seqs : seqs / 2u);
+}
 
-// Rows per block, and the chunks of sequences of about `keys` keys that make enough workgroups.
-inline Wide wide_shape(uint32_t kind, uint64_t rows, uint32_t seqs, uint32_t heads_kv, uint64_t keys, uint32_t* chunk, uint32_t* slots)
+// Rows per block, and the chunks of sequences of about `keys` keys. Blocks of 256 rows have a compute
+// unit each, two of 128 share one. More chunks fill the last round of blocks better and cost a start each
+// (about four tiles) and a join (a row's 8 dim bytes written and read again, about as long as 500
+// bytes take a tile's time per block); the number with the least estimated time is taken.
+inline Wide wide_shape(uint32_t kind, uint64_t rows, uint32_t seqs, uint32_t heads_kv, uint64_t keys, uint32_t dim, uint32_t* chunk,
+                       uint32_t* slots)
 {
     uint64_t most = keys / kSplitKeys;
     most = most < 1 ? 1 : (most < kSplitMax ? most : kSplitMax);
     Wide w{kind, 128u};
     if (rows >= 192ull * seqs && tiles_of(rows, 256, seqs) * heads_kv * most >= 256u) w.rows = 256u;
-    const uint64_t want = 512u / (tiles_of(rows, w.rows, seqs) * heads_kv);
-    *slots = (uint32_t)(want < 1 ? 1 : (want < most ? want : most));
+    const uint64_t blocks = tiles_of(rows, w.rows, seqs) * heads_kv, room = w.rows == 256u ? 256u : 512u;
+    const double tile_us = dim == 128 ? 2.0 : 1.2;
+    double least = 0;
+    for (uint64_t s = 1; s <= most; ++s) {
+        const double rounds = (double)((blocks * s + room - 1u) / room), tiles = (double)((keys + kKeys * s - 1u) / (kKeys * s));
+        const double us = rounds * (tiles + 4.0) * tile_us + (s > 1 ? 4.0 + (double)(s * rows * heads_kv * dim) * 8.0 / 4.0e6 : 0.0);
+        if (s == 1 || us < least) {
+            least = us;
+            *slots = (uint32_t)s;
+        }
+    }
     *chunk = up_to(keys / *slots + 1u, kChunkUnit);
     return w;
 }
@@ -936,7 +985,7 @@ inline Shape prompt_shape(const cr_attn_prompt_args* p)
         s.lists = 1;
         narrow_shape(rows, p->batch, p->heads_kv, keys, p->batch > 1 ? 2 * keys : keys, &s.chunk, &s.slots);
     } else {
-        s.wide[s.wides++] = wide_shape(kPrompt, rows, p->batch, p->heads_kv, keys, &s.chunk, &s.slots);
+        s.wide[s.wides++] = wide_shape(kPrompt, rows, p->batch, p->heads_kv, keys, p->dim, &s.chunk, &s.slots);
     }
     s.join = s.slots > 1;
     return s;
@@ -950,7 +999,7 @@ inline Shape shared_shape(const cr_kv_cache* c, const cr_attn_shared_args* p)
     const uint64_t prefix = (uint64_t)p->prefix_width * c->page_tokens, own = (uint64_t)p->own_width * c->page_tokens;
     if (rows >= (uint64_t)kWholeRows * p->batch) {
         s.first = kWhole;
-        s.wide[s.wides++] = wide_shape(kWhole, rows, p->batch, c->heads, prefix + own, &s.chunk, &s.slots);
+        s.wide[s.wides++] = wide_shape(kWhole, rows, p->batch, c->heads, prefix + own, c->dim, &s.chunk, &s.slots);
         s.join = s.slots > 1;
         return s;
     }
@@ -959,13 +1008,13 @@ inline Shape shared_shape(const cr_kv_cache* c, const cr_attn_shared_args* p)
         s.lists |= 1u;
         narrow_shape(rows, p->groups, c->heads, prefix, prefix, &s.chunk, &s.slots);
     } else {
-        s.wide[s.wides++] = wide_shape(kGroup, rows, p->groups, c->heads, prefix, &s.chunk, &s.slots);
+        s.wide[s.wides++] = wide_shape(kGroup, rows, p->groups, c->heads, prefix, c->dim, &s.chunk, &s.slots);
     }
     if (rows <= (uint64_t)kFewRows * p->batch) {
         s.lists |= 2u;
         narrow_shape(rows, p->batch, c->heads, own, own, &s.own_chunk, &s.own_slots);
     } else {
-        s.wide[s.wides++] = wide_shape(kOwn, rows, p->batch, c->heads, own, &s.own_chunk, &s.own_slots);
+        s.wide[s.wides++] = wide_shape(kOwn, rows, p->batch, c->heads, own, c->dim, &s.own_chunk, &s.own_slots);
     }
     s.join = true;
     return s;
@@ -980,21 +1029,24 @@ template <typename E, int kDim, bool kPaged>
 void launch(const Attn& a, const Shape& s, hipStream_t st)
 {
     const uint64_t rows = (uint64_t)a.total_q * a.group;
+    Part few[2] = {};
+    uint32_t fews = 0;
     for (uint32_t i = 0; i < s.wides; ++i) {
         const Wide& w = s.wide[i];
-        const uint32_t tiles = (uint32_t)(rows / w.rows) + (w.kind == kGroup ? a.groups : a.batch);
-        const dim3 grid(tiles * (w.kind == kOwn ? a.own_slots : a.slots) * a.heads_kv);
-        if (w.rows == 256u) hipLaunchKernelGGL((k_attn<E, kDim, kPaged, 8>), grid, dim3(8 * kWave), 0, st, a, w.kind, tiles);
-        else hipLaunchKernelGGL((k_attn<E, kDim, kPaged, 4>), grid, dim3(4 * kWave), 0, st, a, w.kind, tiles);
+        Part p{w.kind, (uint32_t)(rows / w.rows) + (w.kind == kGroup ? a.groups : a.batch), 0};
+        p.blocks = p.tiles * (w.kind == kOwn ? a.own_slots : a.slots) * a.heads_kv;
+        if (w.rows == 256u) hipLaunchKernelGGL((k_attn_wide<E, kDim, kPaged>), dim3(p.blocks), dim3(8 * kWave), 0, st, a, p);
+        else few[fews++] = p;
     }
+    uint32_t blocks = few[0].blocks + few[1].blocks;
     if (s.lists) {
         uint64_t items = 0;
         if (s.lists & 1u) items += (rows / kNarrowRows + (kPaged ? a.groups : a.batch)) * a.slots;
         if (s.lists & 2u) items += (rows / kNarrowRows + a.batch) * a.own_slots;
         const uint64_t most = (2u * (uint64_t)device_cus() + a.heads_kv - 1u) / a.heads_kv;
-        const dim3 grid((uint32_t)(items < most ? items : most) * a.heads_kv);
-        hipLaunchKernelGGL((k_attn_narrow<E, kDim, kPaged>), grid, dim3(kThreads), 0, st, a, s.lists);
+        blocks += (uint32_t)(items < most ? items : most) * a.heads_kv;
     }
+    if (blocks) hipLaunchKernelGGL((k_attn_mixed<E, kDim, kPaged>), dim3(blocks), dim3(kThreads), 0, st, a, few[0], few[1], s.lists);
     if (s.join) {
         constexpr uint32_t kPer = kDim / 4;
         if (s.slots + s.own_slots > 8u)
