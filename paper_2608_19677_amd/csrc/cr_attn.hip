@@ -906,8 +906,9 @@ struct Shape {
 
 constexpr uint32_t kFewRows = 64;        // mean rows of a sequence up to which the narrow kernel takes it
 constexpr uint32_t kWholeRows = 128;     // mean rows of a request from which its prefix is read again, not joined
-constexpr uint32_t kSplitKeys = 128;     // keys a workgroup should have at least where a call is split
+constexpr uint32_t kSplitKeys = 256;     // keys a workgroup should have at least where a call is split
 constexpr uint32_t kSplitMax = 32;
+constexpr uint32_t kLongKeys = 1024;     // mean keys from which blocks of 256 rows pay
 constexpr uint32_t kNarrowItems = 1024;  // items of the narrow kernel that fill the GPU
 constexpr uint32_t kNarrowSlots = 128;
 
@@ -929,7 +930,7 @@ inline Wide wide_shape(uint32_t kind, uint64_t rows, uint32_t seqs, uint32_t hea
     uint64_t most = keys / kSplitKeys;
     most = most < 1 ? 1 : (most < kSplitMax ? most : kSplitMax);
     Wide w{kind, 128u};
-    if (rows >= 192ull * seqs && tiles_of(rows, 256, seqs) * heads_kv * most >= 256u) w.rows = 256u;
+    if (keys >= kLongKeys && rows >= 192ull * seqs && tiles_of(rows, 256, seqs) * heads_kv * most >= 256u) w.rows = 256u;
     const uint64_t blocks = tiles_of(rows, w.rows, seqs) * heads_kv, room = w.rows == 256u ? 256u : 512u;
     const double tile_us = dim == 128 ? 2.0 : 1.2;
     double least = 0;

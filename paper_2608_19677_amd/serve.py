@@ -35,24 +35,29 @@ def _dtype(t: torch.Tensor) -> int:
         raise B.CrError(f"bfloat16 or float16 wanted, not {t.dtype}") from None
 
 
-def _rows(t: torch.Tensor) -> B.CrRows:
-    """[tokens, heads, dim] with any strides of tokens and heads."""
+def _rows(t: torch.Tensor):
+    """Fields of a cr_rows: [tokens, heads, dim] with any strides of tokens and heads."""
+    stride = t.stride()
+    if len(stride) != 3 or stride[2] != 1:
+        raise B.CrError("rows are [tokens, heads, dim] with dim contiguous")
     if not t.is_cuda:
         raise B.CrError("libcr takes device tensors")
-    if t.dim() != 3 or t.stride(2) != 1:
-        raise B.CrError("rows are [tokens, heads, dim] with dim contiguous")
-    return B.CrRows(t.data_ptr(), t.stride(0), t.stride(1))
+    return t.data_ptr(), stride[0], stride[1]
 
 
-def _index(t: Optional[torch.Tensor], n: Optional[int] = None):
-    """Pointer of an int32 array of n elements (any, if n is None)."""
-    if t is None:
-        return None
-    if t.dtype != torch.int32:
-        raise B.CrError(f"offsets, lengths and tables are int32, not {t.dtype}")
-    if n is not None and t.numel() != n:
-        raise B.CrError(f"{n} entries wanted, not {t.numel()}")
-    return B._ptr(t)
+def _int32(t: Optional[torch.Tensor], n: Optional[int] = None):
+    """An int32 array of n elements (any, if n is None), or None."""
+    if t is not None:
+        if t.dtype is not torch.int32:
+            raise B.CrError(f"offsets, lengths and tables are int32, not {t.dtype}")
+        if n is not None and t.numel() != n:
+            raise B.CrError(f"{n} entries wanted, not {t.numel()}")
+    return t
+
+
+def _index(t: torch.Tensor, n: Optional[int] = None) -> int:
+    """Pointer of such an array."""
+    return B._ptr(_int32(t, n))
 
 
 def _used_on(stream, *tensors):
@@ -112,21 +117,21 @@ class PagePool:
     def extend(self, table, len_old, len_new, stream=None):
         """Free pages for sequences that grow from len_old (None: 0) to len_new tokens."""
         n = len_new.numel()
-        _index(len_new), _index(table), _index(len_old, n)
+        _int32(len_new), _int32(table), _int32(len_old, n)
         _same_rows(table, n)
         B.cr_pages_extend(self.c, len_old, len_new, table, self._scratch(n, stream), self.err, stream)
 
     def fork(self, table, parent, length, child, stream=None):
         """child[i]: the first length[i] tokens of table[parent[i]], the partial tail copied."""
         n = parent.numel()
-        _index(table), _index(parent), _index(length, n), _index(child)
+        _int32(table), _int32(parent), _int32(length, n), _int32(child)
         _same_rows(table, table.shape[0])
         _same_rows(child, n)
         B.cr_pages_fork(self.c, table, parent, length, child, self._scratch(n, stream), self.err, stream)
 
     def free(self, table, length, stream=None):
         """Gives the pages of every row's first length tokens back."""
-        _index(table), _index(length)
+        _int32(table), _int32(length)
         _same_rows(table, length.numel())
         B.cr_pages_free(self.c, table, length, self.err, stream)
 
@@ -134,15 +139,15 @@ class PagePool:
         """Moves the live pages to the front and renames the table's entries (in place, if no
         other place is given)."""
         table_out, refs_out = (table if table_out is None else table_out), (self.refs if refs_out is None else refs_out)
-        _index(table), _index(length), _index(refs_out, self.num_pages)
+        _int32(table), _int32(length), _int32(refs_out, self.num_pages)
         if table is not None:
-            _index(table_out, table.numel())
+            _int32(table_out, table.numel())
             _same_rows(table, length.numel())
         B.cr_pages_compact(self.c, table, length, table_out, refs_out, self._scratch(0, stream), self.err, stream)
 
     def copy(self, src, dst, stream=None):
         """Contents of page src[i] to page dst[i], all layers."""
-        _index(src), _index(dst, src.numel())
+        _int32(src), _int32(dst, src.numel())
         B.cr_pages_copy(self.c, src, dst, self.err, stream)
 
     def append(self, layer: int, k, v, off, length, table, stream=None):
@@ -150,9 +155,9 @@ class PagePool:
         length[i] of sequence i."""
         if k.shape != v.shape or k.shape[1:] != (self.heads, self.dim) or k.dtype != self.k.dtype or v.dtype != self.k.dtype:
             raise B.CrError("new keys and values have the cache's heads, dim and type")
-        _index(length), _index(off, length.numel() + 1), _index(table)
+        _int32(length), _int32(off, length.numel() + 1), _int32(table)
         _same_rows(table, length.numel())
-        B.cr_kv_append(self.c, layer, _rows(k), _rows(v), k.shape[0], off, length, table, self.err, stream)
+        B.cr_kv_append(self.c, layer, B.CrRows(*_rows(k)), B.CrRows(*_rows(v)), k.shape[0], off, length, table, self.err, stream)
 
 
 def _same_rows(table, n: int):
@@ -163,20 +168,18 @@ def _same_rows(table, n: int):
 def _check_out(q, out, lse):
     if out.shape != q.shape or out.dtype != q.dtype:
         raise B.CrError("out has q's shape and type")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2]):
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != q.shape[:2]):
         raise B.CrError("lse is float32 [tokens, heads]")
 
 
-def _prompt_args(q, k, q_off, scale, causal) -> B.CrAttnPromptArgs:
-    a = B.CrAttnPromptArgs()
-    a.dtype, a.heads_q, a.heads_kv, a.dim = _dtype(q), q.shape[1], k.shape[1], q.shape[2]
-    a.batch, a.causal, a.total_q, a.total_k, a.scale = q_off.numel() - 1, int(causal), q.shape[0], k.shape[0], scale
-    return a
+def _prompt_args(q, k, batch, scale, causal, *rest) -> B.CrAttnPromptArgs:
+    nq, hq, d = q.shape
+    return B.CrAttnPromptArgs(_dtype(q), hq, k.shape[1], d, batch, causal, nq, k.shape[0], scale, *rest)
 
 
 def prompt_workspace(q, k, q_off, err: Optional[torch.Tensor] = None) -> Workspace:
     """Scratch for ``attend_prompt`` of tensors of these shapes."""
-    return Workspace(B.cr_attn_prompt_workspace_bytes(_prompt_args(q, k, q_off, 1.0, True)), q.device, err)
+    return Workspace(B.cr_attn_prompt_workspace_bytes(_prompt_args(q, k, q_off.numel() - 1, 1.0, True)), q.device, err)
 
 
 def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, causal: bool = True,
@@ -190,9 +193,9 @@ def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, ca
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         _used_on(stream, out)
     _check_out(q, out, lse)
-    a = _prompt_args(q, k, q_off, scale, causal)
-    a.q, a.k, a.v, a.out, a.lse = _rows(q), _rows(k), _rows(v), _rows(out), B._ptr(lse)
-    a.q_off, a.k_off = _index(q_off), _index(k_off, a.batch + 1)
+    n = q_off.numel()
+    a = _prompt_args(q, k, n - 1, scale, causal, _rows(q), _rows(k), _rows(v), _rows(out), B._ptr(lse), _index(q_off),
+                     _index(k_off, n))
     if ws is None:
         ws = prompt_workspace(q, k, q_off)
         _used_on(stream, ws.buf, ws.err)
@@ -200,16 +203,14 @@ def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, ca
     return out
 
 
-def _shared_args(q, pool: PagePool, layer, group_off, prefix_table, own_table, scale) -> B.CrAttnSharedArgs:
-    a = B.CrAttnSharedArgs()
-    a.heads_q, a.layer, a.batch, a.groups, a.total_q = q.shape[1], layer, own_table.shape[0], group_off.numel() - 1, q.shape[0]
-    a.prefix_width, a.own_width, a.scale = prefix_table.shape[1], own_table.shape[1], scale
-    return a
+def _shared_args(q, pool: PagePool, layer, groups, prefix_table, own_table, scale, *rest) -> B.CrAttnSharedArgs:
+    batch, own_width = own_table.shape
+    return B.CrAttnSharedArgs(q.shape[1], layer, batch, groups, q.shape[0], prefix_table.shape[1], own_width, scale, *rest)
 
 
 def shared_workspace(q, pool: PagePool, group_off, prefix_table, own_table, err: Optional[torch.Tensor] = None) -> Workspace:
     """Scratch for ``attend_shared`` of tensors of these shapes."""
-    a = _shared_args(q, pool, 0, group_off, prefix_table, own_table, 1.0)
+    a = _shared_args(q, pool, 0, group_off.numel() - 1, prefix_table, own_table, 1.0)
     return Workspace(B.cr_attn_shared_workspace_bytes(pool.c, a), q.device, pool.err if err is None else err)
 
 
@@ -225,13 +226,12 @@ def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table,
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         _used_on(stream, out)
     _check_out(q, out, lse)
-    a = _shared_args(q, pool, layer, group_off, prefix_table, own_table, scale)
-    _same_rows(own_table, a.batch)
-    _same_rows(prefix_table, a.groups)
-    a.q, a.out, a.lse = _rows(q), _rows(out), B._ptr(lse)
-    a.q_off, a.group_off = _index(q_off, a.batch + 1), _index(group_off)
-    a.prefix_table, a.prefix_len = _index(prefix_table), _index(prefix_len, a.groups)
-    a.own_table, a.own_len = _index(own_table), _index(own_len, a.batch)
+    batch, groups = own_table.shape[0], group_off.numel() - 1
+    _same_rows(own_table, batch)
+    _same_rows(prefix_table, groups)
+    a = _shared_args(q, pool, layer, groups, prefix_table, own_table, scale, _rows(q), _rows(out), B._ptr(lse),
+                     _index(q_off, batch + 1), _index(group_off), _index(prefix_table), _index(prefix_len, groups),
+                     _index(own_table), _index(own_len, batch))
     if ws is None:
         ws = shared_workspace(q, pool, group_off, prefix_table, own_table)
         _used_on(stream, ws.buf)
