@@ -82,6 +82,7 @@ struct Attn {
     // chunk i's results go to slot i, of the own parts of a call that joins them with prefixes to slot
     // `slots` + i.
     uint32_t chunk, slots, own_chunk, own_slots;
+    uint32_t least_share;  // narrow kernel: tiles a block takes at least, so that no sequence needs more slots
     uint32_t first;        // kind of the first slots (the others are kOwn's)
     float* part_o;         // f32 [slots + own_slots][total_q * heads_q][dim], NULL: results are final
     float* part_lse;       // f32 [slots + own_slots][total_q * heads_q], base 2
@@ -223,7 +224,6 @@ struct Loader {
         piece = mover % kPieces;
         row = mover / kPieces;
         end = last;
-        bad = 0;
         if (kPaged) {
             kb = a.pg.k + (int64_t)head_kv * a.pg.head_stride;
             vb = a.pg.v + (int64_t)head_kv * a.pg.head_stride;
@@ -235,32 +235,32 @@ struct Loader {
             lane_v = row % kWaveRows * (uint32_t)a.v.token_stride + piece * 8u;
         }
     }
-    // The table of the tile at k0, its first key there, and the end of the keys in it.
-    __device__ __forceinline__ void place(const Seq& s, uint32_t k0, const uint32_t** table, uint32_t* first, uint32_t* last) const
+    // The table of the tile at k0, its first key there, and the end of the keys in it (keys end at `stop`).
+    static __device__ __forceinline__ const uint32_t* place(const Seq& s, uint32_t k0, uint32_t stop, uint32_t* first, uint32_t* last)
     {
-        const bool second = k0 >= s.gap_end && end > s.gap_end;
-        *table = second ? s.table1 : s.table0;
+        const bool second = k0 >= s.gap_end && stop > s.gap_end;
         *first = second ? k0 - s.gap_end : k0;
-        *last = second ? end - s.gap_end : min(end, s.len0);
+        *last = second ? stop - s.gap_end : min(stop, s.len0);
+        return second ? s.table1 : s.table0;
     }
-    __device__ __forceinline__ void pages(const Attn& a, const Seq& s, uint32_t k0)
+    static __device__ __forceinline__ void pages_of_tile(const Attn& a, const Seq& s, uint32_t k0, uint32_t stop, uint32_t row,
+                                                         uint32_t (&to)[kPer])
     {
         if (!kPaged) return;
-        const uint32_t* table;
         uint32_t first, last;
-        place(s, k0, &table, &first, &last);
+        const uint32_t* table = place(s, k0, stop, &first, &last);
 #pragma unroll
-        for (uint32_t p = 0; p < kPer; ++p) page[p] = table[min(first + p * kStep + row, last - 1u) >> a.pg.log_tokens];
+        for (uint32_t p = 0; p < kPer; ++p) to[p] = table[min(first + p * kStep + row, last - 1u) >> a.pg.log_tokens];
     }
+    __device__ __forceinline__ void pages(const Attn& a, const Seq& s, uint32_t k0) { pages_of_tile(a, s, k0, end, row, page); }
     // Whole tiles whose rows of one wavefront and pass lie in one page: scalar addresses. Otherwise an
     // address per lane; rows behind the last key repeat it: their weights are 0, and nothing foreign is
     // read.
     __device__ __forceinline__ void load(const Attn& a, const Seq& s, uint32_t k0)
     {
         const uint32_t mask = (1u << a.pg.log_tokens) - 1u;
-        const uint32_t* table = nullptr;
         uint32_t first = k0, last = end;
-        if (kPaged) place(s, k0, &table, &first, &last);
+        if (kPaged) place(s, k0, end, &first, &last);
         if (first + kTile <= last && (!kPaged || mask >= kWaveRows - 1u)) {
             const uint32_t r0 = __builtin_amdgcn_readfirstlane(row);
 #pragma unroll
@@ -385,6 +385,7 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
 
     if (key_begin < key_end) {
         Loader<kDim, kPaged, kKeys, kW * kWave> ld;
+        ld.bad = 0;
         ld.init(a, it, head_kv, key_end, threadIdx.x);
         ld.pages(a, it, key_begin);
         ld.load(a, it, key_begin);
@@ -592,23 +593,36 @@ __global__ __launch_bounds__(8 * kWave, 2) void k_attn_wide(const Attn a, const 
     wide_block<E, kDim, kPaged, 8>(a, p, blockIdx.x, lds);
 }
 
-// Few rows: 32 rows a block, its wavefronts take tiles of 32 keys in turn, each with tiles of its
-// own in LDS and no barrier, and join their results at the end of an item. An item is one tile of
-// rows of one sequence over one chunk of its keys. The blocks stay and walk over the items of up to two
-// lists (prefixes of groups or prompts, own tokens of requests), which every wavefront finds by
-// counting the items of 64 sequences at a time.
-constexpr uint32_t kNarrowRows = 32, kNarrowKeys = 32;
+// Few rows: up to 64 at a time. The block's wavefronts take tiles of 32 keys in turn, each with tiles of
+// its own in LDS and no barrier, and join their results at the end of a stretch. Where a sequence
+// has more than 32 rows, two wavefronts work on each 32 of them and the pairs read the same keys side
+// by side, so that memory is read once for 64 rows.
+//
+// The work of a key head is one line of units: for every sequence of up to two lists (prefixes of groups
+// or prompts, own tokens of requests) and every 64 rows of it, kStart units for the start and one
+// (more than 32 rows: two) for each tile of keys. A block takes an equal share of the line, whatever lengths fall into it;
+// where a share ends inside a sequence's tiles, the parts go to different slots. Lists of one slot are
+// not cut: a sequence is worked on where its first unit lies.
+constexpr uint32_t kNarrowRows = 64, kNarrowKeys = 32;
+constexpr uint32_t kStart = 12; // tiles that a stretch's start and join cost
 
 template <int kDim>
 constexpr uint32_t narrow_lds()  // elements per wavefront: tiles, then its sums [32][dim + 4] f32
 {
-    const uint32_t tiles = key_tile(kNarrowKeys, kDim) + val_tile(kNarrowKeys, kDim), sums = kNarrowRows * (kDim + 4u) * 2u;
+    const uint32_t tiles = key_tile(kNarrowKeys, kDim) + val_tile(kNarrowKeys, kDim), sums = 32u * (kDim + 4u) * 2u;
     return tiles > sums ? tiles : sums;
 }
 
+// What a block keeps of 256 sequences at a time, and its wavefronts' maxima and sums.
+struct NarrowLds {
+    uint32_t at[kThreads];  // units before the sequence, from the first of the 256
+    uint32_t sums[16];
+    uint32_t tok0[kThreads], nq[kThreads], n[kThreads], key0[kThreads];
+    float row_max[kWaves][32], row_sum[kWaves][32];
+};
+
 template <typename E, int kDim, bool kPaged>
-__device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t block, uint32_t blocks, uint16_t* lds,
-                                       float (*sh_max)[kNarrowRows], float (*sh_sum)[kNarrowRows])
+__device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t block, uint32_t blocks, uint16_t* lds, NarrowLds& sh)
 {
     constexpr uint32_t kKeyRun = key_run(kNarrowKeys), kValRun = val_run(kNarrowKeys), kSumRow = kDim + 4u;
 
@@ -618,83 +632,140 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
     uint16_t* lv = lk + key_tile(kNarrowKeys, kDim);
     float* sums = reinterpret_cast<float*>(lk);
 
-    // Sequences 0 .. first_n of the first list, then those of the second. Items `base` and on belong to
-    // the 64 sequences from x0, of which a lane has one.
+    // Sequences 0 .. first_n of the first list, then those of the second.
     const uint32_t first_n = (lists & 1u) ? (kPaged ? a.groups : a.batch) : 0u;
     const uint32_t all_n = first_n + ((lists & 2u) ? a.batch : 0u);
-    uint32_t x0 = 0, base = 0, count = 0, incl = 0, l_tok = 0, l_nq = 0, l_n = 0, l_key0 = 0;
-    auto counted = [&]() {
-        const uint32_t x = x0 + lane;
-        count = 0;
-        if (x < all_n) {
-            const bool own = x >= first_n;
-            const uint32_t y = own ? x - first_n : x;
-            uint32_t r0 = y, r1 = y + 1u;
-            if (kPaged && !own) {
-                r0 = a.group_off[y];
-                r1 = a.group_off[y + 1u];
-            }
-            bool ok = r0 <= r1 && r1 <= a.batch;
-            if (kPaged) {
-                l_n = own ? a.own_len[y] : a.prefix_len[y];
-                ok = ok && pages_of(l_n, a.pg.log_tokens) <= (own ? a.own_width : a.prefix_width);
-            } else {
-                const uint32_t k0 = a.k_off[y], k1 = a.k_off[y + 1u];
-                l_key0 = k0;
-                l_n = k1 - k0;
-                ok = ok && k0 <= k1 && k1 <= a.total_k;
-            }
-            if (ok) {
-                const uint32_t t0 = a.q_off[r0], t1 = a.q_off[r1];
-                l_tok = t0;
-                l_nq = t1 - t0;
-                ok = t0 <= t1 && t1 <= a.total_q;
-            }
-            // a sequence without keys has rows to write all the same
-            if (ok)
-                count = (l_nq * a.group + kNarrowRows - 1u) / kNarrowRows *
-                        max(1u, chunks_of(l_n, own ? a.own_chunk : a.chunk, own ? a.own_slots : a.slots));
-            else
-                atomicOr(a.err, CR_ERR_SEQ);
-        }
-        incl = wave_incl_scan_u32(count);
-    };
-    counted();
-    for (uint32_t id = block / a.heads_kv;; id += blocks / a.heads_kv) {
-        while (id - base >= rdlane(incl, 63)) {
-            base += rdlane(incl, 63);
-            x0 += 64u;
-            if (x0 >= all_n) return;
-            counted();
-        }
-        const uint32_t l = (uint32_t)__builtin_ctzll(ballot(incl > id - base));
-        const uint32_t local = id - base - (rdlane(incl, l) - rdlane(count, l)), x = x0 + l;
+    // Units of sequence x; what does not fit has none.
+    auto units = [&](uint32_t x, uint32_t* tok0, uint32_t* nq, uint32_t* n, uint32_t* key0) CR_INLINE -> uint32_t {
+        if (x >= all_n) return 0u;
         const bool own = x >= first_n;
-        Seq it;
-        it.tok0 = rdlane(l_tok, l);
-        it.nq = rdlane(l_nq, l);
-        it.n = rdlane(l_n, l);
-        it.least = 0;
-        it.gap_end = 0;
-        it.len0 = 0;
-        if (kPaged) {
-            it.causal = own;
-            if (!own) it.len0 = it.gap_end = it.n;
-            it.table0 = a.prefix_table + (uint64_t)x * a.prefix_width;
-            it.table1 = a.own_table + (uint64_t)(x - first_n) * a.own_width;
-        } else {
-            it.causal = a.causal;
-            it.key0 = rdlane(l_key0, l);
+        const uint32_t y = own ? x - first_n : x;
+        uint32_t r0 = y, r1 = y + 1u;
+        if (kPaged && !own) {
+            r0 = a.group_off[y];
+            r1 = a.group_off[y + 1u];
         }
-        it.first_lim = it.causal ? (int32_t)it.n - (int32_t)it.nq + 1 : (int32_t)it.n;
-        const uint32_t slots = own ? a.own_slots : a.slots;
-        const uint32_t chunk = chunk_of(it.n, own ? a.own_chunk : a.chunk, slots), chunks = max(1u, (it.n + chunk - 1u) / chunk);
-        const uint32_t split = local % chunks, row0 = local / chunks * kNarrowRows;
-        const uint32_t rows = min(kNarrowRows, it.nq * a.group - row0);
-        const uint32_t key_begin = split * chunk;
-        const uint32_t key_end = min(row_limit(a, it, row0 + rows - 1u), key_begin + chunk);
-        const uint32_t full = min(row_limit(a, it, row0), key_end);  // keys that every row sees
-        const uint32_t m = row0 + min(col, rows - 1u);
+        bool ok = r0 <= r1 && r1 <= a.batch;
+        if (kPaged) {
+            *n = own ? a.own_len[y] : a.prefix_len[y];
+            ok = ok && pages_of(*n, a.pg.log_tokens) <= (own ? a.own_width : a.prefix_width);
+        } else {
+            const uint32_t k0 = a.k_off[y], k1 = a.k_off[y + 1u];
+            *key0 = k0;
+            *n = k1 - k0;
+            ok = ok && k0 <= k1 && k1 <= a.total_k;
+        }
+        if (ok) {
+            *tok0 = a.q_off[r0];
+            *nq = a.q_off[r1] - *tok0;
+            ok = *tok0 + *nq >= *tok0 && *tok0 + *nq <= a.total_q;
+        }
+        if (!ok) {
+            atomicOr(a.err, CR_ERR_SEQ);
+            return 0u;
+        }
+        const uint32_t rows = *nq * a.group;
+        return (rows + kNarrowRows - 1u) / kNarrowRows *
+               ((*n + kNarrowKeys - 1u) / kNarrowKeys * (rows > 32u ? 2u : 1u) + kStart);
+    };
+    uint32_t here = 0;  // units of the 256 sequences in LDS
+    auto window = [&](uint32_t x0) CR_INLINE {
+        uint32_t tok0 = 0, nq = 0, n = 0, key0 = 0;
+        const uint32_t v = units(x0 + threadIdx.x, &tok0, &nq, &n, &key0);
+        const uint32_t at = block_exscan_u32(v, sh.sums, &here);
+        here = __builtin_amdgcn_readfirstlane(here);
+        sh.at[threadIdx.x] = at;
+        sh.tok0[threadIdx.x] = tok0;
+        sh.nq[threadIdx.x] = nq;
+        sh.n[threadIdx.x] = n;
+        sh.key0[threadIdx.x] = key0;
+        __syncthreads();
+    };
+    window(0);
+    uint32_t all = here;
+    for (uint32_t x0 = kThreads; x0 < all_n; x0 += kThreads) {
+        uint32_t t0, t1, t2, t3, sum;
+        block_exscan_u32(units(x0 + threadIdx.x, &t0, &t1, &t2, &t3), sh.sums, &sum);
+        all += __builtin_amdgcn_readfirstlane(sum);
+    }
+    const uint32_t index = block / a.heads_kv, of = blocks / a.heads_kv;
+    const uint32_t share = max(all / of + 1u, a.least_share);
+    if ((uint64_t)index * share >= all) return;
+    uint32_t u = index * share, base = 0, x0 = 0;
+    const uint32_t u_end = min(all - u, share) + u;
+
+    // A stretch: up to 64 rows of a sequence over the tiles of it that fall into the block's share.
+    struct Stretch {
+        Seq it;
+        uint32_t row0, rows, key_begin, key_end, slot;
+        bool own, pairs, ends, valid;
+    };
+    auto next = [&]() CR_INLINE {
+        Stretch st;
+        st.valid = false;
+        while (u < u_end && !st.valid) {
+            while (u >= base + here) {  // all > u: there is a window behind
+                base += here;
+                x0 += kThreads;
+                window(x0);
+            }
+            uint32_t i = 0;  // the sequence of unit u
+#pragma unroll
+            for (uint32_t y = 0; y < kThreads; y += 64u) i += (uint32_t)__popcll(ballot(sh.at[y + lane] <= u - base));
+            i = __builtin_amdgcn_readfirstlane(i - 1u);
+            const uint32_t x = x0 + i;
+            Seq& it = st.it;
+            st.own = x >= first_n;
+            it.tok0 = __builtin_amdgcn_readfirstlane(sh.tok0[i]);
+            it.nq = __builtin_amdgcn_readfirstlane(sh.nq[i]);
+            it.n = __builtin_amdgcn_readfirstlane(sh.n[i]);
+            it.least = 0;
+            it.gap_end = 0;
+            it.len0 = 0;
+            if (kPaged) {
+                it.causal = st.own;
+                if (!st.own) it.len0 = it.gap_end = it.n;
+                it.table0 = a.prefix_table + (uint64_t)x * a.prefix_width;
+                it.table1 = a.own_table + (uint64_t)(x - first_n) * a.own_width;
+            } else {
+                it.causal = a.causal;
+                it.key0 = __builtin_amdgcn_readfirstlane(sh.key0[i]);
+            }
+            it.first_lim = it.causal ? (int32_t)it.n - (int32_t)it.nq + 1 : (int32_t)it.n;
+            const uint32_t tiles = (it.n + kNarrowKeys - 1u) / kNarrowKeys;
+            st.pairs = it.nq * a.group > 32u;
+            const uint32_t per_tile = st.pairs ? 2u : 1u;  // units
+            const uint32_t from = base + __builtin_amdgcn_readfirstlane(sh.at[i]), step = tiles * per_tile + kStart;
+            const uint32_t row_tile = __builtin_amdgcn_readfirstlane((u - from) / step);
+            const uint32_t first = from + row_tile * step, keys = first + kStart, last = first + step;  // the rows' units
+            uint32_t t0 = 0, t1 = tiles;
+            st.slot = 0;
+            st.ends = true;
+            st.valid = u == first;
+            if ((st.own ? a.own_slots : a.slots) > 1u && tiles != 0u) {
+                // every block whose share has a unit of the keys has a slot, though it may come without a tile
+                st.valid = u_end > keys;
+                t0 = u > keys ? (u - keys) / per_tile : 0u;
+                t1 = u_end < last ? (st.valid ? (u_end - keys) / per_tile : 0u) : tiles;
+                st.slot = index - __builtin_amdgcn_readfirstlane(keys / share);
+                st.ends = last <= u_end;
+            }
+            u = last;
+            st.row0 = row_tile * kNarrowRows;
+            st.rows = min(kNarrowRows, it.nq * a.group - st.row0);
+            st.key_begin = t0 * kNarrowKeys;
+            st.key_end = min(row_limit(a, it, st.row0 + st.rows - 1u), t1 * kNarrowKeys);
+        }
+        return st;
+    };
+    for (Stretch st = next(); st.valid; st = next()) {
+        const Seq& it = st.it;
+        const bool own = st.own, pairs = st.pairs;
+        const uint32_t slots = own ? a.own_slots : a.slots, row0 = st.row0, rows = st.rows, key_end = st.key_end;
+        const uint32_t wave_row = pairs ? (wv & 1u) * 32u : 0u;      // of the 64
+        const uint32_t full = min(row_limit(a, it, row0 + min(wave_row, rows - 1u)), key_end);  // keys that every row of the wave sees
+        const uint32_t key_step = (pairs ? 2u : kWaves) * kNarrowKeys;
+        const uint32_t m = row0 + min(wave_row + col, rows - 1u);
         const uint32_t tok = it.tok0 + m / a.group, head = head_kv * a.group + m % a.group;
         const int32_t lim = (int32_t)min(row_limit(a, it, m), key_end);
 
@@ -704,24 +775,25 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
         float mc = kNoMax, sum = 0.f;
-        uint32_t k0 = key_begin + wv * kNarrowKeys;
-        if (k0 < key_end) {
+        uint32_t k0 = st.key_begin + (pairs ? wv >> 1 : wv) * kNarrowKeys;
+        if (k0 < key_end && wave_row < rows) {
             Loader<kDim, kPaged, kNarrowKeys, kWave> ld;
+            ld.bad = 0;
             ld.init(a, it, head_kv, key_end, lane);
             ld.pages(a, it, k0);
             ld.load(a, it, k0);
-            ld.pages(a, it, k0 + kWaves * kNarrowKeys);
+            ld.pages(a, it, k0 + key_step);
             s16x8 qf[kDim / 16];
             const uint16_t* qp = (const uint16_t*)a.q.p + (int64_t)tok * a.q.token_stride + (int64_t)head * a.q.head_stride;
 #pragma unroll
             for (int s = 0; s < kDim / 16; ++s) qf[s] = *reinterpret_cast<const s16x8*>(qp + s * 16 + half * 8u);
             const uint32_t k_lane = half * kKeyRun + col * 8u;
             const uint32_t v_lane = (half * 4u + (lane & 15u) / 4u) * 32u + ((lane >> 4) & 1u) * 16u + (lane & 3u) * 4u;
-            for (; k0 < key_end; k0 += kWaves * kNarrowKeys) {
+            for (; k0 < key_end; k0 += key_step) {
                 ld.store(lk, lv);
                 wave_lds_fence();
-                ld.load(a, it, k0 + kWaves * kNarrowKeys);
-                ld.pages(a, it, k0 + 2u * kWaves * kNarrowKeys);
+                ld.load(a, it, k0 + key_step);
+                ld.pages(a, it, k0 + 2u * key_step);
                 f32x16 s;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[i] = 0.f;
@@ -775,8 +847,8 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
         }
         sum = both_sum(sum);
         if (half == 0) {
-            sh_max[wv][col] = mc;
-            sh_sum[wv][col] = sum;
+            sh.row_max[wv][col] = mc;
+            sh.row_sum[wv][col] = sum;
         }
 #pragma unroll
         for (int d = 0; d < kDim / 32; ++d)
@@ -786,16 +858,15 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
         __syncthreads();
         // 4 elements of a row per thread
         for (uint32_t y = threadIdx.x; y < rows * (kDim / 4u); y += kThreads) {
-            const uint32_t r = y / (kDim / 4u), e = y % (kDim / 4u) * 4u, mm = row0 + r;
-            float mx = sh_max[0][r], total = 0.f;
-#pragma unroll
-            for (uint32_t w = 1; w < kWaves; ++w) mx = fmaxf(mx, sh_max[w][r]);
+            const uint32_t row = y / (kDim / 4u), r = row & 31u, e = y % (kDim / 4u) * 4u, mm = row0 + row;
+            const uint32_t w0 = row >> 5, w_step = pairs ? 2u : 1u;  // the wavefronts that worked on the row
+            float mx = sh.row_max[w0][r], total = 0.f;
+            for (uint32_t w = w0 + w_step; w < kWaves; w += w_step) mx = fmaxf(mx, sh.row_max[w][r]);
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (uint32_t w = 0; w < kWaves; ++w) {
-                const float f = __builtin_amdgcn_exp2f(sh_max[w][r] - mx);
+            for (uint32_t w = w0; w < kWaves; w += w_step) {
+                const float f = __builtin_amdgcn_exp2f(sh.row_max[w][r] - mx);
                 const f32x4 v = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds + w * narrow_lds<kDim>()) + r * kSumRow + e);
-                total = __builtin_fmaf(f, sh_sum[w][r], total);
+                total = __builtin_fmaf(f, sh.row_sum[w][r], total);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(f, v[i], acc[i]);
             }
@@ -804,11 +875,11 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             const uint32_t ot = it.tok0 + mm / a.group, oh = head_kv * a.group + mm % a.group;
             const uint64_t orow = (uint64_t)ot * a.heads_q + oh;
             if (a.part_o) {
-                const uint64_t at = (uint64_t)(split + (own ? a.slots : 0u)) * a.total_q * a.heads_q + orow;
+                const uint64_t at = (uint64_t)(st.slot + (own ? a.slots : 0u)) * a.total_q * a.heads_q + orow;
                 if (e == 0) {
                     a.part_lse[at] = lse2;
-                    if (split == chunks - 1u)  // slots without a chunk
-                        for (uint32_t z = chunks; z < slots; ++z) a.part_lse[at + (uint64_t)(z - split) * a.total_q * a.heads_q] = -INFINITY;
+                    if (st.ends)  // slots that are left
+                        for (uint32_t z = st.slot + 1u; z < slots; ++z) a.part_lse[at + (uint64_t)(z - st.slot) * a.total_q * a.heads_q] = -INFINITY;
                 }
                 *reinterpret_cast<f32x4*>(a.part_o + at * kDim + e) = acc * inv;
             } else {
@@ -823,18 +894,20 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
 
 // One launch of what is not wide: tiles of 128 rows (up to two parts) and the narrow lists' blocks,
 // so that neither waits for the other's last.
+constexpr uint32_t mixed_per_cu(uint32_t dim) { return dim == 128u ? 2u : 3u; }  // blocks that fit a compute unit
+
 template <typename E, int kDim, bool kPaged>
-__global__ __launch_bounds__(kThreads, 2) void k_attn_mixed(const Attn a, const Part p0, const Part p1, uint32_t lists)
+__global__ __launch_bounds__(kThreads, mixed_per_cu(kDim)) void k_attn_mixed(const Attn a, const Part p0, const Part p1, uint32_t lists)
 {
     constexpr uint32_t kWide = wide_lds(kWaves, kDim), kNarrow = kWaves * narrow_lds<kDim>();
     __shared__ __align__(16) uint16_t lds[kWide > kNarrow ? kWide : kNarrow];
-    __shared__ float sh_max[kWaves][kNarrowRows], sh_sum[kWaves][kNarrowRows];
+    __shared__ NarrowLds sh;
     const uint32_t wides = p0.blocks + p1.blocks;
     if (blockIdx.x < wides) {
         const bool second = blockIdx.x >= p0.blocks;
         wide_block<E, kDim, kPaged, kWaves>(a, second ? p1 : p0, second ? blockIdx.x - p0.blocks : blockIdx.x, lds);
     } else {
-        narrow_block<E, kDim, kPaged>(a, lists, blockIdx.x - wides, gridDim.x - wides, lds, sh_max, sh_sum);
+        narrow_block<E, kDim, kPaged>(a, lists, blockIdx.x - wides, gridDim.x - wides, lds, sh);
     }
 }
 
@@ -901,6 +974,8 @@ struct Shape {
     Wide wide[2];
     uint32_t wides, lists;  // lists of the narrow launch: 1 the first kind's, 2 own tokens
     uint32_t first, chunk, slots, own_chunk, own_slots;
+    uint32_t least;                                        // share of a narrow block, in tiles
+    uint64_t blocks;                                       // of the narrow launch, per key head
     bool join;
 };
 
@@ -909,8 +984,8 @@ constexpr uint32_t kWholeRows = 128;     // mean rows of a request from which it
 constexpr uint32_t kSplitKeys = 256;     // keys a workgroup should have at least where a call is split
 constexpr uint32_t kSplitMax = 32;
 constexpr uint32_t kLongKeys = 1024;     // mean keys from which blocks of 256 rows pay
-constexpr uint32_t kNarrowItems = 1024;  // items of the narrow kernel that fill the GPU
-constexpr uint32_t kNarrowSlots = 128;
+constexpr uint32_t kNarrowParts = 63;    // shares a sequence's keys may fall into
+constexpr uint32_t kShareLeast = 8;      // tiles a narrow block should have
 
 inline uint32_t up_to(uint64_t x, uint32_t m) { return (uint32_t)((x + m - 1u) / m * m); }
 
@@ -946,15 +1021,36 @@ inline Wide wide_shape(uint32_t kind, uint64_t rows, uint32_t seqs, uint32_t hea
     return w;
 }
 
-inline void narrow_shape(uint64_t rows, uint32_t seqs, uint32_t heads_kv, uint64_t keys, uint64_t most_keys, uint32_t* chunk,
-                         uint32_t* slots)
+// Slots of a narrow list of sequences of up to `keys` keys, where a block's share of the work is about
+// `share` tiles; *least: the share from which no sequence passes its slots.
+inline uint32_t narrow_slots(uint64_t keys, uint64_t share, uint32_t* least)
 {
-    const uint64_t total = tiles_of(rows, kNarrowRows, seqs) * heads_kv * keys;
-    uint64_t c = 256;
-    while (c < 4096 && c * 2u * kNarrowItems <= total) c *= 2u;
-    const uint64_t n = (most_keys + c - 1u) / c;
-    *chunk = (uint32_t)c;
-    *slots = (uint32_t)(n < 1 ? 1 : (n < kNarrowSlots ? n : kNarrowSlots));
+    const uint64_t tiles = (keys + kNarrowKeys - 1u) / kNarrowKeys * 2u;  // units, where there are more than 32 rows
+    if (tiles * 2u <= share) return 1u;  // cutting would not level the shares by much
+    uint64_t parts = (tiles + share - 1u) / share;
+    parts = parts < kNarrowParts ? parts : kNarrowParts;
+    const uint32_t need = (uint32_t)((tiles + parts - 1u) / parts);
+    *least = need > *least ? need : *least;
+    return (uint32_t)parts + 1u;
+}
+
+// Units of a list per key head, its sequences half as long as they may be.
+inline uint64_t narrow_units(uint64_t rows, uint32_t seqs, uint64_t keys)
+{
+    return tiles_of(rows, kNarrowRows, seqs) * (keys / (2u * kNarrowKeys) * (rows > 32ull * seqs ? 2u : 1u) + kStart);
+}
+
+// Whether the list's units stay in 32 bits whatever the lengths.
+inline bool narrow_fits(uint64_t rows, uint32_t seqs, uint64_t keys)
+{
+    return (rows / kNarrowRows + seqs) * (keys / (kNarrowKeys / 2u) + 2u + kStart) < (1ull << 31);
+}
+
+// Blocks per key head: what the wide parts of the launch leave of the GPU, at least half of it.
+inline uint64_t narrow_blocks(uint32_t dim, uint32_t heads_kv, uint64_t wides)
+{
+    const uint64_t room = (uint64_t)mixed_per_cu(dim) * (uint64_t)device_cus();
+    return ((wides < room / 2u ? room - wides : room / 2u) + heads_kv - 1u) / heads_kv;
 }
 
 inline bool good_scale(float s) { return s > 0.f && s <= 3.0e38f; }
@@ -982,9 +1078,18 @@ inline Shape prompt_shape(const cr_attn_prompt_args* p)
     Shape s{};
     s.first = kPrompt;
     const uint64_t rows = (uint64_t)p->total_q * (p->heads_q / p->heads_kv), keys = p->total_k / p->batch;
-    if (rows <= (uint64_t)kFewRows * p->batch) {
+    if (rows <= (uint64_t)kFewRows * p->batch && narrow_fits(rows, p->batch, p->total_k)) {
         s.lists = 1;
-        narrow_shape(rows, p->batch, p->heads_kv, keys, p->batch > 1 ? 2 * keys : keys, &s.chunk, &s.slots);
+        s.blocks = narrow_blocks(p->dim, p->heads_kv, 0);
+        s.least = kShareLeast;
+        const uint64_t units = narrow_units(rows, p->batch, 2u * keys), equal = units / s.blocks;
+        s.slots = narrow_slots(p->batch > 1 ? 2u * keys : keys, equal > kShareLeast ? equal : kShareLeast, &s.least);
+        if (s.slots > 1 && p->batch > 1) {  // a sequence may be longer than twice the mean
+            const uint32_t need = (2u * (p->total_k / kNarrowKeys + 1u) + s.slots - 2u) / (s.slots - 1u);
+            s.least = need > s.least ? need : s.least;
+        }
+        const uint64_t most = (2u * units + s.least - 1u) / s.least;  // more blocks would have no share
+        if (most < s.blocks) s.blocks = most ? most : 1u;
     } else {
         s.wide[s.wides++] = wide_shape(kPrompt, rows, p->batch, p->heads_kv, keys, p->dim, &s.chunk, &s.slots);
     }
@@ -1005,19 +1110,31 @@ inline Shape shared_shape(const cr_kv_cache* c, const cr_attn_shared_args* p)
         return s;
     }
     s.first = kGroup;
-    if (rows <= (uint64_t)kFewRows * p->groups) {
+    s.join = true;
+    uint64_t units = 0, wides = 0;
+    if (rows <= (uint64_t)kFewRows * p->groups && narrow_fits(rows, p->groups, prefix)) {
         s.lists |= 1u;
-        narrow_shape(rows, p->groups, c->heads, prefix, prefix, &s.chunk, &s.slots);
+        units += narrow_units(rows, p->groups, prefix);
     } else {
-        s.wide[s.wides++] = wide_shape(kGroup, rows, p->groups, c->heads, prefix, c->dim, &s.chunk, &s.slots);
+        const Wide w = wide_shape(kGroup, rows, p->groups, c->heads, prefix, c->dim, &s.chunk, &s.slots);
+        if (w.rows == 128u) wides += tiles_of(rows, w.rows, p->groups) * s.slots * c->heads;
+        s.wide[s.wides++] = w;
     }
-    if (rows <= (uint64_t)kFewRows * p->batch) {
+    if (rows <= (uint64_t)kFewRows * p->batch && narrow_fits(rows, p->batch, own)) {
         s.lists |= 2u;
-        narrow_shape(rows, p->batch, c->heads, own, own, &s.own_chunk, &s.own_slots);
+        units += narrow_units(rows, p->batch, own);
     } else {
         s.wide[s.wides++] = wide_shape(kOwn, rows, p->batch, c->heads, own, c->dim, &s.own_chunk, &s.own_slots);
     }
-    s.join = true;
+    if (s.lists) {
+        s.blocks = narrow_blocks(c->dim, c->heads, wides);
+        s.least = kShareLeast;
+        const uint64_t equal = units / s.blocks, share = equal > kShareLeast ? equal : kShareLeast;
+        if (s.lists & 1u) s.slots = narrow_slots(prefix, share, &s.least);
+        if (s.lists & 2u) s.own_slots = narrow_slots(own, share, &s.least);
+        const uint64_t most = (2u * units + s.least - 1u) / s.least;  // more blocks would have no share
+        if (most < s.blocks) s.blocks = most ? most : 1u;
+    }
     return s;
 }
 
@@ -1040,13 +1157,7 @@ void launch(const Attn& a, const Shape& s, hipStream_t st)
         else few[fews++] = p;
     }
     uint32_t blocks = few[0].blocks + few[1].blocks;
-    if (s.lists) {
-        uint64_t items = 0;
-        if (s.lists & 1u) items += (rows / kNarrowRows + (kPaged ? a.groups : a.batch)) * a.slots;
-        if (s.lists & 2u) items += (rows / kNarrowRows + a.batch) * a.own_slots;
-        const uint64_t most = (2u * (uint64_t)device_cus() + a.heads_kv - 1u) / a.heads_kv;
-        blocks += (uint32_t)(items < most ? items : most) * a.heads_kv;
-    }
+    if (s.lists) blocks += (uint32_t)s.blocks * a.heads_kv;
     if (blocks) hipLaunchKernelGGL((k_attn_mixed<E, kDim, kPaged>), dim3(blocks), dim3(kThreads), 0, st, a, few[0], few[1], s.lists);
     if (s.join) {
         constexpr uint32_t kPer = kDim / 4;
@@ -1069,6 +1180,7 @@ cr_status dispatch(Attn& a, const Shape& s, void* ws, uint32_t dtype, uint32_t d
     a.slots = s.slots;
     a.own_chunk = s.own_chunk;
     a.own_slots = s.own_slots;
+    a.least_share = s.least;
     if (s.join) {
         a.part_o = (float*)ws;
         a.part_lse = a.part_o + ((uint64_t)s.slots + s.own_slots) * a.total_q * a.heads_q * dim;
