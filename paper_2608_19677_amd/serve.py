@@ -172,14 +172,14 @@ def _check_out(q, out, lse):
         raise B.CrError("lse is float32 [tokens, heads]")
 
 
-def _prompt_args(q, k, batch, scale, causal, *rest) -> B.CrAttnPromptArgs:
+def _prompt_args(dtype, q, k, batch, scale, causal, *rest) -> B.CrAttnPromptArgs:
     nq, hq, d = q.shape
-    return B.CrAttnPromptArgs(_dtype(q), hq, k.shape[1], d, batch, causal, nq, k.shape[0], scale, *rest)
+    return B.CrAttnPromptArgs(dtype, hq, k.shape[1], d, batch, causal, nq, k.shape[0], scale, *rest)
 
 
 def prompt_workspace(q, k, q_off, err: Optional[torch.Tensor] = None) -> Workspace:
     """Scratch for ``attend_prompt`` of tensors of these shapes."""
-    return Workspace(B.cr_attn_prompt_workspace_bytes(_prompt_args(q, k, q_off.numel() - 1, 1.0, True)), q.device, err)
+    return Workspace(B.cr_attn_prompt_workspace_bytes(_prompt_args(_dtype(q), q, k, q_off.numel() - 1, 1.0, True)), q.device, err)
 
 
 def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, causal: bool = True,
@@ -189,12 +189,13 @@ def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, ca
     float32 [total_q, heads_q], if given)."""
     if k.shape != v.shape or k.shape[2] != q.shape[2] or k.dtype != q.dtype or v.dtype != q.dtype:
         raise B.CrError("q, k and v have one type and dim, k and v one shape")
+    dtype = _dtype(q)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         _used_on(stream, out)
     _check_out(q, out, lse)
     n = q_off.numel()
-    a = _prompt_args(q, k, n - 1, scale, causal, _rows(q), _rows(k), _rows(v), _rows(out), B._ptr(lse), _index(q_off),
+    a = _prompt_args(dtype, q, k, n - 1, scale, causal, _rows(q), _rows(k), _rows(v), _rows(out), B._ptr(lse), _index(q_off),
                      _index(k_off, n))
     if ws is None:
         ws = prompt_workspace(q, k, q_off)
