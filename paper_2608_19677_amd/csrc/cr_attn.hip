@@ -894,10 +894,10 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
 
 // One launch of what is not wide: tiles of 128 rows (up to two parts) and the narrow lists' blocks,
 // so that neither waits for the other's last.
-constexpr uint32_t mixed_per_cu(uint32_t dim) { return dim == 128u ? 2u : 3u; }  // blocks that fit a compute unit
+constexpr uint32_t kMixedPerCu = 2;  // blocks that share a compute unit
 
 template <typename E, int kDim, bool kPaged>
-__global__ __launch_bounds__(kThreads, mixed_per_cu(kDim)) void k_attn_mixed(const Attn a, const Part p0, const Part p1, uint32_t lists)
+__global__ __launch_bounds__(kThreads, kMixedPerCu) void k_attn_mixed(const Attn a, const Part p0, const Part p1, uint32_t lists)
 {
     constexpr uint32_t kWide = wide_lds(kWaves, kDim), kNarrow = kWaves * narrow_lds<kDim>();
     __shared__ __align__(16) uint16_t lds[kWide > kNarrow ? kWide : kNarrow];
@@ -1040,16 +1040,28 @@ inline uint64_t narrow_units(uint64_t rows, uint32_t seqs, uint64_t keys)
     return tiles_of(rows, kNarrowRows, seqs) * (keys / (2u * kNarrowKeys) * (rows > 32ull * seqs ? 2u : 1u) + kStart);
 }
 
+// Most units that a list can have per key head.
+inline uint64_t narrow_most(uint64_t rows, uint32_t seqs, uint64_t keys)
+{
+    return (rows / kNarrowRows + seqs) * (keys / (kNarrowKeys / 2u) + 2u + kStart);
+}
+
 // Whether the list's units stay in 32 bits whatever the lengths.
 inline bool narrow_fits(uint64_t rows, uint32_t seqs, uint64_t keys)
 {
-    return (rows / kNarrowRows + seqs) * (keys / (kNarrowKeys / 2u) + 2u + kStart) < (1ull << 31);
+    return narrow_most(rows, seqs, keys) < (1ull << 31);
 }
 
+// Whether every sequence can have a block to itself: shares of kStart units hold one sequence's first
+// unit at most, so with whole sequences (one slot) and as many blocks none works on two. For short ones:
+// a block's wavefronts take four tiles at a time.
+constexpr uint32_t kAloneKeys = 512;
+inline bool narrow_alone(uint64_t most, uint64_t keys, uint64_t blocks) { return keys <= kAloneKeys && most <= blocks * kStart; }
+
 // Blocks per key head: what the wide parts of the launch leave of the GPU, at least half of it.
-inline uint64_t narrow_blocks(uint32_t dim, uint32_t heads_kv, uint64_t wides)
+inline uint64_t narrow_blocks(uint32_t heads_kv, uint64_t wides)
 {
-    const uint64_t room = (uint64_t)mixed_per_cu(dim) * (uint64_t)device_cus();
+    const uint64_t room = kMixedPerCu * (uint64_t)device_cus();
     return ((wides < room / 2u ? room - wides : room / 2u) + heads_kv - 1u) / heads_kv;
 }
 
@@ -1080,7 +1092,7 @@ inline Shape prompt_shape(const cr_attn_prompt_args* p)
     const uint64_t rows = (uint64_t)p->total_q * (p->heads_q / p->heads_kv), keys = p->total_k / p->batch;
     if (rows <= (uint64_t)kFewRows * p->batch && narrow_fits(rows, p->batch, p->total_k)) {
         s.lists = 1;
-        s.blocks = narrow_blocks(p->dim, p->heads_kv, 0);
+        s.blocks = narrow_blocks(p->heads_kv, 0);
         s.least = kShareLeast;
         const uint64_t units = narrow_units(rows, p->batch, 2u * keys), equal = units / s.blocks;
         s.slots = narrow_slots(p->batch > 1 ? 2u * keys : keys, equal > kShareLeast ? equal : kShareLeast, &s.least);
@@ -1089,7 +1101,13 @@ inline Shape prompt_shape(const cr_attn_prompt_args* p)
             s.least = need > s.least ? need : s.least;
         }
         const uint64_t most = (2u * units + s.least - 1u) / s.least;  // more blocks would have no share
-        if (most < s.blocks) s.blocks = most ? most : 1u;
+        const uint64_t all = narrow_most(rows, p->batch, p->total_k);
+        if (narrow_alone(all, p->total_k, s.blocks)) {
+            s.slots = s.least = 1u;
+            s.blocks = (all + kStart - 1u) / kStart;
+        } else if (most < s.blocks) {
+            s.blocks = most ? most : 1u;
+        }
     } else {
         s.wide[s.wides++] = wide_shape(kPrompt, rows, p->batch, p->heads_kv, keys, p->dim, &s.chunk, &s.slots);
     }
@@ -1127,13 +1145,21 @@ inline Shape shared_shape(const cr_kv_cache* c, const cr_attn_shared_args* p)
         s.wide[s.wides++] = wide_shape(kOwn, rows, p->batch, c->heads, own, c->dim, &s.own_chunk, &s.own_slots);
     }
     if (s.lists) {
-        s.blocks = narrow_blocks(c->dim, c->heads, wides);
+        s.blocks = narrow_blocks(c->heads, wides);
         s.least = kShareLeast;
         const uint64_t equal = units / s.blocks, share = equal > kShareLeast ? equal : kShareLeast;
         if (s.lists & 1u) s.slots = narrow_slots(prefix, share, &s.least);
         if (s.lists & 2u) s.own_slots = narrow_slots(own, share, &s.least);
         const uint64_t most = (2u * units + s.least - 1u) / s.least;  // more blocks would have no share
-        if (most < s.blocks) s.blocks = most ? most : 1u;
+        const uint64_t all = ((s.lists & 1u) ? narrow_most(rows, p->groups, prefix) : 0u) + ((s.lists & 2u) ? narrow_most(rows, p->batch, own) : 0u);
+        if (narrow_alone(all, (s.lists & 1u) && prefix > own ? prefix : own, s.blocks)) {
+            if (s.lists & 1u) s.slots = 1u;
+            if (s.lists & 2u) s.own_slots = 1u;
+            s.least = 1u;
+            s.blocks = (all + kStart - 1u) / kStart;
+        } else if (most < s.blocks) {
+            s.blocks = most ? most : 1u;
+        }
     }
     return s;
 }

@@ -134,6 +134,24 @@ __global__ __launch_bounds__(256) void k_pages_count(const uint32_t* __restrict_
     if (bad) atomicOr(err, bad);
 }
 
+// The sequence that takes the page of rank r: first[i] <= r < first[i + 1].
+__device__ __forceinline__ uint32_t pg_taker(const PgWs& w, const PgTake& t, uint32_t r)
+{
+    uint32_t lo = 0, hi = t.n;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (w.first[mid] <= r) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Pages that its row has before those it takes.
+__device__ __forceinline__ uint32_t pg_had(const PgTake& t, uint32_t i)
+{
+    return t.parent ? t.length[i] >> t.log_tokens : pages_of(t.len_old ? t.len_old[i] : 0u, t.log_tokens);
+}
+
 // Blocks 0 .. chunks-1 hand their chunk's free pages out by rank; for a fork, the blocks behind count
 // a child's shared pages each.
 __global__ __launch_bounds__(256) void k_pages_take(uint32_t* __restrict__ refs, uint32_t chunks, PgWs w, PgTake t,
@@ -162,15 +180,8 @@ __global__ __launch_bounds__(256) void k_pages_take(uint32_t* __restrict__ refs,
     uint32_t m = pg_free_mask(refs, t.num_pages, p0), tot;
     uint32_t r = before + block_exscan_u32((uint32_t)__popc(m), sh, &tot);
     for (; m && r < want; ++r, m &= m - 1u) {
-        const uint32_t p = p0 + (uint32_t)__builtin_ctz(m);
-        uint32_t lo = 0, hi = t.n;  // the sequence with first[lo] <= r < first[lo + 1]
-        while (hi - lo > 1) {
-            const uint32_t mid = (lo + hi) >> 1;
-            if (w.first[mid] <= r) lo = mid;
-            else hi = mid;
-        }
-        const uint32_t had = t.parent ? t.length[lo] >> t.log_tokens : pages_of(t.len_old ? t.len_old[lo] : 0u, t.log_tokens);
-        t.out[(uint64_t)lo * t.out_width + had + (r - w.first[lo])] = p;
+        const uint32_t p = p0 + (uint32_t)__builtin_ctz(m), i = pg_taker(w, t, r);
+        t.out[(uint64_t)i * t.out_width + pg_had(t, i) + (r - w.first[i])] = p;
         refs[p] = 1u;
     }
 }
@@ -206,30 +217,97 @@ __device__ __forceinline__ int64_t pg_piece(const PgGeom& g, uint32_t x)
     return (int64_t)head * g.head_stride + (int64_t)tok * g.token_stride + (int64_t)(x % g.row16) * 8;
 }
 
-// A fork's tails: the tokens behind the full pages, a unit per child and plane (keys or values of a
-// layer).
-__global__ __launch_bounds__(256) void k_pages_tail(uint16_t* __restrict__ k, uint16_t* __restrict__ v, int64_t layer_stride,
-                                                    int64_t page_stride, PgGeom g, uint32_t planes, PgTake t)
+// A fork's tail: the tokens behind child i's full pages in one plane (keys or values of a layer), copied by
+// `movers` threads.
+struct PgPlanes {
+    uint16_t* k;
+    uint16_t* v;
+    int64_t layer_stride, page_stride;
+    PgGeom g;
+    uint32_t planes;
+};
+
+__device__ __forceinline__ void pg_copy_tail(const PgPlanes& c, const PgTake& t, uint32_t i, uint32_t plane, uint32_t mover, uint32_t movers)
 {
-    for (uint64_t u = blockIdx.x; u < (uint64_t)t.n * planes; u += gridDim.x) {
-        const uint32_t i = (uint32_t)(u / planes), plane = (uint32_t)(u % planes);
-        const uint32_t len = t.length[i], full = len >> t.log_tokens, tail = len & ((1u << t.log_tokens) - 1u);
-        if (tail == 0u || full >= t.out_width) continue;
-        const uint32_t dst = t.out[(uint64_t)i * t.out_width + full];
-        if (dst >= t.num_pages) continue;  // not served
-        const uint32_t src = t.table[(uint64_t)t.parent[i] * t.width + full];
-        if (src >= t.num_pages) continue;  // reported with the rows
-        uint16_t* base = ((plane & 1u) ? v : k) + (int64_t)(plane >> 1) * layer_stride;
-        const uint16_t* s = base + (int64_t)src * page_stride;
-        uint16_t* d = base + (int64_t)dst * page_stride;
-        const uint32_t per_head = tail * g.row16, all = per_head * g.heads;
-        for (uint32_t x = threadIdx.x; x < all; x += kCopyThreads) {
-            const uint32_t head = x / per_head, r = x % per_head;
-            const int64_t at =
-                (int64_t)head * g.head_stride + (int64_t)(r / g.row16) * g.token_stride + (int64_t)(r % g.row16) * 8;
-            *reinterpret_cast<uint4*>(d + at) = *reinterpret_cast<const uint4*>(s + at);
+    const PgGeom& g = c.g;
+    const uint32_t len = t.length[i], full = len >> t.log_tokens, tail = len & ((1u << t.log_tokens) - 1u);
+    if (tail == 0u || full >= t.out_width) return;
+    const uint32_t dst = t.out[(uint64_t)i * t.out_width + full];
+    if (dst >= t.num_pages) return;  // not served
+    const uint32_t src = t.table[(uint64_t)t.parent[i] * t.width + full];
+    if (src >= t.num_pages) return;  // reported with the rows
+    uint16_t* base = ((plane & 1u) ? c.v : c.k) + (int64_t)(plane >> 1) * c.layer_stride;
+    const uint16_t* s = base + (int64_t)src * c.page_stride;
+    uint16_t* d = base + (int64_t)dst * c.page_stride;
+    const uint32_t per_head = tail * g.row16, all = per_head * g.heads;
+    for (uint32_t x = mover; x < all; x += movers) {
+        const uint32_t head = x / per_head, r = x % per_head;
+        const int64_t at =
+            (int64_t)head * g.head_stride + (int64_t)(r / g.row16) * g.token_stride + (int64_t)(r % g.row16) * 8;
+        *reinterpret_cast<uint4*>(d + at) = *reinterpret_cast<const uint4*>(s + at);
+    }
+}
+
+__global__ __launch_bounds__(256) void k_pages_tail(PgPlanes c, PgTake t)
+{
+    for (uint64_t u = blockIdx.x; u < (uint64_t)t.n * c.planes; u += gridDim.x)
+        pg_copy_tail(c, t, (uint32_t)(u / c.planes), (uint32_t)(u % c.planes), threadIdx.x, kCopyThreads);
+}
+
+// cr_pages_extend and cr_pages_fork of few sequences in one block, which holds the free pages among up to
+// kOnePages in registers: three launches' work in one. Four children of a 512-page cache forked and freed
+// take 15 us a pass, 20 with the launches. Every read of refs comes before the first write.
+constexpr uint32_t kOneThreads = 1024, kOnePages = kOneThreads * kPgPer;
+
+__global__ __launch_bounds__(1024) void k_pages_one(uint32_t* __restrict__ refs, PgWs w, PgTake t, PgPlanes c, uint32_t* __restrict__ err)
+{
+    __shared__ uint32_t sh[16];
+    uint32_t tot, bad = 0, want = 0;
+    for (uint32_t i0 = 0; i0 < t.n; i0 += kOneThreads) {
+        const uint32_t i = i0 + threadIdx.x;
+        const uint32_t need = i < t.n ? pg_need(t, i, &bad) : 0u;
+        const uint32_t pre = block_exscan_u32(need, sh, &tot);
+        if (i < t.n) w.first[i] = want + pre;
+        want += tot;
+    }
+    if (threadIdx.x == 0) w.first[t.n] = want;
+    const uint32_t p0 = threadIdx.x * kPgPer;
+    uint32_t m = pg_free_mask(refs, t.num_pages, p0);
+    uint32_t r = block_exscan_u32((uint32_t)__popc(m), sh, &tot);
+    const bool short_of = want > tot;
+    if (short_of) bad |= CR_ERR_PAGES_OUT;
+    if (t.parent) {
+        for (uint32_t x = threadIdx.x; x < t.n * t.out_width; x += kOneThreads) {
+            const uint32_t i = x / t.out_width, j = x % t.out_width;
+            const uint32_t p = t.parent[i], len = t.length[i], pages = pages_of(len, t.log_tokens), full = len >> t.log_tokens;
+            uint32_t g = CR_NO_PAGE;
+            if (p < t.rows && pages <= t.width && pages <= t.out_width && j < pages) {
+                g = t.table[(uint64_t)p * t.width + j];
+                if (g >= t.num_pages || refs[g] == 0u) {
+                    bad |= CR_ERR_PAGE;
+                    g = CR_NO_PAGE;
+                }
+            }
+            t.out[x] = j < full && !short_of ? g : CR_NO_PAGE;
         }
     }
+    if (bad) atomicOr(err, bad);
+    if (short_of) return;
+    __syncthreads();
+    if (t.parent)
+        for (uint32_t x = threadIdx.x; x < t.n * t.out_width; x += kOneThreads)
+            if (t.out[x] != CR_NO_PAGE) atomicAdd(&refs[t.out[x]], 1u);
+    __syncthreads();
+    for (; m && r < want; ++r, m &= m - 1u) {
+        const uint32_t p = p0 + (uint32_t)__builtin_ctz(m), i = pg_taker(w, t, r);
+        t.out[(uint64_t)i * t.out_width + pg_had(t, i) + (r - w.first[i])] = p;
+        refs[p] = 1u;
+    }
+    if (!t.parent) return;
+    __syncthreads();
+    // sixteen waves, a child's plane each
+    for (uint32_t u = threadIdx.x >> 6; u < t.n * c.planes; u += kOneThreads / 64u)
+        pg_copy_tail(c, t, u / c.planes, u % c.planes, lane_id(), 64u);
 }
 
 __global__ __launch_bounds__(256) void k_pages_free(uint32_t* __restrict__ refs, uint32_t num_pages, uint32_t log_tokens,
@@ -260,17 +338,20 @@ __global__ __launch_bounds__(256) void k_pages_free(uint32_t* __restrict__ refs,
 
 // Ranks for compaction. With L live pages: free pages below L in order of id go to holes[]; a live
 // page's rank is the number of live pages before it, so those at or above L have the ranks from
-// L - moves on. A free page's rank is CR_NO_PAGE.
-__global__ __launch_bounds__(256) void k_pages_rank(const uint32_t* __restrict__ refs, uint32_t num_pages, uint32_t chunks,
-                                                    PgWs w)
+// L - moves on. A free page's rank is CR_NO_PAGE. kCounted: the chunks' counts are there; else one block of
+// kOneThreads counts all pages itself (up to kOnePages of them, a launch less).
+template <bool kCounted>
+__global__ __launch_bounds__(kCounted ? 256 : 1024) void k_pages_rank(const uint32_t* __restrict__ refs, uint32_t num_pages,
+                                                                      uint32_t chunks, PgWs w)
 {
     __shared__ uint32_t sh[16];
-    uint32_t before, all, tot;
-    pg_sums(w.free_in, chunks, sh, &before, &all);
-    const uint32_t live = num_pages - all;
-    const uint32_t p0 = blockIdx.x * kPgChunk + threadIdx.x * kPgPer;
+    uint32_t before = 0, all, tot;
+    if (kCounted) pg_sums(w.free_in, chunks, sh, &before, &all);
+    const uint32_t p0 = (kCounted ? blockIdx.x * kPgChunk : 0u) + threadIdx.x * kPgPer;
     const uint32_t m = pg_free_mask(refs, num_pages, p0);
     uint32_t f = before + block_exscan_u32((uint32_t)__popc(m), sh, &tot);  // free pages before p
+    if (!kCounted) all = tot;
+    const uint32_t live = num_pages - all;
     for (uint32_t x = 0; x < kPgPer && p0 + x < num_pages; ++x) {
         const uint32_t p = p0 + x;
         if (p == live) *w.moves = f;
@@ -291,20 +372,20 @@ __global__ __launch_bounds__(256) void k_pages_rank(const uint32_t* __restrict__
 constexpr uint32_t kCopyPer = 4;                           // pieces per thread and unit
 constexpr uint32_t kCopyUnit = kCopyThreads * kCopyPer;    // pieces per unit of a block
 
-// One unit of a page's contents, all loads before the stores.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// One unit of a page's contents, all loads before the stores; pieces behind the page repeat its last.
 __device__ __forceinline__ void pg_copy_unit(const uint16_t* __restrict__ s, uint16_t* __restrict__ d, const PgGeom& g, uint32_t part)
 {
-    uint4 r[kCopyPer];
+    u32x4 r[kCopyPer];
     int64_t at[kCopyPer];
 #pragma unroll
     for (uint32_t y = 0; y < kCopyPer; ++y) {
-        const uint32_t x = part * kCopyUnit + y * kCopyThreads + threadIdx.x;
-        at[y] = x < g.page16 ? pg_piece(g, x) : -1;
-        if (at[y] >= 0) r[y] = *reinterpret_cast<const uint4*>(s + at[y]);
+        at[y] = pg_piece(g, min(part * kCopyUnit + y * kCopyThreads + threadIdx.x, g.page16 - 1u));
+        r[y] = *reinterpret_cast<const u32x4*>(s + at[y]);
     }
 #pragma unroll
-    for (uint32_t y = 0; y < kCopyPer; ++y)
-        if (at[y] >= 0) *reinterpret_cast<uint4*>(d + at[y]) = r[y];
+    for (uint32_t y = 0; y < kCopyPer; ++y) *reinterpret_cast<u32x4*>(d + at[y]) = r[y];
 }
 
 // Contents of pages: of the `moves` pages behind the live ones into the holes (w.holes set), or src
@@ -407,6 +488,10 @@ __global__ __launch_bounds__(256) void k_kv_append(KvPages c, uint16_t* __restri
     }
 }
 
+// Up to these sizes one block does the work of a call faster than three launches: sequences of an
+// extension, table entries of a fork, 16-byte pieces of the pages it may copy.
+constexpr uint32_t kOneSeqs = 1024, kOneEntries = 8192, kOnePieces = 16384;
+
 inline PgCopy pg_copy(const cr_kv_cache* c)
 {
     PgCopy m{};
@@ -452,8 +537,12 @@ extern "C" cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_o
     t.num_pages = c->num_pages;
     const hipStream_t st = as_stream(stream);
     (void)hipGetLastError();
-    hipLaunchKernelGGL(k_pages_count, dim3(chunks + 1), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
-    hipLaunchKernelGGL(k_pages_take, dim3(chunks), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
+    if (c->num_pages <= kOnePages && n <= kOneSeqs) {
+        hipLaunchKernelGGL(k_pages_one, dim3(1), dim3(kOneThreads), 0, st, c->refs, w, t, PgPlanes{}, err);
+    } else {
+        hipLaunchKernelGGL(k_pages_count, dim3(chunks + 1), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
+        hipLaunchKernelGGL(k_pages_take, dim3(chunks), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
+    }
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
 }
 
@@ -483,12 +572,15 @@ extern "C" cr_status cr_pages_fork(const cr_kv_cache* c, const uint32_t* table, 
     t.num_pages = c->num_pages;
     const hipStream_t st = as_stream(stream);
     (void)hipGetLastError();
-    hipLaunchKernelGGL(k_pages_count, dim3(chunks + 1 + n), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
-    hipLaunchKernelGGL(k_pages_take, dim3(chunks + n), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
-    const PgGeom g = pg_geom(c);
-    const uint64_t units = (uint64_t)n * 2u * c->layers;
-    hipLaunchKernelGGL(k_pages_tail, dim3((uint32_t)(units < (1u << 20) ? units : (1u << 20))), dim3(kCopyThreads), 0, st,
-                       (uint16_t*)c->k, (uint16_t*)c->v, c->layer_stride, c->page_stride, g, 2u * c->layers, t);
+    const PgPlanes planes{(uint16_t*)c->k, (uint16_t*)c->v, c->layer_stride, c->page_stride, pg_geom(c), 2u * c->layers};
+    const uint64_t units = (uint64_t)n * planes.planes;
+    if (c->num_pages <= kOnePages && n <= kOneSeqs && (uint64_t)n * child_width <= kOneEntries && units * planes.g.page16 <= kOnePieces) {
+        hipLaunchKernelGGL(k_pages_one, dim3(1), dim3(kOneThreads), 0, st, c->refs, w, t, planes, err);
+    } else {
+        hipLaunchKernelGGL(k_pages_count, dim3(chunks + 1 + n), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
+        hipLaunchKernelGGL(k_pages_take, dim3(chunks + n), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
+        hipLaunchKernelGGL(k_pages_tail, dim3((uint32_t)(units < (1u << 20) ? units : (1u << 20))), dim3(kCopyThreads), 0, st, planes, t);
+    }
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
 }
 
@@ -529,8 +621,12 @@ extern "C" cr_status cr_pages_compact(const cr_kv_cache* c, const uint32_t* tabl
     const uint32_t copy_blocks = (uint32_t)(units < 8u * cus ? (units ? units : 1u) : 8u * cus);
     const hipStream_t st = as_stream(stream);
     (void)hipGetLastError();
-    hipLaunchKernelGGL(k_pages_count, dim3(chunks), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
-    hipLaunchKernelGGL(k_pages_rank, dim3(chunks), dim3(kPgThreads), 0, st, c->refs, c->num_pages, chunks, w);
+    if (c->num_pages <= kOnePages) {
+        hipLaunchKernelGGL(k_pages_rank<false>, dim3(1), dim3(kOneThreads), 0, st, c->refs, c->num_pages, chunks, w);
+    } else {
+        hipLaunchKernelGGL(k_pages_count, dim3(chunks), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
+        hipLaunchKernelGGL(k_pages_rank<true>, dim3(chunks), dim3(kPgThreads), 0, st, c->refs, c->num_pages, chunks, w);
+    }
     hipLaunchKernelGGL(k_pages_move, dim3(name_blocks + copy_blocks), dim3(kPgThreads), 0, st, m, w, name_blocks, c->refs,
                        refs_out, table, table_out, length, rows, width, log2_of(c->page_tokens), err);
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
