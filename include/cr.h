@@ -515,8 +515,8 @@ typedef struct {
     const uint32_t* k_off;                  /* u32 [batch + 1], 0 .. total_k                */
 } cr_attn_prompt_args;
 
-/* total_q * heads_q < 2^31 (CR_EINVAL otherwise). Offsets that do not fit set CR_ERR_SEQ; the
- * rows of such a sequence are then unspecified. The workspace holds partial results where
+/* total_q * heads_q < 2^31 (CR_EINVAL otherwise). Offsets that do not fit, or do not cover all rows,
+ * set CR_ERR_SEQ; the rows of such a sequence, or of none, are then unspecified. The workspace holds partial results where
  * the keys of a call with few rows are split over more workgroups; its size follows from the
  * args' scalars alone (pointers and strides are not read). */
 size_t cr_attn_prompt_workspace_bytes(const cr_attn_prompt_args* a);
@@ -546,8 +546,8 @@ typedef struct {
     const uint32_t* own_len;                /* u32 [batch]                                  */
 } cr_attn_shared_args;
 
-/* Errors as cr_attn_prompt; lengths beyond a table's width set CR_ERR_SEQ, pages out of range
- * CR_ERR_PAGE. The workspace size follows from the scalars of the cache and the args. */
+/* Errors as cr_attn_prompt; groups that do not cover all requests and lengths beyond a table's width
+ * set CR_ERR_SEQ, pages out of range CR_ERR_PAGE. The workspace size follows from the scalars of the cache and the args. */
 size_t cr_attn_shared_workspace_bytes(const cr_kv_cache* c, const cr_attn_shared_args* a);
 cr_status cr_attn_shared(const cr_kv_cache* c, const cr_attn_shared_args* a, void* ws, size_t ws_bytes, uint32_t* err,
                          void* stream);

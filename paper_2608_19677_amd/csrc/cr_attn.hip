@@ -5,6 +5,11 @@
 // in one pass, o = sum_j exp(s_j - m) v_j / l, lse = m + ln l. Results over disjoint sets of keys
 // are joined by lse = ln sum exp(lse_p), o = sum exp(lse_p - lse) o_p. Exponentials are taken base
 // 2 with log2(e) folded into the scale.
+//
+// The weights exp(s_j - m) are rounded to 16 bits for the second product. l for the lse is summed
+// before that; what o is divided by is the sum of the rounded weights, so that a row that leans on
+// few keys keeps their values exactly (divided by l, the rounding of one large weight would scale the
+// whole row, up to 2^-8).
 #include "cr_kv.h"
 
 #include <type_traits>
@@ -43,6 +48,10 @@ struct Bf16 {
     {
         return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
     }
+    static __device__ __forceinline__ float add(uint32_t two, float sum)  // sum + both elements
+    {
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
+    }
 };
 
 struct F16 {
@@ -53,6 +62,10 @@ struct F16 {
     static __device__ __forceinline__ uint32_t pack(float x, float y)
     {
         return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), f16x2));
+    }
+    static __device__ __forceinline__ float add(uint32_t two, float sum)
+    {
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, two), __builtin_bit_cast(f16x2, 0x3C003C00u), sum, false);
     }
 };
 
@@ -117,9 +130,11 @@ __device__ __forceinline__ bool get_seq(const Attn& a, uint32_t kind, uint32_t x
         r0 = a.group_off[x];
         r1 = a.group_off[x + 1u];
         if (r0 > r1 || r1 > a.batch) return bad_seq(a);
+        if ((x == 0u && r0 != 0u) || (x + 1u == a.groups && r1 != a.batch)) bad_seq(a);  // requests without a group
     }
     const uint32_t t0 = a.q_off[r0], t1 = a.q_off[r1];
     if (t0 > t1 || t1 > a.total_q) return bad_seq(a);
+    if ((r0 == 0u && t0 != 0u) || (r1 == a.batch && t1 != a.total_q)) bad_seq(a);  // rows without a sequence
     s->tok0 = t0;
     s->nq = t1 - t0;
     s->least = 0;
@@ -133,6 +148,7 @@ __device__ __forceinline__ bool get_seq(const Attn& a, uint32_t kind, uint32_t x
         uint32_t pre = 0, own = 0;
         if (kind != kOwn) {
             const uint32_t g = kind == kGroup ? x : wave_find(a.groups, x, [&](uint32_t i) { return a.group_off[i]; });
+            if (kind != kGroup && (a.group_off[g] > x || a.group_off[g + 1u] <= x)) return bad_seq(a);
             pre = a.prefix_len[g];
             if (pages_of(pre, a.pg.log_tokens) > a.prefix_width) return bad_seq(a);
             s->table0 = a.prefix_table + (uint64_t)g * a.prefix_width;
@@ -377,7 +393,7 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
     }
 
     f32x16 o[kDim / 32];
-    float mc = kNoMax, sum = 0.f;
+    float mc = kNoMax, sum = 0.f, rounded = 0.f;  // sums of the weights and of the rounded ones
 #pragma unroll
     for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
@@ -398,7 +414,7 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
 
         f32x16 s[2];            // scores of the two halves of a tile
         uint32_t pk[2][8];      // their weights
-        float top, part[2];
+        float top, part[2], part_rounded;
         float late = 1.f;       // factor that o lacks: its values come a half tile after their weights
         bool is_late = false;
         const uint32_t k_lane = half * kKeyRun + col * 8u;
@@ -447,6 +463,7 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
                 late = __builtin_amdgcn_exp2f(mc - up);
                 is_late = true;
                 sum *= late;
+                rounded *= late;
                 mc = up;
             }
         };
@@ -457,6 +474,7 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
             part[1] = i ? part[1] + y : y;
             pk[h][i / 2] = E::pack(x, y);
             stay(pk[h][i / 2]);
+            part_rounded = E::add(pk[h][i / 2], i ? part_rounded : 0.f);
         };
         auto value = [&](s16x8 vf, int h, int n) CR_INLINE {
             const int ks = n / (kDim / 32), d = n % (kDim / 32);
@@ -502,7 +520,9 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
                 __builtin_amdgcn_sched_barrier(0);
             }
             sum += part[0] + part[1];
+            rounded += part_rounded;
             stay(sum);
+            stay(rounded);
             move_maximum();
         };
 
@@ -558,10 +578,10 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
         ld.report(a);
     }
 
-    const float total = both_sum(sum);
+    const float total = both_sum(sum), total_rounded = both_sum(rounded);
     if (wrow + col >= rows) return;
-    const bool none = total == 0.f;  // the largest weight of a row that sees a key is 2^-kSlack or more
-    const float inv = none ? 0.f : 1.f / total;
+    const bool none = total == 0.f;  // the largest weight of a row that sees a key is 1 or more
+    const float inv = none ? 0.f : 1.f / total_rounded;
     const float lse2 = none ? -INFINITY : mc + log2f(total);
     const uint64_t orow = (uint64_t)tok * a.heads_q + head;
     if (a.part_o) {
@@ -618,7 +638,7 @@ struct NarrowLds {
     uint32_t at[kThreads];  // units before the sequence, from the first of the 256
     uint32_t sums[16];
     uint32_t tok0[kThreads], nq[kThreads], n[kThreads], key0[kThreads];
-    float row_max[kWaves][32], row_sum[kWaves][32];
+    float row_max[kWaves][32], row_sum[kWaves][32], row_rounded[kWaves][32];
 };
 
 template <typename E, int kDim, bool kPaged>
@@ -646,6 +666,7 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             r1 = a.group_off[y + 1u];
         }
         bool ok = r0 <= r1 && r1 <= a.batch;
+        if (kPaged && !own && ((y == 0u && r0 != 0u) || (y + 1u == a.groups && r1 != a.batch))) atomicOr(a.err, CR_ERR_SEQ);
         if (kPaged) {
             *n = own ? a.own_len[y] : a.prefix_len[y];
             ok = ok && pages_of(*n, a.pg.log_tokens) <= (own ? a.own_width : a.prefix_width);
@@ -659,6 +680,7 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             *tok0 = a.q_off[r0];
             *nq = a.q_off[r1] - *tok0;
             ok = *tok0 + *nq >= *tok0 && *tok0 + *nq <= a.total_q;
+            if ((r0 == 0u && *tok0 != 0u) || (r1 == a.batch && *tok0 + *nq != a.total_q)) atomicOr(a.err, CR_ERR_SEQ);
         }
         if (!ok) {
             atomicOr(a.err, CR_ERR_SEQ);
@@ -774,7 +796,7 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
         for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        float mc = kNoMax, sum = 0.f;
+        float mc = kNoMax, sum = 0.f, rounded = 0.f;
         uint32_t k0 = st.key_begin + (pairs ? wv >> 1 : wv) * kNarrowKeys;
         if (k0 < key_end && wave_row < rows) {
             Loader<kDim, kPaged, kNarrowKeys, kWave> ld;
@@ -814,13 +836,14 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
                     const float up = fmaxf(mc, top), f = __builtin_amdgcn_exp2f(mc - up);
                     mc = up;
                     sum *= f;
+                    rounded *= f;
 #pragma unroll
                     for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) o[d][i] *= f;
                 }
                 uint32_t pk[8];
-                float t[4];
+                float t[4], part_rounded = 0.f;
 #pragma unroll
                 for (int i = 0; i < 16; i += 2) {
                     const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c, -mc));
@@ -828,8 +851,10 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
                     t[i & 3] = i < 4 ? x : t[i & 3] + x;
                     t[(i & 3) + 1] = i < 4 ? y : t[(i & 3) + 1] + y;
                     pk[i / 2] = E::pack(x, y);
+                    part_rounded = E::add(pk[i / 2], part_rounded);
                 }
                 sum += (t[0] + t[1]) + (t[2] + t[3]);
+                rounded += part_rounded;
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks) {
                     const u32x4 w = {pk[ks * 4], pk[ks * 4 + 1], pk[ks * 4 + 2], pk[ks * 4 + 3]};
@@ -846,9 +871,11 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             ld.report(a);
         }
         sum = both_sum(sum);
+        rounded = both_sum(rounded);
         if (half == 0) {
             sh.row_max[wv][col] = mc;
             sh.row_sum[wv][col] = sum;
+            sh.row_rounded[wv][col] = rounded;
         }
 #pragma unroll
         for (int d = 0; d < kDim / 32; ++d)
@@ -860,18 +887,19 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
         for (uint32_t y = threadIdx.x; y < rows * (kDim / 4u); y += kThreads) {
             const uint32_t row = y / (kDim / 4u), r = row & 31u, e = y % (kDim / 4u) * 4u, mm = row0 + row;
             const uint32_t w0 = row >> 5, w_step = pairs ? 2u : 1u;  // the wavefronts that worked on the row
-            float mx = sh.row_max[w0][r], total = 0.f;
+            float mx = sh.row_max[w0][r], total = 0.f, total_rounded = 0.f;
             for (uint32_t w = w0 + w_step; w < kWaves; w += w_step) mx = fmaxf(mx, sh.row_max[w][r]);
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
             for (uint32_t w = w0; w < kWaves; w += w_step) {
                 const float f = __builtin_amdgcn_exp2f(sh.row_max[w][r] - mx);
                 const f32x4 v = *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds + w * narrow_lds<kDim>()) + r * kSumRow + e);
                 total = __builtin_fmaf(f, sh.row_sum[w][r], total);
+                total_rounded = __builtin_fmaf(f, sh.row_rounded[w][r], total_rounded);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(f, v[i], acc[i]);
             }
             const bool none = total == 0.f;
-            const float inv = none ? 0.f : 1.f / total, lse2 = none ? -INFINITY : mx + log2f(total);
+            const float inv = none ? 0.f : 1.f / total_rounded, lse2 = none ? -INFINITY : mx + log2f(total);
             const uint32_t ot = it.tok0 + mm / a.group, oh = head_kv * a.group + mm % a.group;
             const uint64_t orow = (uint64_t)ot * a.heads_q + oh;
             if (a.part_o) {
@@ -981,7 +1009,7 @@ struct Shape {
 
 constexpr uint32_t kFewRows = 64;        // mean rows of a sequence up to which the narrow kernel takes it
 constexpr uint32_t kWholeRows = 128;     // mean rows of a request from which its prefix is read again, not joined
-constexpr uint32_t kSplitKeys = 256;     // keys a workgroup should have at least where a call is split
+constexpr uint32_t kSplitKeys = 384;     // keys a workgroup should have at least where a call is split
 constexpr uint32_t kSplitMax = 32;
 constexpr uint32_t kLongKeys = 1024;     // mean keys from which blocks of 256 rows pay
 constexpr uint32_t kNarrowParts = 63;    // shares a sequence's keys may fall into

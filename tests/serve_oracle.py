@@ -151,3 +151,33 @@ class Pages:
             self.refs[d], self.refs[s] = self.refs[s], 0
         table = [[name.get(g, g) if j < self.pages(n) else g for j, g in enumerate(row)] for row, n in zip(table, length)]
         return table, list(name.items())
+
+
+def head_on_gpu(q, parts, scale):
+    """`rows` for one head's many rows, float64 on the GPU: q [n, D]; parts (k, v, limit [n])."""
+    dev = q.device
+    s, ab = [], []
+    for k, _, lim in parts:
+        seen = torch.arange(k.shape[0], device=dev) < lim[:, None]
+        s.append(torch.where(seen, (q @ k.t().contiguous()) * scale, -math.inf))
+        ab.append(torch.where(seen, (q.abs() @ k.abs().t().contiguous()) * scale, 0.0).amax(1) if k.shape[0] else torch.zeros(len(q), dtype=q.dtype, device=dev))
+    s, v = torch.cat(s, 1), torch.cat([p[1] for p in parts])
+    lse = torch.logsumexp(s, 1)
+    w = torch.exp(s - torch.where(lse == -math.inf, torch.zeros_like(lse), lse)[:, None])
+    return w @ v, lse, w @ v.abs(), torch.stack(ab).amax(0)
+
+
+def many(q, seqs, hkv, scale):
+    """Sequences of (first row, rows, parts) with parts (k [m, Hkv, D], v, limit): the four results of `rows`
+    for all rows and heads, flat."""
+    n, hq, d = q.shape
+    g = hq // hkv
+    res = [torch.zeros(n, hq, d, dtype=torch.float64, device=q.device), torch.full((n, hq), -math.inf, dtype=torch.float64, device=q.device),
+           torch.zeros(n, hq, d, dtype=torch.float64, device=q.device), torch.zeros(n, hq, dtype=torch.float64, device=q.device)]
+    for a, m, parts in seqs:
+        for h in range(hkv):
+            rows_ = q[a:a + m, h * g:(h + 1) * g].double().transpose(0, 1).reshape(-1, d)
+            got = head_on_gpu(rows_, [(k[:, h].double(), v[:, h].double(), lim.repeat(g)) for k, v, lim in parts], scale)
+            for x, y in zip(res, got):
+                x[a:a + m, h * g:(h + 1) * g] = y.reshape(g, m, *y.shape[1:]).transpose(0, 1)
+    return flat([x.cpu().numpy() for x in res])
