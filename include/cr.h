@@ -405,6 +405,7 @@ cr_status cr_keymap_scatter(const void* table, size_t table_bytes, uint32_t capa
 #define CR_MAX_HEADS 1024            /* heads of queries, or of keys and values         */
 #define CR_MAX_LAYERS 1024           /* layers of a cache                               */
 #define CR_MAX_PAGES (1u << 26)      /* pages of a cache                                */
+#define CR_MAX_KEYS 0x7FFFFC00u      /* total_k, and tokens of both table widths, are below this */
 
 /* Rows of a packed tensor [tokens][heads][dim]: element (t, h, x) at p[t * token_stride +
  * h * head_stride + x]. Strides count elements, are multiples of 8, not negative and below 2^31
@@ -443,7 +444,7 @@ size_t cr_pages_workspace_bytes(uint32_t num_pages, uint32_t n);
  * ceil(len_old[i] / page_tokens) <= j < ceil(len_new[i] / page_tokens) become free pages, the
  * lowest ids first in the order of (i, j), with refs 1. len_old, len_new u32 [n] (len_old
  * NULL: all 0); table u32 [n][width]. A sequence that shrinks or passes the table's width
- * sets CR_ERR_SEQ and takes none. Too few free pages set CR_ERR_PAGES_OUT, and then nothing
+ * sets CR_ERR_SEQ and takes none. n * width < 2^32 here and in cr_pages_free. Too few free pages set CR_ERR_PAGES_OUT, and then nothing
  * is changed. */
 cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_old, const uint32_t* len_new, uint32_t n,
                           uint32_t* table, uint32_t width, void* ws, size_t ws_bytes, uint32_t* err, void* stream);
@@ -515,8 +516,9 @@ typedef struct {
     const uint32_t* k_off;                  /* u32 [batch + 1], 0 .. total_k                */
 } cr_attn_prompt_args;
 
-/* total_q * heads_q < 2^31 (CR_EINVAL otherwise). Offsets that do not fit, or do not cover all rows,
- * set CR_ERR_SEQ; the rows of such a sequence, or of none, are then unspecified. The workspace holds partial results where
+/* total_q * heads_q < 2^31, total_k < CR_MAX_KEYS (CR_EINVAL otherwise; so are calls of more workgroups than
+ * a launch takes). Offsets that do not fit, or do not cover all rows, set CR_ERR_SEQ; the rows of such a
+ * sequence, or of none, are then unspecified, and all rows where q_off (or group_off) is out of order. The workspace holds partial results where
  * the keys of a call with few rows are split over more workgroups; its size follows from the
  * args' scalars alone (pointers and strides are not read). */
 size_t cr_attn_prompt_workspace_bytes(const cr_attn_prompt_args* a);

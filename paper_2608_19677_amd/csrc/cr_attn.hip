@@ -638,6 +638,7 @@ struct NarrowLds {
     uint32_t at[kThreads];  // units before the sequence, from the first of the 256
     uint32_t sums[16];
     uint32_t tok0[kThreads], nq[kThreads], n[kThreads], key0[kThreads];
+    uint32_t disorder[kWaves];
     float row_max[kWaves][32], row_sum[kWaves][32], row_rounded[kWaves][32];
 };
 
@@ -655,7 +656,9 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
     // Sequences 0 .. first_n of the first list, then those of the second.
     const uint32_t first_n = (lists & 1u) ? (kPaged ? a.groups : a.batch) : 0u;
     const uint32_t all_n = first_n + ((lists & 2u) ? a.batch : 0u);
-    // Units of sequence x; what does not fit has none.
+    // Units of sequence x; what does not fit has none. Where offsets of rows or groups are out of order
+    // sequences may overlap, and the sum of their units passes what the host allowed for: no list is worked on.
+    bool disorder = false;
     auto units = [&](uint32_t x, uint32_t* tok0, uint32_t* nq, uint32_t* n, uint32_t* key0) CR_INLINE -> uint32_t {
         if (x >= all_n) return 0u;
         const bool own = x >= first_n;
@@ -666,6 +669,7 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             r1 = a.group_off[y + 1u];
         }
         bool ok = r0 <= r1 && r1 <= a.batch;
+        disorder |= !ok;
         if (kPaged && !own && ((y == 0u && r0 != 0u) || (y + 1u == a.groups && r1 != a.batch))) atomicOr(a.err, CR_ERR_SEQ);
         if (kPaged) {
             *n = own ? a.own_len[y] : a.prefix_len[y];
@@ -680,6 +684,7 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             *tok0 = a.q_off[r0];
             *nq = a.q_off[r1] - *tok0;
             ok = *tok0 + *nq >= *tok0 && *tok0 + *nq <= a.total_q;
+            disorder |= !ok;
             if ((r0 == 0u && *tok0 != 0u) || (r1 == a.batch && *tok0 + *nq != a.total_q)) atomicOr(a.err, CR_ERR_SEQ);
         }
         if (!ok) {
@@ -694,6 +699,8 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
     auto window = [&](uint32_t x0) CR_INLINE {
         uint32_t tok0 = 0, nq = 0, n = 0, key0 = 0;
         const uint32_t v = units(x0 + threadIdx.x, &tok0, &nq, &n, &key0);
+        const uint64_t wrong = ballot(disorder);
+        if (lane == 0) sh.disorder[wv] = wrong != 0;
         const uint32_t at = block_exscan_u32(v, sh.sums, &here);
         here = __builtin_amdgcn_readfirstlane(here);
         sh.at[threadIdx.x] = at;
@@ -707,9 +714,14 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
     uint32_t all = here;
     for (uint32_t x0 = kThreads; x0 < all_n; x0 += kThreads) {
         uint32_t t0, t1, t2, t3, sum;
-        block_exscan_u32(units(x0 + threadIdx.x, &t0, &t1, &t2, &t3), sh.sums, &sum);
+        const uint32_t v = units(x0 + threadIdx.x, &t0, &t1, &t2, &t3);
+        const uint64_t wrong = ballot(disorder);
+        if (lane == 0) sh.disorder[wv] = wrong != 0;
+        block_exscan_u32(v, sh.sums, &sum);
         all += __builtin_amdgcn_readfirstlane(sum);
     }
+    for (uint32_t w = 0; w < kWaves; ++w)
+        if (sh.disorder[w]) return;
     const uint32_t index = block / a.heads_kv, of = blocks / a.heads_kv;
     const uint32_t share = max(all / of + 1u, a.least_share);
     if ((uint64_t)index * share >= all) return;

@@ -459,32 +459,36 @@ __global__ __launch_bounds__(256) void k_pages_move(PgCopy c, PgWs w, uint32_t n
     }
 }
 
-// New tokens: a block per token, a thread per 16 bytes of its keys and values.
+// New tokens: a block per token (of more than kAppendBlocks: in turn), a thread per 16 bytes of its keys
+// and values.
+constexpr uint32_t kAppendBlocks = 1u << 20;
+
 __global__ __launch_bounds__(256) void k_kv_append(KvPages c, uint16_t* __restrict__ ck, uint16_t* __restrict__ cv, cr_rows k,
                                                    cr_rows v, uint32_t total, const uint32_t* __restrict__ off,
                                                    const uint32_t* __restrict__ length, uint32_t n,
                                                    const uint32_t* __restrict__ table, uint32_t width,
                                                    uint32_t* __restrict__ err)
 {
-    const uint32_t tok = blockIdx.x;
-    const uint32_t i = wave_find(n, tok, [&](uint32_t x) { return off[x]; });
-    const uint32_t o0 = off[i], o1 = off[i + 1], len = length[i];
-    if (tok < o0 || tok >= o1 || o1 > total || o1 - o0 > len || pages_of(len, c.log_tokens) > width) {
-        if (threadIdx.x == 0) atomicOr(err, CR_ERR_SEQ);
-        return;
-    }
-    const uint32_t pos = len - (o1 - tok), page = table[(uint64_t)i * width + (pos >> c.log_tokens)];
-    if (page >= c.num_pages) {
-        if (threadIdx.x == 0) atomicOr(err, CR_ERR_PAGE);
-        return;
-    }
-    const int64_t at = (int64_t)page * c.page_stride + (int64_t)(pos & ((1u << c.log_tokens) - 1u)) * c.token_stride;
     const uint32_t row16 = c.dim / 8u, per = c.heads * row16;
-    for (uint32_t x = threadIdx.x; x < 2u * per; x += kCopyThreads) {
-        const uint32_t y = x < per ? x : x - per, h = y / row16, e = y % row16 * 8u;
-        const cr_rows& r = x < per ? k : v;
-        const uint16_t* s = (const uint16_t*)r.p + (int64_t)tok * r.token_stride + (int64_t)h * r.head_stride + e;
-        *reinterpret_cast<uint4*>((x < per ? ck : cv) + at + (int64_t)h * c.head_stride + e) = *reinterpret_cast<const uint4*>(s);
+    for (uint32_t tok = blockIdx.x; tok < total; tok += gridDim.x) {
+        const uint32_t i = wave_find(n, tok, [&](uint32_t x) { return off[x]; });
+        const uint32_t o0 = off[i], o1 = off[i + 1], len = length[i];
+        if (tok < o0 || tok >= o1 || o1 > total || o1 - o0 > len || pages_of(len, c.log_tokens) > width) {
+            if (threadIdx.x == 0) atomicOr(err, CR_ERR_SEQ);
+            continue;
+        }
+        const uint32_t pos = len - (o1 - tok), page = table[(uint64_t)i * width + (pos >> c.log_tokens)];
+        if (page >= c.num_pages) {
+            if (threadIdx.x == 0) atomicOr(err, CR_ERR_PAGE);
+            continue;
+        }
+        const int64_t at = (int64_t)page * c.page_stride + (int64_t)(pos & ((1u << c.log_tokens) - 1u)) * c.token_stride;
+        for (uint32_t x = threadIdx.x; x < 2u * per; x += kCopyThreads) {
+            const uint32_t y = x < per ? x : x - per, h = y / row16, e = y % row16 * 8u;
+            const cr_rows& r = x < per ? k : v;
+            const uint16_t* s = (const uint16_t*)r.p + (int64_t)tok * r.token_stride + (int64_t)h * r.head_stride + e;
+            *reinterpret_cast<uint4*>((x < per ? ck : cv) + at + (int64_t)h * c.head_stride + e) = *reinterpret_cast<const uint4*>(s);
+        }
     }
 }
 
@@ -523,6 +527,7 @@ extern "C" cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_o
     if (!good_cache(c) || !c->refs || !err || !ws || !aligned4(ws) || (n > 0 && (!len_new || (width > 0 && !table))) ||
         n > (1u << 24) || width > (1u << 28))
         return CR_EINVAL;
+    if ((uint64_t)n * width >= ((uint64_t)1 << 32)) return CR_EINVAL;  // pages that the sequences take are counted in 32 bits
     if (ws_bytes < cr_pages_workspace_bytes(c->num_pages, n)) return CR_ESIZE;
     if (n == 0) return CR_OK;
     const uint32_t chunks = pg_chunks(c->num_pages);
@@ -590,7 +595,7 @@ extern "C" cr_status cr_pages_free(const cr_kv_cache* c, const uint32_t* table, 
     using namespace cr;
     if (!good_cache(c) || !c->refs || !err || n > (1u << 24) || width > (1u << 28) || (n > 0 && (!length || (width > 0 && !table))))
         return CR_EINVAL;
-    if ((uint64_t)n * (width ? width : 1u) > ((uint64_t)1 << 38)) return CR_EINVAL;
+    if ((uint64_t)n * (width ? width : 1u) >= ((uint64_t)1 << 32) - kPgThreads) return CR_EINVAL;  // threads of a launch
     if (n == 0) return CR_OK;
     const uint64_t threads = (uint64_t)n * (width ? width : 1u);
     (void)hipGetLastError();
@@ -661,7 +666,7 @@ extern "C" cr_status cr_kv_append(const cr_kv_cache* c, uint32_t layer, const cr
     KvPages p = kv_pages(c);
     const int64_t at = (int64_t)layer * c->layer_stride;
     (void)hipGetLastError();
-    hipLaunchKernelGGL(k_kv_append, dim3(total), dim3(kCopyThreads), 0, as_stream(stream), p, (uint16_t*)c->k + at,
+    hipLaunchKernelGGL(k_kv_append, dim3(total < kAppendBlocks ? total : kAppendBlocks), dim3(kCopyThreads), 0, as_stream(stream), p, (uint16_t*)c->k + at,
                        (uint16_t*)c->v + at, *k, *v, total, off, length, n, table, width, err);
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
 }

@@ -182,3 +182,30 @@ def test_offsets_that_do_not_cover_are_reported():
             say(f"[case] groups {go}, {ql[0]} queries")
             serve.attend_shared(q, pool, 0, _i32(_cum(ql)), _i32(go), ptab, _i32([20, 30]), otab, _i32([40] * 4), 0.1)
             assert int(pool.err.item()) == B.CR_ERR_SEQ
+
+
+def test_offsets_out_of_order_stop_the_call():
+    """Rows counted again and again by offsets that go back: more units than 32 bits hold, none is worked on."""
+    n, total_k = 4096, 65536
+    q = torch.zeros(32768, 8, 64, dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros(total_k, 1, 64, dtype=torch.bfloat16, device="cuda")
+    qo, ko = [32768 * (i % 2) for i in range(n + 1)], [total_k * (i % 2) for i in range(n + 1)]
+    ws = serve.prompt_workspace(q, k, _i32(qo))
+    say("[case] prompt offsets out of order, 4,096 sequences")
+    serve.attend_prompt(q, k, k, _i32(qo), _i32(ko), 0.1, ws=ws)
+    assert int(ws.err.item()) == B.CR_ERR_SEQ
+
+
+def test_many_small_weights_in_sixteen_bit_floats():
+    """60,000 keys of weight 2^-26 beside one of 1: below what a 16-bit float near 1 resolves, together 2^-10.
+    The weights are exact, the output's rounding is 2^-11 of it, the scores' (26 in 24 bits) 2^-19."""
+    n, d = 60001, 64
+    q = torch.zeros(1, 1, d, dtype=torch.float16, device="cuda")
+    k = torch.zeros(n, 1, d, dtype=torch.float16, device="cuda")
+    v = torch.ones(n, 1, d, dtype=torch.float16, device="cuda")
+    q[..., 0], k[0, 0, 0], v[0] = 1.0, 26.0, 0.0
+    rest = (n - 1) * 2.0 ** -26
+    for rows in (1, 300):  # few rows, and tiles of rows
+        say(f"[case] small weights, {rows} rows")
+        out = serve.attend_prompt(q.expand(rows, 1, d).contiguous(), k, v, _i32([0, rows]), _i32([0, n]), math.log(2.0), causal=False)
+        assert (out.double() / (rest / (1 + rest)) - 1).abs().max() <= 2.0 ** -10

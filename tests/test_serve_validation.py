@@ -170,3 +170,14 @@ def test_wrappers_refuse_tensors_that_do_not_fit():
         serve.attend_prompt(q.transpose(1, 2), q.transpose(1, 2), q.transpose(1, 2), off, off, 1.0)
     with pytest.raises(B.CrError, match="device tensors"):
         serve.attend_prompt(q, q, q, off, off, 1.0)
+
+
+def test_counts_that_pass_32_bits_are_refused(L):
+    c = ctypes.byref(_cache())
+    assert L.cr_pages_extend(c, None, FAKE, 1 << 16, FAKE, 1 << 16, FAKE, 1 << 40, FAKE, None) == B.CR_EINVAL
+    assert L.cr_pages_free(c, FAKE, 1 << 16, FAKE, 1 << 16, FAKE, None) == B.CR_EINVAL
+    assert L.cr_attn_prompt(ctypes.byref(_prompt(total_k=0x7FFFFC00)), FAKE, 1 << 50, FAKE, None) == B.CR_EINVAL
+    wide = _shared(prefix_width=(1 << 27) - 64, own_width=0)  # 2^31 - 1,024 tokens
+    assert L.cr_attn_shared(c, ctypes.byref(wide), FAKE, 1 << 50, FAKE, None) == B.CR_EINVAL
+    many = _prompt(heads_q=1024, heads_kv=1024, batch=1 << 15, total_q=1 << 20, total_k=1 << 30)  # 2^25 workgroups
+    assert L.cr_attn_prompt(ctypes.byref(many), FAKE, 1 << 50, FAKE, None) == B.CR_EINVAL
