@@ -40,6 +40,7 @@ constexpr float kNoMax = -3.0e38f;       // running maximum before the first key
 constexpr float kSlack = 8.f;            // weights may reach 2^kSlack before the maximum is moved
 
 struct Bf16 {
+    static constexpr float kLift = 0.f;
     static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -54,7 +55,10 @@ struct Bf16 {
     }
 };
 
+// The largest weight lies between 2^kLift and 2^(kLift + kSlack), so that 16 bits hold weights down to 2^-30
+// of it at least; around 1 those below 2^-24 would be lost, and many of them may add up.
 struct F16 {
+    static constexpr float kLift = 6.f;
     static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -458,8 +462,8 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
                 scale_o(late);
                 is_late = false;
             }
-            if (ballot(top > mc + kSlack)) {
-                const float up = fmaxf(mc, top);
+            if (ballot(top > mc + (kSlack + E::kLift))) {
+                const float up = fmaxf(mc, top - E::kLift);
                 late = __builtin_amdgcn_exp2f(mc - up);
                 is_late = true;
                 sum *= late;
@@ -580,7 +584,7 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
 
     const float total = both_sum(sum), total_rounded = both_sum(rounded);
     if (wrow + col >= rows) return;
-    const bool none = total == 0.f;  // the largest weight of a row that sees a key is 1 or more
+    const bool none = total == 0.f;  // the largest weight of a row that sees a key is 2^kLift or more
     const float inv = none ? 0.f : 1.f / total_rounded;
     const float lse2 = none ? -INFINITY : mc + log2f(total);
     const uint64_t orow = (uint64_t)tok * a.heads_q + head;
@@ -844,8 +848,8 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
                 for (int i = 2; i < 16; i += 2)
                     top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top, s[i]), s[i + 1]);
                 top = both_max(top) * a.c;
-                if (ballot(top > mc + kSlack)) {
-                    const float up = fmaxf(mc, top), f = __builtin_amdgcn_exp2f(mc - up);
+                if (ballot(top > mc + (kSlack + E::kLift))) {
+                    const float up = fmaxf(mc, top - E::kLift), f = __builtin_amdgcn_exp2f(mc - up);
                     mc = up;
                     sum *= f;
                     rounded *= f;
@@ -1113,7 +1117,7 @@ inline bool good_prompt_sizes(const cr_attn_prompt_args* p)
 {
     return p && p->dtype <= CR_F16 && good_heads(p->heads_q, p->heads_kv) && (p->dim == 64 || p->dim == 128) &&
            p->causal <= 1 && good_scale(p->scale) && (uint64_t)p->total_q * p->heads_q < (1ull << 31) &&
-           p->total_k < (1u << 31) && p->batch <= (1u << 24) && (p->batch > 0 || p->total_q == 0);
+           p->total_k < CR_MAX_KEYS && p->batch <= (1u << 24) && (p->batch > 0 || p->total_q == 0);
 }
 
 inline bool good_shared_sizes(const cr_kv_cache* c, const cr_attn_shared_args* p)
@@ -1121,7 +1125,7 @@ inline bool good_shared_sizes(const cr_kv_cache* c, const cr_attn_shared_args* p
     return good_cache_sizes(c) && p && good_heads(p->heads_q, c->heads) && p->layer < c->layers && good_scale(p->scale) &&
            (uint64_t)p->total_q * p->heads_q < (1ull << 31) && p->batch <= (1u << 24) && p->groups <= p->batch &&
            (p->total_q == 0 || p->groups > 0) &&
-           ((uint64_t)p->prefix_width + p->own_width) * c->page_tokens < (1ull << 31);
+           ((uint64_t)p->prefix_width + p->own_width) * c->page_tokens < CR_MAX_KEYS;
 }
 
 // Lengths are on the device: the mean stands for them, and a sequence's chunks grow where it is longer.
@@ -1240,7 +1244,8 @@ cr_status dispatch(Attn& a, const Shape& s, void* ws, uint32_t dtype, uint32_t d
     const hipStream_t st = as_stream(stream);
     const uint64_t rows = (uint64_t)a.total_q * a.group;
     for (uint32_t i = 0; i < s.wides; ++i)
-        if ((rows / s.wide[i].rows + a.batch) * (s.wide[i].kind == kOwn ? s.own_slots : s.slots) * a.heads_kv >= (1ull << 31)) return CR_EINVAL;
+        if ((rows / s.wide[i].rows + a.batch) * (s.wide[i].kind == kOwn ? s.own_slots : s.slots) * a.heads_kv >= (1ull << 32) / (8u * kWave))
+            return CR_EINVAL;  // threads of a launch
     a.first = s.first;
     a.chunk = s.chunk;
     a.slots = s.slots;
