@@ -349,7 +349,62 @@ struct Loader {
 // unit to itself (one barrier per tile), else two and a barrier more.
 struct Part {
     uint32_t kind, tiles, blocks;  // blocks: tiles x slots x key heads
+    uint32_t sorted;               // sequences in the order of their keys, the longest first
 };
+
+// The tile of a rank where sequences follow each other by falling numbers of keys, each with its last tile
+// first: a call of several rounds of blocks then ends with short ones. For up to 64 sequences, one a lane;
+// what does not fit has no tiles. false: no such tile.
+constexpr uint32_t kSortSeqs = 64;
+
+template <bool kPaged, uint32_t kRows>
+__device__ __forceinline__ bool longest_first(const Attn& a, uint32_t kind, uint32_t rank, uint32_t* x, uint32_t* row0)
+{
+    const uint32_t lane = lane_id(), seqs = kPaged && kind == kGroup ? a.groups : a.batch, y = min(lane, seqs - 1u);
+    uint32_t r0 = y, r1 = y + 1u, n;
+    bool ok = true, covers = true;
+    if (kPaged) {
+        const uint32_t g = min(lane, a.groups - 1u), g0 = a.group_off[g], g1 = a.group_off[g + 1u], prefix = a.prefix_len[g];
+        covers = (g != 0u || g0 == 0u) && (g + 1u != a.groups || g1 == a.batch);
+        if (kind == kGroup) {
+            r0 = g0;
+            r1 = g1;
+            ok = r0 <= r1 && r1 <= a.batch;
+            n = prefix;
+        } else {
+            n = a.own_len[y];
+            if (kind == kWhole) {
+                uint32_t of = 0;
+                for (uint32_t j = 1; j < a.groups; ++j) of = (uint32_t)__builtin_amdgcn_readlane((int)g0, (int)j) <= y ? j : of;
+                n += (uint32_t)__shfl((int)prefix, (int)of);
+            }
+        }
+    } else {
+        const uint32_t k0 = a.k_off[y], k1 = a.k_off[y + 1u];
+        covers = k0 <= k1 && k1 <= a.total_k;
+        n = k1 - k0;
+    }
+    uint32_t t0 = 0, t1 = 0;
+    if (ok) {
+        t0 = a.q_off[r0];
+        t1 = a.q_off[r1];
+        ok = t0 <= t1 && t1 <= a.total_q;
+        covers = covers && (r0 != 0u || t0 == 0u) && (r1 != a.batch || t1 == a.total_q);
+    }
+    if (!ok || !covers) atomicOr(a.err, CR_ERR_SEQ);
+    const uint32_t tiles = ok && lane < seqs ? ((t1 - t0) * a.group + kRows - 1u) / kRows : 0u;
+    uint32_t before = 0;  // tiles of longer sequences
+    for (uint32_t j = 0; j < seqs; ++j) {
+        const uint32_t nj = (uint32_t)__builtin_amdgcn_readlane((int)n, (int)j), tj = (uint32_t)__builtin_amdgcn_readlane((int)tiles, (int)j);
+        before += nj > n || (nj == n && j < lane) ? tj : 0u;
+    }
+    const uint64_t mine = ballot(before <= rank && rank - before < tiles);
+    if (!mine) return false;
+    const uint32_t l = (uint32_t)__builtin_ctzll(mine);
+    *x = l;
+    *row0 = ((uint32_t)__builtin_amdgcn_readlane((int)tiles, (int)l) - 1u - (rank - (uint32_t)__builtin_amdgcn_readlane((int)before, (int)l))) * kRows;
+    return true;
+}
 
 constexpr uint32_t val_bufs(uint32_t waves) { return waves == 8u ? 3u : 2u; }
 constexpr uint32_t wide_lds(uint32_t waves, uint32_t dim)  // elements
@@ -368,17 +423,24 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
 
     // Tiles of sequence x start at floor(first row / kRows) + x: steps of at least ceil(rows / kRows),
     // so the tiles of all sequences fit into floor(all rows / kRows) + sequences without a pass that
-    // counts them; some are empty. The last rows of causal sequences, the longest, come first.
+    // counts them; some are empty. The last rows of causal sequences, the longest, come first. Where the
+    // blocks are more than one round of few sequences, the longest sequences do too.
     const uint32_t head_kv = block % a.heads_kv, id = block / a.heads_kv;
     const uint32_t slots = kind == kOwn ? a.own_slots : a.slots;
     const uint32_t split = id / tiles, tile = tiles - 1u - id % tiles;  // tiles that read the same keys side by side
     auto start = [&](uint32_t x) {
         return a.q_off[kPaged && kind == kGroup ? min(a.group_off[x], a.batch) : x] * a.group / kRows + x;
     };
-    const uint32_t x = wave_find(kPaged && kind == kGroup ? a.groups : a.batch, tile, start);
+    uint32_t x, row0;
+    if (part_of.sorted) {
+        if (!longest_first<kPaged, kRows>(a, kind, id % tiles, &x, &row0)) return;
+    } else {
+        x = wave_find(kPaged && kind == kGroup ? a.groups : a.batch, tile, start);
+        row0 = (tile - min(start(x), tile)) * kRows;
+    }
     Seq it;
     if (!get_seq<kPaged>(a, kind, x, &it)) return;
-    const uint32_t row0 = (tile - min(start(x), tile)) * kRows, seq_rows = it.nq * a.group;
+    const uint32_t seq_rows = it.nq * a.group;
     if (row0 >= seq_rows) return;
     const uint32_t rows = min(kRows, seq_rows - row0);
     const uint32_t chunk = chunk_of(it.n, kind == kOwn ? a.own_chunk : a.chunk, slots), key_begin = split * chunk;
@@ -1221,8 +1283,10 @@ void launch(const Attn& a, const Shape& s, hipStream_t st)
     uint32_t fews = 0;
     for (uint32_t i = 0; i < s.wides; ++i) {
         const Wide& w = s.wide[i];
-        Part p{w.kind, (uint32_t)(rows / w.rows) + (w.kind == kGroup ? a.groups : a.batch), 0};
+        const uint32_t seqs = w.kind == kGroup ? a.groups : a.batch;
+        Part p{w.kind, (uint32_t)(rows / w.rows) + seqs, 0, 0};
         p.blocks = p.tiles * (w.kind == kOwn ? a.own_slots : a.slots) * a.heads_kv;
+        p.sorted = seqs > 1u && seqs <= kSortSeqs && p.blocks > (w.rows == 256u ? 1u : kMixedPerCu) * (uint32_t)device_cus();
         if (w.rows == 256u) hipLaunchKernelGGL((k_attn_wide<E, kDim, kPaged>), dim3(p.blocks), dim3(8 * kWave), 0, st, a, p);
         else few[fews++] = p;
     }
