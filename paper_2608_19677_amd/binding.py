@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -87,8 +88,22 @@ class CrAttnSharedArgs(ctypes.Structure):
                 ("own_len", _P)]
 
 
+# The same three laid out in one step (a ctypes structure takes ten times as long to fill); the calls take either.
+ROWS = struct.Struct("@Pqq")
+PROMPT_ARGS = struct.Struct("@8If" + "Pqq" * 4 + "PPP")
+SHARED_ARGS = struct.Struct("@7If" + "Pqq" * 2 + "PPPPPPP")
+assert [x.size for x in (ROWS, PROMPT_ARGS, SHARED_ARGS)] == [ctypes.sizeof(x) for x in (CrRows, CrAttnPromptArgs, CrAttnSharedArgs)]
+
+
 class CrError(RuntimeError):
     pass
+
+
+def packed(layout: struct.Struct, *values) -> bytes:
+    try:
+        return layout.pack(*values)
+    except (struct.error, OverflowError) as e:
+        raise CrError(f"an argument is out of range: {e}") from None
 
 
 _lib = None
@@ -147,12 +162,11 @@ def load(path: Optional[str] = None):
     L.cr_pages_free.argtypes = [cache, _P, _u32, _P, _u32, _P, _P]
     L.cr_pages_compact.argtypes = [cache, _P, _P, _u32, _u32, _P, _P, _P, size, _P, _P]
     L.cr_pages_copy.argtypes = [cache, _P, _P, _u32, _P, _P]
-    L.cr_kv_append.argtypes = [cache, _u32, ctypes.POINTER(CrRows), ctypes.POINTER(CrRows), _u32, _P, _P, _u32, _P, _u32,
-                               _P, _P]
-    L.cr_attn_prompt_workspace_bytes.argtypes = [ctypes.POINTER(CrAttnPromptArgs)]
-    L.cr_attn_prompt.argtypes = [ctypes.POINTER(CrAttnPromptArgs), _P, size, _P, _P]
-    L.cr_attn_shared_workspace_bytes.argtypes = [cache, ctypes.POINTER(CrAttnSharedArgs)]
-    L.cr_attn_shared.argtypes = [cache, ctypes.POINTER(CrAttnSharedArgs), _P, size, _P, _P]
+    L.cr_kv_append.argtypes = [cache, _u32, _P, _P, _u32, _P, _P, _u32, _P, _u32, _P, _P]
+    L.cr_attn_prompt_workspace_bytes.argtypes = [_P]
+    L.cr_attn_prompt.argtypes = [_P, _P, size, _P, _P]
+    L.cr_attn_shared_workspace_bytes.argtypes = [cache, _P]
+    L.cr_attn_shared.argtypes = [cache, _P, _P, size, _P, _P]
     for f in ("cr_pages_workspace_bytes", "cr_attn_prompt_workspace_bytes", "cr_attn_shared_workspace_bytes"):
         getattr(L, f).restype = size
     L.cr_version.restype = ctypes.c_char_p
@@ -177,13 +191,14 @@ def _ptr(t: Optional[torch.Tensor]):
 
 # The current stream's handle without a Stream object around it (4 us less per call), where torch has it.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream.cuda_stream
     if _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -378,26 +393,31 @@ def cr_pages_copy(cache: CrKvCache, src, dst, err, stream=None):
            "cr_pages_copy")
 
 
+def _ref(s):
+    """A structure, or its packed bytes."""
+    return s if type(s) is bytes else ctypes.byref(s)
+
+
 def cr_kv_append(cache: CrKvCache, layer: int, k: CrRows, v: CrRows, total: int, off, length, table, err, stream=None):
-    _check(load().cr_kv_append(ctypes.byref(cache), layer, ctypes.byref(k), ctypes.byref(v), total, _ptr(off), _ptr(length),
+    _check(load().cr_kv_append(ctypes.byref(cache), layer, _ref(k), _ref(v), total, _ptr(off), _ptr(length),
                                length.numel(), _ptr(table), _table_width(table), _ptr(err), _stream(stream)), "cr_kv_append")
 
 
 def cr_attn_prompt_workspace_bytes(args: CrAttnPromptArgs) -> int:
-    return int(load().cr_attn_prompt_workspace_bytes(ctypes.byref(args)))
+    return int(load().cr_attn_prompt_workspace_bytes(_ref(args)))
 
 
 def cr_attn_prompt(args: CrAttnPromptArgs, ws, err, stream=None):
-    _check(load().cr_attn_prompt(ctypes.byref(args), _ptr(ws), 0 if ws is None else _nbytes(ws), _ptr(err), _stream(stream)),
+    _check(load().cr_attn_prompt(_ref(args), _ptr(ws), 0 if ws is None else _nbytes(ws), _ptr(err), _stream(stream)),
            "cr_attn_prompt")
 
 
 def cr_attn_shared_workspace_bytes(cache: CrKvCache, args: CrAttnSharedArgs) -> int:
-    return int(load().cr_attn_shared_workspace_bytes(ctypes.byref(cache), ctypes.byref(args)))
+    return int(load().cr_attn_shared_workspace_bytes(ctypes.byref(cache), _ref(args)))
 
 
 def cr_attn_shared(cache: CrKvCache, args: CrAttnSharedArgs, ws, err, stream=None):
-    _check(load().cr_attn_shared(ctypes.byref(cache), ctypes.byref(args), _ptr(ws), 0 if ws is None else _nbytes(ws),
+    _check(load().cr_attn_shared(ctypes.byref(cache), _ref(args), _ptr(ws), 0 if ws is None else _nbytes(ws),
                                  _ptr(err), _stream(stream)), "cr_attn_shared")
 
 

@@ -26,6 +26,7 @@ import torch
 from . import binding as B
 
 _DTYPES = {torch.bfloat16: B.CR_BF16, torch.float16: B.CR_F16}
+_INT32, _FLOAT32 = torch.int32, torch.float32
 
 
 def _dtype(t: torch.Tensor) -> int:
@@ -34,6 +35,9 @@ def _dtype(t: torch.Tensor) -> int:
     except KeyError:
         raise B.CrError(f"bfloat16 or float16 wanted, not {t.dtype}") from None
 
+
+# The checks below are in every call of a serving loop, whose small calls are bound by the host: each attribute
+# of a tensor is looked at once, and what a check refuses is told apart afterwards.
 
 def _rows(t: torch.Tensor):
     """Fields of a cr_rows: [tokens, heads, dim] with any strides of tokens and heads."""
@@ -45,19 +49,27 @@ def _rows(t: torch.Tensor):
     return t.data_ptr(), stride[0], stride[1]
 
 
-def _int32(t: Optional[torch.Tensor], n: Optional[int] = None):
-    """An int32 array of n elements (any, if n is None), or None."""
-    if t is not None:
-        if t.dtype is not torch.int32:
-            raise B.CrError(f"offsets, lengths and tables are int32, not {t.dtype}")
-        if n is not None and t.numel() != n:
-            raise B.CrError(f"{n} entries wanted, not {t.numel()}")
-    return t
+def _refuse(t, n):
+    if t.dtype is not _INT32:
+        raise B.CrError(f"offsets, lengths and tables are int32, not {t.dtype}")
+    if n is not None and t.numel() != n:
+        raise B.CrError(f"{n} entries wanted, not {t.numel()}")
+    B._ptr(t)
 
 
 def _index(t: torch.Tensor, n: Optional[int] = None) -> int:
-    """Pointer of such an array."""
-    return B._ptr(_int32(t, n))
+    """Pointer of an int32 array of n elements (any, if n is None)."""
+    if t.dtype is not _INT32 or not t.is_cuda or not t.is_contiguous() or (n is not None and t.numel() != n):
+        _refuse(t, n)
+    return t.data_ptr()
+
+
+def _table(t: torch.Tensor, n: int):
+    """Pointer and width of a table of n rows."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != n:
+        raise B.CrError(f"a table is [{n}, width], not {list(shape)}")
+    return _index(t), shape[1]
 
 
 def _used_on(stream, *tensors):
@@ -73,6 +85,7 @@ class Workspace:
     def __init__(self, nbytes: int, device, err: Optional[torch.Tensor] = None):
         self.buf = torch.empty(max(16, nbytes), dtype=torch.uint8, device=device)
         self.err = torch.zeros(1, dtype=torch.int32, device=device) if err is None else err
+        self.args = self.buf.data_ptr(), self.buf.numel(), _index(self.err, 1)
 
 
 class PagePool:
@@ -93,6 +106,7 @@ class PagePool:
         self.err = torch.zeros(1, dtype=torch.int32, device=k.device)
         self.c = B.CrKvCache(_dtype(k), self.heads, self.dim, self.page_tokens, self.num_pages, self.layers, k.data_ptr(),
                              v.data_ptr(), k.stride(0), k.stride(1), k.stride(h), k.stride(t), _index(refs, self.num_pages))
+        self._ref, self._err = ctypes.byref(self.c), _index(self.err)
         self._ws: Optional[torch.Tensor] = None
 
     @classmethod
@@ -103,13 +117,13 @@ class PagePool:
         return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device),
                    torch.zeros(num_pages, dtype=torch.int32, device=device), order)
 
-    def _scratch(self, n: int, stream) -> torch.Tensor:
+    def _scratch(self, n: int, stream):
         """The page calls' workspace, kept with the handle: its calls are for one stream at a time."""
-        need = B.cr_pages_workspace_bytes(self.num_pages, n)
+        need = B.load().cr_pages_workspace_bytes(self.num_pages, n)
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.k.device)
         _used_on(stream, self._ws)
-        return self._ws
+        return self._ws.data_ptr(), self._ws.numel(), self._err, B._stream(stream)
 
     def pages_of(self, tokens: int) -> int:
         return -(-tokens // self.page_tokens)
@@ -117,69 +131,65 @@ class PagePool:
     def extend(self, table, len_old, len_new, stream=None):
         """Free pages for sequences that grow from len_old (None: 0) to len_new tokens."""
         n = len_new.numel()
-        _int32(len_new), _int32(table), _int32(len_old, n)
-        _same_rows(table, n)
-        B.cr_pages_extend(self.c, len_old, len_new, table, self._scratch(n, stream), self.err, stream)
+        new, old = _index(len_new), None if len_old is None else _index(len_old, n)
+        p, width = _table(table, n)
+        B._check(B.load().cr_pages_extend(self._ref, old, new, n, p, width, *self._scratch(n, stream)), "cr_pages_extend")
 
     def fork(self, table, parent, length, child, stream=None):
         """child[i]: the first length[i] tokens of table[parent[i]], the partial tail copied."""
-        n = parent.numel()
-        _int32(table), _int32(parent), _int32(length, n), _int32(child)
-        _same_rows(table, table.shape[0])
-        _same_rows(child, n)
-        B.cr_pages_fork(self.c, table, parent, length, child, self._scratch(n, stream), self.err, stream)
+        n, rows = parent.numel(), table.shape[0]
+        (p, width), (c, child_width) = _table(table, rows), _table(child, n)
+        B._check(B.load().cr_pages_fork(self._ref, p, rows, width, _index(parent), _index(length, n), n, c, child_width,
+                                        *self._scratch(n, stream)), "cr_pages_fork")
 
     def free(self, table, length, stream=None):
         """Gives the pages of every row's first length tokens back."""
-        _int32(table), _int32(length)
-        _same_rows(table, length.numel())
-        B.cr_pages_free(self.c, table, length, self.err, stream)
+        n = length.numel()
+        p, width = _table(table, n)
+        B._check(B.load().cr_pages_free(self._ref, p, width, _index(length), n, self._err, B._stream(stream)), "cr_pages_free")
 
     def compact(self, table, length, table_out=None, refs_out=None, stream=None):
         """Moves the live pages to the front and renames the table's entries (in place, if no
         other place is given)."""
-        table_out, refs_out = (table if table_out is None else table_out), (self.refs if refs_out is None else refs_out)
-        _int32(table), _int32(length), _int32(refs_out, self.num_pages)
+        refs = _index(self.refs if refs_out is None else refs_out, self.num_pages)
+        p = lengths = out = None
+        rows = width = 0
         if table is not None:
-            _int32(table_out, table.numel())
-            _same_rows(table, length.numel())
-        B.cr_pages_compact(self.c, table, length, table_out, refs_out, self._scratch(0, stream), self.err, stream)
+            rows = length.numel()
+            p, width = _table(table, rows)
+            lengths, out = _index(length), p if table_out is None else _index(table_out, rows * width)
+        B._check(B.load().cr_pages_compact(self._ref, p, lengths, rows, width, out, refs, *self._scratch(0, stream)), "cr_pages_compact")
 
     def copy(self, src, dst, stream=None):
         """Contents of page src[i] to page dst[i], all layers."""
-        _int32(src), _int32(dst, src.numel())
-        B.cr_pages_copy(self.c, src, dst, self.err, stream)
+        n = src.numel()
+        B._check(B.load().cr_pages_copy(self._ref, _index(src), _index(dst, n), n, self._err, B._stream(stream)), "cr_pages_copy")
 
     def append(self, layer: int, k, v, off, length, table, stream=None):
         """Rows off[i]..off[i+1] of k and v ([total, heads, dim]) become the last tokens of the
         length[i] of sequence i."""
-        if k.shape != v.shape or k.shape[1:] != (self.heads, self.dim) or k.dtype != self.k.dtype or v.dtype != self.k.dtype:
+        shape, n, dtype = k.shape, length.numel(), self.k.dtype
+        if shape != v.shape or shape[1:] != (self.heads, self.dim) or k.dtype is not dtype or v.dtype is not dtype:
             raise B.CrError("new keys and values have the cache's heads, dim and type")
-        _int32(length), _int32(off, length.numel() + 1), _int32(table)
-        _same_rows(table, length.numel())
-        B.cr_kv_append(self.c, layer, B.CrRows(*_rows(k)), B.CrRows(*_rows(v)), k.shape[0], off, length, table, self.err, stream)
+        p, width = _table(table, n)
+        B._check(B.load().cr_kv_append(self._ref, layer, B.packed(B.ROWS, *_rows(k)), B.packed(B.ROWS, *_rows(v)), shape[0],
+                                       _index(off, n + 1), _index(length), n, p, width, self._err, B._stream(stream)), "cr_kv_append")
 
 
-def _same_rows(table, n: int):
-    if table.dim() != 2 or table.shape[0] != n:
-        raise B.CrError(f"a table is [{n}, width], not {list(table.shape)}")
-
-
-def _check_out(q, out, lse):
-    if out.shape != q.shape or out.dtype != q.dtype:
+def _check_out(q, shape, out, lse):
+    if out.shape != shape or out.dtype is not q.dtype:
         raise B.CrError("out has q's shape and type")
-    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != q.shape[:2]):
+    if lse is not None and (lse.dtype is not _FLOAT32 or lse.shape != shape[:2]):
         raise B.CrError("lse is float32 [tokens, heads]")
 
 
-def _prompt_args(dtype, q, k, batch, scale, causal, *rest) -> B.CrAttnPromptArgs:
-    nq, hq, d = q.shape
-    return B.CrAttnPromptArgs(dtype, hq, k.shape[1], d, batch, causal, nq, k.shape[0], scale, *rest)
+def _prompt_args(dtype, q, k, batch, scale, causal, *rest) -> bytes:
+    return B.packed(B.PROMPT_ARGS, dtype, q[1], k[1], q[2], batch, causal, q[0], k[0], scale, *(rest or (0,) * 15))
 
 
 def prompt_workspace(q, k, q_off, err: Optional[torch.Tensor] = None) -> Workspace:
     """Scratch for ``attend_prompt`` of tensors of these shapes."""
-    return Workspace(B.cr_attn_prompt_workspace_bytes(_prompt_args(_dtype(q), q, k, q_off.numel() - 1, 1.0, True)), q.device, err)
+    return Workspace(B.cr_attn_prompt_workspace_bytes(_prompt_args(_dtype(q), q.shape, k.shape, q_off.numel() - 1, 1.0, True)), q.device, err)
 
 
 def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, causal: bool = True,
@@ -187,31 +197,32 @@ def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, ca
     """Attention of packed sequences: q [total_q, heads_q, dim], k, v [total_k, heads_kv, dim],
     sequence b at q_off[b]..q_off[b+1] and k_off[b]..k_off[b+1]. Returns out (and fills lse,
     float32 [total_q, heads_q], if given)."""
-    if k.shape != v.shape or k.shape[2] != q.shape[2] or k.dtype != q.dtype or v.dtype != q.dtype:
+    shape, keys, dtype = q.shape, k.shape, q.dtype
+    if keys != v.shape or len(keys) != 3 or len(shape) != 3 or keys[2] != shape[2] or k.dtype is not dtype or v.dtype is not dtype:
         raise B.CrError("q, k and v have one type and dim, k and v one shape")
-    dtype = _dtype(q)
+    code = _dtype(q)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         _used_on(stream, out)
-    _check_out(q, out, lse)
+    _check_out(q, shape, out, lse)
     n = q_off.numel()
-    a = _prompt_args(dtype, q, k, n - 1, scale, causal, _rows(q), _rows(k), _rows(v), _rows(out), B._ptr(lse), _index(q_off),
-                     _index(k_off, n))
+    a = _prompt_args(code, shape, keys, n - 1, scale, causal, *_rows(q), *_rows(k), *_rows(v), *_rows(out),
+                     B._ptr(lse) or 0, _index(q_off), _index(k_off, n))
     if ws is None:
         ws = prompt_workspace(q, k, q_off)
         _used_on(stream, ws.buf, ws.err)
-    B.cr_attn_prompt(a, ws.buf, ws.err, stream)
+    B._check(B.load().cr_attn_prompt(a, *ws.args, B._stream(stream)), "cr_attn_prompt")
     return out
 
 
-def _shared_args(q, pool: PagePool, layer, groups, prefix_table, own_table, scale, *rest) -> B.CrAttnSharedArgs:
-    batch, own_width = own_table.shape
-    return B.CrAttnSharedArgs(q.shape[1], layer, batch, groups, q.shape[0], prefix_table.shape[1], own_width, scale, *rest)
+def _shared_args(q, layer, batch, groups, prefix_width, own_width, scale, *rest) -> bytes:
+    return B.packed(B.SHARED_ARGS, q[1], layer, batch, groups, q[0], prefix_width, own_width, scale, *(rest or (0,) * 13))
 
 
 def shared_workspace(q, pool: PagePool, group_off, prefix_table, own_table, err: Optional[torch.Tensor] = None) -> Workspace:
     """Scratch for ``attend_shared`` of tensors of these shapes."""
-    a = _shared_args(q, pool, 0, group_off.numel() - 1, prefix_table, own_table, 1.0)
+    batch, own_width = own_table.shape
+    a = _shared_args(q.shape, 0, batch, group_off.numel() - 1, prefix_table.shape[1], own_width, 1.0)
     return Workspace(B.cr_attn_shared_workspace_bytes(pool.c, a), q.device, pool.err if err is None else err)
 
 
@@ -221,20 +232,20 @@ def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table,
     group_off[g+1] see the prefix_len[g] tokens of prefix_table[g] and, causally, their own
     own_len[r] tokens of own_table[r], the last of which are the queries' (append them first).
     q [total_q, heads_q, dim], request r's at q_off[r]..q_off[r+1]. Returns out."""
-    if q.dtype != pool.k.dtype or q.dim() != 3 or q.shape[2] != pool.dim:
+    shape = q.shape
+    if q.dtype is not pool.k.dtype or len(shape) != 3 or shape[2] != pool.dim:
         raise B.CrError("q has the cache's type and dim")
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         _used_on(stream, out)
-    _check_out(q, out, lse)
-    batch, groups = own_table.shape[0], group_off.numel() - 1
-    _same_rows(own_table, batch)
-    _same_rows(prefix_table, groups)
-    a = _shared_args(q, pool, layer, groups, prefix_table, own_table, scale, _rows(q), _rows(out), B._ptr(lse),
-                     _index(q_off, batch + 1), _index(group_off), _index(prefix_table), _index(prefix_len, groups),
-                     _index(own_table), _index(own_len, batch))
+    _check_out(q, shape, out, lse)
+    batch, groups = own_len.numel(), group_off.numel() - 1
+    own, own_width = _table(own_table, batch)
+    prefix, prefix_width = _table(prefix_table, groups)
+    a = _shared_args(shape, layer, batch, groups, prefix_width, own_width, scale, *_rows(q), *_rows(out),
+                     B._ptr(lse) or 0, _index(q_off, batch + 1), _index(group_off), prefix, _index(prefix_len, groups), own, _index(own_len))
     if ws is None:
         ws = shared_workspace(q, pool, group_off, prefix_table, own_table)
         _used_on(stream, ws.buf)
-    B.cr_attn_shared(pool.c, a, ws.buf, ws.err, stream)
+    B._check(B.load().cr_attn_shared(pool._ref, a, *ws.args, B._stream(stream)), "cr_attn_shared")
     return out
