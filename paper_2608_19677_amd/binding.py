@@ -99,13 +99,6 @@ class CrError(RuntimeError):
     pass
 
 
-def packed(layout: struct.Struct, *values) -> bytes:
-    try:
-        return layout.pack(*values)
-    except (struct.error, OverflowError) as e:
-        raise CrError(f"an argument is out of range: {e}") from None
-
-
 _lib = None
 
 

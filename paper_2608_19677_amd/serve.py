@@ -19,6 +19,7 @@ skipped as the library documents.
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional
 
 import torch
@@ -27,6 +28,7 @@ from . import binding as B
 
 _DTYPES = {torch.bfloat16: B.CR_BF16, torch.float16: B.CR_F16}
 _INT32, _FLOAT32 = torch.int32, torch.float32
+_pack_rows, _pack_prompt, _pack_shared, _RANGE = B.ROWS.pack, B.PROMPT_ARGS.pack, B.SHARED_ARGS.pack, (struct.error, OverflowError)
 
 
 def _dtype(t: torch.Tensor) -> int:
@@ -169,27 +171,27 @@ class PagePool:
         """Rows off[i]..off[i+1] of k and v ([total, heads, dim]) become the last tokens of the
         length[i] of sequence i."""
         shape, n, dtype = k.shape, length.numel(), self.k.dtype
-        if shape != v.shape or shape[1:] != (self.heads, self.dim) or k.dtype is not dtype or v.dtype is not dtype:
+        if len(shape) != 3 or shape[1] != self.heads or shape[2] != self.dim or shape != v.shape or k.dtype is not dtype or v.dtype is not dtype:
             raise B.CrError("new keys and values have the cache's heads, dim and type")
         p, width = _table(table, n)
-        B._check(B.load().cr_kv_append(self._ref, layer, B.packed(B.ROWS, *_rows(k)), B.packed(B.ROWS, *_rows(v)), shape[0],
+        B._check(B.load().cr_kv_append(self._ref, layer, _pack_rows(*_rows(k)), _pack_rows(*_rows(v)), shape[0],
                                        _index(off, n + 1), _index(length), n, p, width, self._err, B._stream(stream)), "cr_kv_append")
 
 
 def _check_out(q, shape, out, lse):
     if out.shape != shape or out.dtype is not q.dtype:
         raise B.CrError("out has q's shape and type")
-    if lse is not None and (lse.dtype is not _FLOAT32 or lse.shape != shape[:2]):
-        raise B.CrError("lse is float32 [tokens, heads]")
-
-
-def _prompt_args(dtype, q, k, batch, scale, causal, *rest) -> bytes:
-    return B.packed(B.PROMPT_ARGS, dtype, q[1], k[1], q[2], batch, causal, q[0], k[0], scale, *(rest or (0,) * 15))
+    if lse is not None:
+        rows = lse.shape
+        if lse.dtype is not _FLOAT32 or len(rows) != 2 or rows[0] != shape[0] or rows[1] != shape[1]:
+            raise B.CrError("lse is float32 [tokens, heads]")
 
 
 def prompt_workspace(q, k, q_off, err: Optional[torch.Tensor] = None) -> Workspace:
     """Scratch for ``attend_prompt`` of tensors of these shapes."""
-    return Workspace(B.cr_attn_prompt_workspace_bytes(_prompt_args(_dtype(q), q.shape, k.shape, q_off.numel() - 1, 1.0, True)), q.device, err)
+    (nq, hq, d), (nk, hkv, _) = q.shape, k.shape
+    a = B.CrAttnPromptArgs(_dtype(q), hq, hkv, d, q_off.numel() - 1, 1, nq, nk, 1.0)
+    return Workspace(B.cr_attn_prompt_workspace_bytes(a), q.device, err)
 
 
 def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, causal: bool = True,
@@ -206,8 +208,11 @@ def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, ca
         _used_on(stream, out)
     _check_out(q, shape, out, lse)
     n = q_off.numel()
-    a = _prompt_args(code, shape, keys, n - 1, scale, causal, *_rows(q), *_rows(k), *_rows(v), *_rows(out),
-                     B._ptr(lse) or 0, _index(q_off), _index(k_off, n))
+    try:
+        a = _pack_prompt(code, shape[1], keys[1], shape[2], n - 1, causal, shape[0], keys[0], scale, *_rows(q), *_rows(k), *_rows(v),
+                         *_rows(out), B._ptr(lse) or 0, _index(q_off), _index(k_off, n))
+    except _RANGE as e:
+        raise B.CrError(f"an argument is out of range: {e}") from None
     if ws is None:
         ws = prompt_workspace(q, k, q_off)
         _used_on(stream, ws.buf, ws.err)
@@ -215,14 +220,10 @@ def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, ca
     return out
 
 
-def _shared_args(q, layer, batch, groups, prefix_width, own_width, scale, *rest) -> bytes:
-    return B.packed(B.SHARED_ARGS, q[1], layer, batch, groups, q[0], prefix_width, own_width, scale, *(rest or (0,) * 13))
-
-
 def shared_workspace(q, pool: PagePool, group_off, prefix_table, own_table, err: Optional[torch.Tensor] = None) -> Workspace:
     """Scratch for ``attend_shared`` of tensors of these shapes."""
     batch, own_width = own_table.shape
-    a = _shared_args(q.shape, 0, batch, group_off.numel() - 1, prefix_table.shape[1], own_width, 1.0)
+    a = B.CrAttnSharedArgs(q.shape[1], 0, batch, group_off.numel() - 1, q.shape[0], prefix_table.shape[1], own_width, 1.0)
     return Workspace(B.cr_attn_shared_workspace_bytes(pool.c, a), q.device, pool.err if err is None else err)
 
 
@@ -242,8 +243,11 @@ def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table,
     batch, groups = own_len.numel(), group_off.numel() - 1
     own, own_width = _table(own_table, batch)
     prefix, prefix_width = _table(prefix_table, groups)
-    a = _shared_args(shape, layer, batch, groups, prefix_width, own_width, scale, *_rows(q), *_rows(out),
-                     B._ptr(lse) or 0, _index(q_off, batch + 1), _index(group_off), prefix, _index(prefix_len, groups), own, _index(own_len))
+    try:
+        a = _pack_shared(shape[1], layer, batch, groups, shape[0], prefix_width, own_width, scale, *_rows(q), *_rows(out),
+                         B._ptr(lse) or 0, _index(q_off, batch + 1), _index(group_off), prefix, _index(prefix_len, groups), own, _index(own_len))
+    except _RANGE as e:
+        raise B.CrError(f"an argument is out of range: {e}") from None
     if ws is None:
         ws = shared_workspace(q, pool, group_off, prefix_table, own_table)
         _used_on(stream, ws.buf)

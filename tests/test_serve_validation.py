@@ -181,3 +181,13 @@ def test_counts_that_pass_32_bits_are_refused(L):
     assert L.cr_attn_shared(c, ctypes.byref(wide), FAKE, 1 << 50, FAKE, None) == B.CR_EINVAL
     many = _prompt(heads_q=1024, heads_kv=1024, batch=1 << 15, total_q=1 << 20, total_k=1 << 30)  # 2^25 workgroups
     assert L.cr_attn_prompt(ctypes.byref(many), FAKE, 1 << 50, FAKE, None) == B.CR_EINVAL
+
+
+def test_packed_arguments_are_the_structures():
+    v = [(1, 8, 2, 128, 5, 1, 70, 90, 0.25), [(11 * i, 8 * i, 16 * i) for i in range(1, 5)], (3, 4, 5)]
+    a = B.CrAttnPromptArgs(*v[0], *v[1], *v[2])
+    assert B.PROMPT_ARGS.pack(*v[0], *(x for r in v[1] for x in r), *v[2]) == bytes(a)
+    s = (8, 1, 5, 2, 70, 9, 4, 0.5)
+    b = B.CrAttnSharedArgs(*s, *v[1][:2], *range(3, 10))
+    assert B.SHARED_ARGS.pack(*s, *(x for r in v[1][:2] for x in r), *range(3, 10)) == bytes(b)
+    assert B.ROWS.pack(*v[1][0]) == bytes(B.CrRows(*v[1][0]))
