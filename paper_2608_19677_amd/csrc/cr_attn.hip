@@ -1029,7 +1029,7 @@ __global__ __launch_bounds__(kThreads, kMixedPerCu) void k_attn_mixed(const Attn
 
 // Joins the partial results of a token's rows: 4 elements of a row per thread, kPar threads share the
 // slots of a row's elements (eight where there are more than eight slots). Bound by memory and the launch: two
-// slots of 3 tokens 4 us, 22 slots of 128 tokens' 64 heads (46 MB) 16.
+// slots of 3 tokens 4 us, 11 slots of 128 tokens' 64 heads (46 MB) 16.
 template <typename E, int kDim, uint32_t kPar>
 __global__ __launch_bounds__(kThreads) void k_attn_join(const Attn a)
 {

@@ -135,12 +135,12 @@ __global__ __launch_bounds__(256) void k_pages_count(const uint32_t* __restrict_
 }
 
 // The sequence that takes the page of rank r: first[i] <= r < first[i + 1].
-__device__ __forceinline__ uint32_t pg_taker(const PgWs& w, const PgTake& t, uint32_t r)
+__device__ __forceinline__ uint32_t pg_taker(const uint32_t* first, uint32_t n, uint32_t r)
 {
-    uint32_t lo = 0, hi = t.n;
+    uint32_t lo = 0, hi = n;
     while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) >> 1;
-        if (w.first[mid] <= r) lo = mid;
+        if (first[mid] <= r) lo = mid;
         else hi = mid;
     }
     return lo;
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(256) void k_pages_take(uint32_t* __restrict__ refs,
     uint32_t m = pg_free_mask(refs, t.num_pages, p0), tot;
     uint32_t r = before + block_exscan_u32((uint32_t)__popc(m), sh, &tot);
     for (; m && r < want; ++r, m &= m - 1u) {
-        const uint32_t p = p0 + (uint32_t)__builtin_ctz(m), i = pg_taker(w, t, r);
+        const uint32_t p = p0 + (uint32_t)__builtin_ctz(m), i = pg_taker(w.first, t.n, r);
         t.out[(uint64_t)i * t.out_width + pg_had(t, i) + (r - w.first[i])] = p;
         refs[p] = 1u;
     }
@@ -217,8 +217,8 @@ __device__ __forceinline__ int64_t pg_piece(const PgGeom& g, uint32_t x)
     return (int64_t)head * g.head_stride + (int64_t)tok * g.token_stride + (int64_t)(x % g.row16) * 8;
 }
 
-// A fork's tail: the tokens behind child i's full pages in one plane (keys or values of a layer), copied by
-// `movers` threads. Bound by memory: 192 children's tails of 32 layers (336 MB read, from cache where children
+// A fork's tail: the tokens behind a child's full pages in one plane (keys or values of a layer), copied from page
+// src to page dst by `movers` threads. Bound by memory: 192 children's tails of 32 layers (336 MB read, from cache where children
 // share a parent, and 336 MB written) take 110 us.
 struct PgPlanes {
     uint16_t* k;
@@ -228,15 +228,10 @@ struct PgPlanes {
     uint32_t planes;
 };
 
-__device__ __forceinline__ void pg_copy_tail(const PgPlanes& c, const PgTake& t, uint32_t i, uint32_t plane, uint32_t mover, uint32_t movers)
+__device__ __forceinline__ void pg_copy_tail(const PgPlanes& c, uint32_t src, uint32_t dst, uint32_t tail, uint32_t plane, uint32_t mover,
+                                             uint32_t movers)
 {
     const PgGeom& g = c.g;
-    const uint32_t len = t.length[i], full = len >> t.log_tokens, tail = len & ((1u << t.log_tokens) - 1u);
-    if (tail == 0u || full >= t.out_width) return;
-    const uint32_t dst = t.out[(uint64_t)i * t.out_width + full];
-    if (dst >= t.num_pages) return;  // not served
-    const uint32_t src = t.table[(uint64_t)t.parent[i] * t.width + full];
-    if (src >= t.num_pages) return;  // reported with the rows
     uint16_t* base = ((plane & 1u) ? c.v : c.k) + (int64_t)(plane >> 1) * c.layer_stride;
     const uint16_t* s = base + (int64_t)src * c.page_stride;
     uint16_t* d = base + (int64_t)dst * c.page_stride;
@@ -251,64 +246,86 @@ __device__ __forceinline__ void pg_copy_tail(const PgPlanes& c, const PgTake& t,
 
 __global__ __launch_bounds__(256) void k_pages_tail(PgPlanes c, PgTake t)
 {
-    for (uint64_t u = blockIdx.x; u < (uint64_t)t.n * c.planes; u += gridDim.x)
-        pg_copy_tail(c, t, (uint32_t)(u / c.planes), (uint32_t)(u % c.planes), threadIdx.x, kCopyThreads);
+    for (uint64_t u = blockIdx.x; u < (uint64_t)t.n * c.planes; u += gridDim.x) {
+        const uint32_t i = (uint32_t)(u / c.planes);
+        const uint32_t len = t.length[i], full = len >> t.log_tokens, tail = len & ((1u << t.log_tokens) - 1u);
+        if (tail == 0u || full >= t.out_width) continue;
+        const uint32_t dst = t.out[(uint64_t)i * t.out_width + full];
+        if (dst >= t.num_pages) continue;  // not served
+        const uint32_t src = t.table[(uint64_t)t.parent[i] * t.width + full];
+        if (src >= t.num_pages) continue;  // reported with the rows
+        pg_copy_tail(c, src, dst, tail, (uint32_t)(u % c.planes), threadIdx.x, kCopyThreads);
+    }
 }
 
 // cr_pages_extend and cr_pages_fork of few sequences in one block, which holds the free pages among up to
-// kOnePages in registers: three launches' work in one. Four children of a 512-page cache forked and freed
-// take 15 us a pass, 20 with the launches. Every read of refs comes before the first write.
+// kOnePages in registers: three launches' work in one. Bound by its chain of dependent loads, so what the steps
+// hand on stays in registers and LDS: four children of a 512-page cache forked and freed take 12.5 us a pass (13.0
+// through global memory, 20 with the three launches). Every read of refs comes before the first write; pages that are shared and
+// pages that are taken are different ones, as are the entries that name them.
 constexpr uint32_t kOneThreads = 1024, kOnePages = kOneThreads * kPgPer;
+// Sequences, a thread each; table entries of a fork; 16-byte pieces of the pages it may copy.
+constexpr uint32_t kOneSeqs = kOneThreads, kOneEntries = 8 * kOneThreads, kOnePieces = 16384;
 
-__global__ __launch_bounds__(1024) void k_pages_one(uint32_t* __restrict__ refs, PgWs w, PgTake t, PgPlanes c, uint32_t* __restrict__ err)
+__global__ __launch_bounds__(1024) void k_pages_one(uint32_t* __restrict__ refs, PgTake t, PgPlanes c, uint32_t* __restrict__ err)
 {
-    __shared__ uint32_t sh[16];
-    uint32_t tot, bad = 0, want = 0;
-    for (uint32_t i0 = 0; i0 < t.n; i0 += kOneThreads) {
-        const uint32_t i = i0 + threadIdx.x;
-        const uint32_t need = i < t.n ? pg_need(t, i, &bad) : 0u;
-        const uint32_t pre = block_exscan_u32(need, sh, &tot);
-        if (i < t.n) w.first[i] = want + pre;
-        want += tot;
-    }
-    if (threadIdx.x == 0) w.first[t.n] = want;
-    const uint32_t p0 = threadIdx.x * kPgPer;
+    __shared__ uint32_t sh[16], first[kOneSeqs + 1], had[kOneSeqs], from[kOneSeqs], to[kOneSeqs];
+    uint32_t tot, want, bad = 0;
+    const uint32_t p0 = threadIdx.x * kPgPer, me = threadIdx.x, mask = (1u << t.log_tokens) - 1u;
     uint32_t m = pg_free_mask(refs, t.num_pages, p0);
+    const uint32_t need = me < t.n ? pg_need(t, me, &bad) : 0u;
+    if (me < t.n) {
+        had[me] = pg_had(t, me);
+        from[me] = to[me] = CR_NO_PAGE;
+    }
+    const uint32_t pre = block_exscan_u32(need, sh, &want);
+    if (me < t.n) first[me] = pre;
+    if (me == 0) first[t.n] = want;
     uint32_t r = block_exscan_u32((uint32_t)__popc(m), sh, &tot);
     const bool short_of = want > tot;
     if (short_of) bad |= CR_ERR_PAGES_OUT;
-    if (t.parent) {
-        for (uint32_t x = threadIdx.x; x < t.n * t.out_width; x += kOneThreads) {
-            const uint32_t i = x / t.out_width, j = x % t.out_width;
-            const uint32_t p = t.parent[i], len = t.length[i], pages = pages_of(len, t.log_tokens), full = len >> t.log_tokens;
-            uint32_t g = CR_NO_PAGE;
-            if (p < t.rows && pages <= t.width && pages <= t.out_width && j < pages) {
-                g = t.table[(uint64_t)p * t.width + j];
-                if (g >= t.num_pages || refs[g] == 0u) {
-                    bad |= CR_ERR_PAGE;
-                    g = CR_NO_PAGE;
-                }
+    uint32_t shared[kOneEntries / kOneThreads];
+#pragma unroll
+    for (uint32_t y = 0; y < kOneEntries / kOneThreads; ++y) {
+        shared[y] = CR_NO_PAGE;
+        const uint32_t x = y * kOneThreads + me;
+        if (!t.parent || x >= t.n * t.out_width) continue;
+        const uint32_t i = x / t.out_width, j = x % t.out_width;
+        const uint32_t p = t.parent[i], len = t.length[i], pages = pages_of(len, t.log_tokens), full = len >> t.log_tokens;
+        uint32_t g = CR_NO_PAGE;
+        if (p < t.rows && pages <= t.width && pages <= t.out_width && j < pages) {
+            g = t.table[(uint64_t)p * t.width + j];
+            if (g >= t.num_pages || refs[g] == 0u) {
+                bad |= CR_ERR_PAGE;
+                g = CR_NO_PAGE;
             }
-            t.out[x] = j < full && !short_of ? g : CR_NO_PAGE;
+            if (j == full) {  // the page of the tail: copied, and its entry the taken page's
+                from[i] = g;
+                if (!short_of) continue;
+            }
         }
+        if (j < full && !short_of) shared[y] = g;
+        t.out[x] = shared[y];
     }
     if (bad) atomicOr(err, bad);
     if (short_of) return;
     __syncthreads();
-    if (t.parent)
-        for (uint32_t x = threadIdx.x; x < t.n * t.out_width; x += kOneThreads)
-            if (t.out[x] != CR_NO_PAGE) atomicAdd(&refs[t.out[x]], 1u);
-    __syncthreads();
+#pragma unroll
+    for (uint32_t y = 0; y < kOneEntries / kOneThreads; ++y)
+        if (shared[y] != CR_NO_PAGE) atomicAdd(&refs[shared[y]], 1u);
     for (; m && r < want; ++r, m &= m - 1u) {
-        const uint32_t p = p0 + (uint32_t)__builtin_ctz(m), i = pg_taker(w, t, r);
-        t.out[(uint64_t)i * t.out_width + pg_had(t, i) + (r - w.first[i])] = p;
+        const uint32_t p = p0 + (uint32_t)__builtin_ctz(m), i = pg_taker(first, t.n, r);
+        t.out[(uint64_t)i * t.out_width + had[i] + (r - first[i])] = p;
+        to[i] = p;  // a fork's child takes one
         refs[p] = 1u;
     }
     if (!t.parent) return;
     __syncthreads();
     // sixteen waves, a child's plane each
-    for (uint32_t u = threadIdx.x >> 6; u < t.n * c.planes; u += kOneThreads / 64u)
-        pg_copy_tail(c, t, u / c.planes, u % c.planes, lane_id(), 64u);
+    for (uint32_t u = threadIdx.x >> 6; u < t.n * c.planes; u += kOneThreads / 64u) {
+        const uint32_t i = u / c.planes, src = from[i], dst = to[i];
+        if (src != CR_NO_PAGE && dst != CR_NO_PAGE) pg_copy_tail(c, src, dst, t.length[i] & mask, u % c.planes, lane_id(), 64u);
+    }
 }
 
 __global__ __launch_bounds__(256) void k_pages_free(uint32_t* __restrict__ refs, uint32_t num_pages, uint32_t log_tokens,
@@ -494,10 +511,6 @@ __global__ __launch_bounds__(256) void k_kv_append(KvPages c, uint16_t* __restri
     }
 }
 
-// Up to these sizes one block does the work of a call faster than three launches: sequences of an
-// extension, table entries of a fork, 16-byte pieces of the pages it may copy.
-constexpr uint32_t kOneSeqs = 1024, kOneEntries = 8192, kOnePieces = 16384;
-
 inline PgCopy pg_copy(const cr_kv_cache* c)
 {
     PgCopy m{};
@@ -545,7 +558,7 @@ extern "C" cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_o
     const hipStream_t st = as_stream(stream);
     (void)hipGetLastError();
     if (c->num_pages <= kOnePages && n <= kOneSeqs) {
-        hipLaunchKernelGGL(k_pages_one, dim3(1), dim3(kOneThreads), 0, st, c->refs, w, t, PgPlanes{}, err);
+        hipLaunchKernelGGL(k_pages_one, dim3(1), dim3(kOneThreads), 0, st, c->refs, t, PgPlanes{}, err);
     } else {
         hipLaunchKernelGGL(k_pages_count, dim3(chunks + 1), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
         hipLaunchKernelGGL(k_pages_take, dim3(chunks), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
@@ -582,7 +595,7 @@ extern "C" cr_status cr_pages_fork(const cr_kv_cache* c, const uint32_t* table, 
     const PgPlanes planes{(uint16_t*)c->k, (uint16_t*)c->v, c->layer_stride, c->page_stride, pg_geom(c), 2u * c->layers};
     const uint64_t units = (uint64_t)n * planes.planes;
     if (c->num_pages <= kOnePages && n <= kOneSeqs && (uint64_t)n * child_width <= kOneEntries && units * planes.g.page16 <= kOnePieces) {
-        hipLaunchKernelGGL(k_pages_one, dim3(1), dim3(kOneThreads), 0, st, c->refs, w, t, planes, err);
+        hipLaunchKernelGGL(k_pages_one, dim3(1), dim3(kOneThreads), 0, st, c->refs, t, planes, err);
     } else {
         hipLaunchKernelGGL(k_pages_count, dim3(chunks + 1 + n), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
         hipLaunchKernelGGL(k_pages_take, dim3(chunks + n), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);

@@ -110,6 +110,7 @@ class PagePool:
                              v.data_ptr(), k.stride(0), k.stride(1), k.stride(h), k.stride(t), _index(refs, self.num_pages))
         self._ref, self._err = ctypes.byref(self.c), _index(self.err)
         self._ws: Optional[torch.Tensor] = None
+        self._ws_for = -1  # sequences that it is large enough for
 
     @classmethod
     def empty(cls, layers: int, num_pages: int, heads: int, page_tokens: int, dim: int, dtype=torch.bfloat16, device="cuda",
@@ -121,9 +122,9 @@ class PagePool:
 
     def _scratch(self, n: int, stream):
         """The page calls' workspace, kept with the handle: its calls are for one stream at a time."""
-        need = B.load().cr_pages_workspace_bytes(self.num_pages, n)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.k.device)
+        if n > self._ws_for:
+            self._ws = torch.empty(B.cr_pages_workspace_bytes(self.num_pages, n), dtype=torch.uint8, device=self.k.device)
+            self._ws_for = n
         _used_on(stream, self._ws)
         return self._ws.data_ptr(), self._ws.numel(), self._err, B._stream(stream)
 
