@@ -47,6 +47,7 @@ SHARED = [
     ("bf16", 32, 8, 128, 16, "head", [1500, 0, 700, 1500], [3, 2, 0, 9], [100 + 20 * i for i in range(14)], [100 + 20 * i for i in range(14)]),
     ("f16", 32, 16, 64, 32, "token", [130, 700, 65], [8, 40, 16], [40 + i for i in range(64)], [40 + i % 9 for i in range(64)]),
     ("bf16", 16, 16, 64, 16, "head", [600, 200, 0, 900], [90, 110, 130, 90], [3] * 420, [1] * 420),  # prefixes of many rows
+    ("bf16", 128, 128, 64, 16, "head", [600, 200, 0, 900], [7, 9, 5, 7], [30] * 28, [10] * 28),      # the same, more blocks than a round
 ]
 
 
