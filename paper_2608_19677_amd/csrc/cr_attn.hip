@@ -744,8 +744,8 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             r0 = a.group_off[y];
             r1 = a.group_off[y + 1u];
         }
-        bool ok = r0 <= r1 && r1 <= a.batch;
-        disorder |= !ok;
+        const bool in_order = r0 <= r1 && r1 <= a.batch;
+        bool ok = in_order;
         if (kPaged && !own && ((y == 0u && r0 != 0u) || (y + 1u == a.groups && r1 != a.batch))) atomicOr(a.err, CR_ERR_SEQ);
         if (kPaged) {
             *n = own ? a.own_len[y] : a.prefix_len[y];
@@ -756,12 +756,15 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             *n = k1 - k0;
             ok = ok && k0 <= k1 && k1 <= a.total_k;
         }
-        if (ok) {
-            *tok0 = a.q_off[r0];
-            *nq = a.q_off[r1] - *tok0;
-            ok = *tok0 + *nq >= *tok0 && *tok0 + *nq <= a.total_q;
-            disorder |= !ok;
-            if ((r0 == 0u && *tok0 != 0u) || (r1 == a.batch && *tok0 + *nq != a.total_q)) atomicOr(a.err, CR_ERR_SEQ);
+        disorder |= !in_order;
+        if (in_order) {  // looked at whatever the keys are: the other sequences' sum depends on it
+            const uint32_t t0 = a.q_off[r0], t1 = a.q_off[r1];
+            const bool fits = t0 <= t1 && t1 <= a.total_q;
+            disorder |= !fits;
+            ok = ok && fits;
+            *tok0 = t0;
+            *nq = t1 - t0;
+            if ((r0 == 0u && t0 != 0u) || (r1 == a.batch && t1 != a.total_q)) atomicOr(a.err, CR_ERR_SEQ);
         }
         if (!ok) {
             atomicOr(a.err, CR_ERR_SEQ);

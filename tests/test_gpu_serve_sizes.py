@@ -209,3 +209,16 @@ def test_many_small_weights_in_sixteen_bit_floats():
         say(f"[case] small weights, {rows} rows")
         out = serve.attend_prompt(q.expand(rows, 1, d).contiguous(), k, v, _i32([0, rows]), _i32([0, n]), math.log(2.0), causal=False)
         assert (out.double() / (rest / (1 + rest)) - 1).abs().max() <= 2.0 ** -10
+
+
+def test_offsets_out_of_order_write_nothing():
+    """Few rows: query offsets that go back stop the call whether the sequence's key offsets fit or not."""
+    g = _gen(12)
+    q, k = _randn(g, 30, 4, 64, dtype=torch.bfloat16), _randn(g, 50, 4, 64, dtype=torch.bfloat16)
+    for ko in ([0, 10, 20, 50], [0, 10, 60, 50], [0, 10, 5, 50]):
+        qo = [0, 20, 10, 30]
+        ws = serve.prompt_workspace(q, k, _i32(qo))
+        out = torch.full_like(q, 7.0)
+        say(f"[case] prompt offsets {qo}, keys {ko}")
+        serve.attend_prompt(q, k, k, _i32(qo), _i32(ko), 0.1, out=out, ws=ws)
+        assert int(ws.err.item()) == B.CR_ERR_SEQ and bool((out == 7.0).all())
