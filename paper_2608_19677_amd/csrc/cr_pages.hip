@@ -13,13 +13,14 @@ constexpr uint32_t kPgChunk = kPgThreads * kPgPer;   // pages per block
 constexpr uint32_t kCopyThreads = 256;
 
 // Workspace: free pages per chunk [chunks], pages live, pages that move, then the first page of each
-// sequence in the order of taking [n + 1] (extend, fork) or, for compact, holes, pages by live rank and
-// live rank by page [3][num_pages].
+// sequence in the order of taking [n + 1] and the page its tail is copied from [n] (extend, fork) or, for
+// compact, holes, pages by live rank and live rank by page [3][num_pages].
 struct PgWs {
     uint32_t* free_in;
     uint32_t* live;
     uint32_t* moves;
     uint32_t* first;
+    uint32_t* from;
     uint32_t* holes;
     uint32_t* by_rank;
     uint32_t* rank;
@@ -27,13 +28,14 @@ struct PgWs {
 
 inline uint32_t pg_chunks(uint32_t num_pages) { return (num_pages + kPgChunk - 1) / kPgChunk; }
 
-inline PgWs pg_ws(void* ws, uint32_t num_pages)
+inline PgWs pg_ws(void* ws, uint32_t num_pages, uint32_t n)
 {
     PgWs w;
     w.free_in = reinterpret_cast<uint32_t*>(ws);
     w.live = w.free_in + pg_chunks(num_pages);
     w.moves = w.live + 1;
     w.first = w.moves + 1;
+    w.from = w.first + n + 1;
     w.holes = w.moves + 1;
     w.by_rank = w.holes + num_pages;
     w.rank = w.by_rank + num_pages;
@@ -95,7 +97,8 @@ __device__ __forceinline__ void pg_sums(const uint32_t* __restrict__ free_in, ui
 }
 
 // Blocks 0 .. chunks-1: free pages of each chunk. Block `chunks`: exclusive prefix of the sequences'
-// needs. Blocks behind: a child's row each, its parent's full pages and CR_NO_PAGE behind them.
+// needs. Blocks behind: a child's row each, its parent's full pages and CR_NO_PAGE behind them, and the page
+// its tail is copied from. Counts are as they were before the call here only: pages taken later look live.
 __global__ __launch_bounds__(256) void k_pages_count(const uint32_t* __restrict__ refs, uint32_t chunks, PgWs w, PgTake t,
                                                      uint32_t* __restrict__ err)
 {
@@ -119,6 +122,7 @@ __global__ __launch_bounds__(256) void k_pages_count(const uint32_t* __restrict_
         const uint32_t i = blockIdx.x - chunks - 1u;
         const uint32_t p = t.parent[i], len = t.length[i], pages = pages_of(len, t.log_tokens), full = len >> t.log_tokens;
         const bool fits = p < t.rows && pages <= t.width && pages <= t.out_width;
+        if (threadIdx.x == 0 && !(fits && full < pages)) w.from[i] = CR_NO_PAGE;  // no tail
         for (uint32_t j = threadIdx.x; j < t.out_width; j += kPgThreads) {
             uint32_t g = CR_NO_PAGE;
             if (fits && j < pages) {
@@ -128,6 +132,7 @@ __global__ __launch_bounds__(256) void k_pages_count(const uint32_t* __restrict_
                     g = CR_NO_PAGE;
                 }
             }
+            if (fits && j == full && full < pages) w.from[i] = g;
             t.out[(uint64_t)i * t.out_width + j] = j < full ? g : CR_NO_PAGE;
         }
     }
@@ -244,17 +249,16 @@ __device__ __forceinline__ void pg_copy_tail(const PgPlanes& c, uint32_t src, ui
     }
 }
 
-__global__ __launch_bounds__(256) void k_pages_tail(PgPlanes c, PgTake t)
+__global__ __launch_bounds__(256) void k_pages_tail(PgPlanes c, PgWs w, PgTake t)
 {
     for (uint64_t u = blockIdx.x; u < (uint64_t)t.n * c.planes; u += gridDim.x) {
         const uint32_t i = (uint32_t)(u / c.planes);
-        const uint32_t len = t.length[i], full = len >> t.log_tokens, tail = len & ((1u << t.log_tokens) - 1u);
-        if (tail == 0u || full >= t.out_width) continue;
-        const uint32_t dst = t.out[(uint64_t)i * t.out_width + full];
-        if (dst >= t.num_pages) continue;  // not served
-        const uint32_t src = t.table[(uint64_t)t.parent[i] * t.width + full];
-        if (src >= t.num_pages) continue;  // reported with the rows
-        pg_copy_tail(c, src, dst, tail, (uint32_t)(u % c.planes), threadIdx.x, kCopyThreads);
+        const uint32_t src = w.from[i];
+        if (src == CR_NO_PAGE) continue;  // no tail, or reported with the rows
+        const uint32_t len = t.length[i];
+        const uint32_t dst = t.out[(uint64_t)i * t.out_width + (len >> t.log_tokens)];
+        if (dst == CR_NO_PAGE) continue;  // not served
+        pg_copy_tail(c, src, dst, len & ((1u << t.log_tokens) - 1u), (uint32_t)(u % c.planes), threadIdx.x, kCopyThreads);
     }
 }
 
@@ -530,7 +534,7 @@ inline PgCopy pg_copy(const cr_kv_cache* c)
 
 extern "C" size_t cr_pages_workspace_bytes(uint32_t num_pages, uint32_t n)
 {
-    const size_t a = (size_t)n + 1u, b = 3u * (size_t)num_pages;
+    const size_t a = 2u * (size_t)n + 1u, b = 3u * (size_t)num_pages;
     return ((size_t)cr::pg_chunks(num_pages) + 2u + (a > b ? a : b)) * sizeof(uint32_t);
 }
 
@@ -546,7 +550,7 @@ extern "C" cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_o
     if (ws_bytes < cr_pages_workspace_bytes(c->num_pages, n)) return CR_ESIZE;
     if (n == 0) return CR_OK;
     const uint32_t chunks = pg_chunks(c->num_pages);
-    const PgWs w = pg_ws(ws, c->num_pages);
+    const PgWs w = pg_ws(ws, c->num_pages, n);
     PgTake t{};
     t.len_old = len_old;
     t.len_new = len_new;
@@ -578,7 +582,7 @@ extern "C" cr_status cr_pages_fork(const cr_kv_cache* c, const uint32_t* table, 
     if (ws_bytes < cr_pages_workspace_bytes(c->num_pages, n)) return CR_ESIZE;
     if (n == 0) return CR_OK;
     const uint32_t chunks = pg_chunks(c->num_pages);
-    const PgWs w = pg_ws(ws, c->num_pages);
+    const PgWs w = pg_ws(ws, c->num_pages, n);
     PgTake t{};
     t.parent = parent;
     t.length = length;
@@ -599,7 +603,7 @@ extern "C" cr_status cr_pages_fork(const cr_kv_cache* c, const uint32_t* table, 
     } else {
         hipLaunchKernelGGL(k_pages_count, dim3(chunks + 1 + n), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
         hipLaunchKernelGGL(k_pages_take, dim3(chunks + n), dim3(kPgThreads), 0, st, c->refs, chunks, w, t, err);
-        hipLaunchKernelGGL(k_pages_tail, dim3((uint32_t)(units < (1u << 20) ? units : (1u << 20))), dim3(kCopyThreads), 0, st, planes, t);
+        hipLaunchKernelGGL(k_pages_tail, dim3((uint32_t)(units < (1u << 20) ? units : (1u << 20))), dim3(kCopyThreads), 0, st, planes, w, t);
     }
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
 }
@@ -629,7 +633,7 @@ extern "C" cr_status cr_pages_compact(const cr_kv_cache* c, const uint32_t* tabl
         return CR_EINVAL;
     if (ws_bytes < cr_pages_workspace_bytes(c->num_pages, 0)) return CR_ESIZE;
     const uint32_t chunks = pg_chunks(c->num_pages);
-    const PgWs w = pg_ws(ws, c->num_pages);
+    const PgWs w = pg_ws(ws, c->num_pages, 0);
     PgTake t{};
     t.num_pages = c->num_pages;
     const PgCopy m = pg_copy(c);
