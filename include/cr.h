@@ -458,7 +458,8 @@ cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_old, const u
  * length beyond either width sets CR_ERR_SEQ and that child gets no pages; an entry that is out of
  * range or names a free page sets CR_ERR_PAGE and becomes CR_NO_PAGE (a tail's is copied from
  * nowhere). CR_ERR_PAGES_OUT as cr_pages_extend, and then no page is taken or shared and all
- * children's entries are CR_NO_PAGE. */
+ * children's entries are CR_NO_PAGE. n + ceil(num_pages / 4096) + 1 < 2^24 (CR_EINVAL otherwise: blocks of a
+ * launch). */
 cr_status cr_pages_fork(const cr_kv_cache* c, const uint32_t* table, uint32_t rows, uint32_t width,
                         const uint32_t* parent, const uint32_t* length, uint32_t n, uint32_t* child,
                         uint32_t child_width, void* ws, size_t ws_bytes, uint32_t* err, void* stream);

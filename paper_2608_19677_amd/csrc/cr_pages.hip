@@ -579,9 +579,10 @@ extern "C" cr_status cr_pages_fork(const cr_kv_cache* c, const uint32_t* table, 
         child_width > (1u << 28) ||
         (n > 0 && (!parent || !length || (rows > 0 && width > 0 && !table) || (child_width > 0 && !child) || child == table)))
         return CR_EINVAL;
+    const uint32_t chunks = pg_chunks(c->num_pages);
+    if ((uint64_t)chunks + 1u + n >= ((uint64_t)1 << 32) / kPgThreads) return CR_EINVAL;  // threads of a launch
     if (ws_bytes < cr_pages_workspace_bytes(c->num_pages, n)) return CR_ESIZE;
     if (n == 0) return CR_OK;
-    const uint32_t chunks = pg_chunks(c->num_pages);
     const PgWs w = pg_ws(ws, c->num_pages, n);
     PgTake t{};
     t.parent = parent;

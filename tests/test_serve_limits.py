@@ -1,0 +1,23 @@
+"""Sizes that pass what a launch takes are refused on the host, before any kernel of the call is enqueued
+(no GPU, no pointer is dereferenced)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2608_19677_amd import binding as B
+
+from test_serve_validation import FAKE, L, _cache  # noqa: F401
+
+# As in test_serve_validation.py: a regression would launch a kernel on a fake address where a GPU is.
+pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="host-side validation tests run without a GPU")
+
+
+@pytest.mark.parametrize("pages", [40, 4097, 1 << 26])
+def test_fork_of_more_children_than_a_launch_takes(L, pages):  # noqa: F811
+    """A block of 256 threads a child, one for the prefix of needs and one per 4,096 pages: 2^32 threads are too many."""
+    c = ctypes.byref(_cache(num_pages=pages))
+    chunks = -(-pages // 4096)
+    fork = lambda n: L.cr_pages_fork(c, FAKE, 1, 4, FAKE, FAKE, n, FAKE + 64, 4, FAKE, 0, FAKE, None)  # noqa: E731
+    assert fork((1 << 24) - chunks - 1) == B.CR_EINVAL and fork(1 << 24) == B.CR_EINVAL
+    assert fork((1 << 24) - chunks - 2) == B.CR_ESIZE  # the sizes are taken, the workspace is too small
