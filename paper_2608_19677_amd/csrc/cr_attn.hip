@@ -1321,9 +1321,11 @@ cr_status dispatch(Attn& a, const Shape& s, void* ws, uint32_t dtype, uint32_t d
 {
     const hipStream_t st = as_stream(stream);
     const uint64_t rows = (uint64_t)a.total_q * a.group;
+    // Threads of a launch: two parts' tiles of 128 rows, or one's and the few-row blocks, stay below 2^32 with these.
     for (uint32_t i = 0; i < s.wides; ++i)
         if ((rows / s.wide[i].rows + a.batch) * (s.wide[i].kind == kOwn ? s.own_slots : s.slots) * a.heads_kv >= (1ull << 32) / (8u * kWave))
-            return CR_EINVAL;  // threads of a launch
+            return CR_EINVAL;
+    if (s.join && a.total_q >= (1ull << 32) / kThreads) return CR_EINVAL;  // a block of the join per token
     a.first = s.first;
     a.chunk = s.chunk;
     a.slots = s.slots;
