@@ -109,8 +109,9 @@ class PagePool:
         self.c = B.CrKvCache(_dtype(k), self.heads, self.dim, self.page_tokens, self.num_pages, self.layers, k.data_ptr(),
                              v.data_ptr(), k.stride(0), k.stride(1), k.stride(h), k.stride(t), _index(refs, self.num_pages))
         self._ref, self._err = ctypes.byref(self.c), _index(self.err)
-        self._ws: Optional[torch.Tensor] = None
-        self._ws_for = -1  # sequences that it is large enough for
+        self._ws = torch.empty(B.cr_pages_workspace_bytes(self.num_pages, 0), dtype=torch.uint8, device=k.device)
+        self._ws_for = 0  # sequences that it is known to be large enough for
+        self._outgrown = []  # smaller ones before it: captured graphs may go on using them
 
     @classmethod
     def empty(cls, layers: int, num_pages: int, heads: int, page_tokens: int, dim: int, dtype=torch.bfloat16, device="cuda",
@@ -121,9 +122,14 @@ class PagePool:
                    torch.zeros(num_pages, dtype=torch.int32, device=device), order)
 
     def _scratch(self, n: int, stream):
-        """The page calls' workspace, kept with the handle: its calls are for one stream at a time."""
+        """The page calls' workspace, kept with the handle: its calls are for one stream at a time. It stays where it
+        is until a call has more than about 1.5 sequences per page of the cache; at least doubled then, so that those
+        it has outgrown are no more than it."""
         if n > self._ws_for:
-            self._ws = torch.empty(B.cr_pages_workspace_bytes(self.num_pages, n), dtype=torch.uint8, device=self.k.device)
+            nbytes = B.cr_pages_workspace_bytes(self.num_pages, n)
+            if nbytes > self._ws.numel():
+                self._outgrown.append(self._ws)
+                self._ws = torch.empty(max(nbytes, 2 * self._ws.numel()), dtype=torch.uint8, device=self.k.device)
             self._ws_for = n
         _used_on(stream, self._ws)
         return self._ws.data_ptr(), self._ws.numel(), self._err, B._stream(stream)

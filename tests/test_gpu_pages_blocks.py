@@ -51,3 +51,33 @@ def test_fork_of_a_tail_in_a_free_page(pages):
     assert torch.equal(pool.refs, refs)
     k[:, 5, :, :3], v[:, 5, :, :3] = k[:, 2, :, :3], v[:, 2, :, :3]
     assert torch.equal(pool.k, k) and torch.equal(pool.v, v)
+
+
+@pytest.mark.parametrize("later", [40, 31_000], ids=["same", "grown"])
+def test_a_graph_keeps_its_workspace(later):
+    """A captured call's workspace stays the pool's when later calls have more sequences, whether they fit it or
+    not: a replay writes into nobody else's memory."""
+    pool = _pool(PAGES)
+    live = torch.randperm(PAGES, generator=torch.Generator().manual_seed(5))[:9000].sort().values.cuda()
+    table, length = live[::300].to(torch.int32).reshape(1, -1).contiguous(), _i32([4 * 30])
+    out, counts = torch.empty_like(table), torch.empty_like(pool.refs)
+    pool.refs[live] = 1
+    pool.compact(table, length, table_out=out, refs_out=counts)
+    want, want_counts = out.clone(), counts.clone()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        pool.compact(table, length, table_out=out, refs_out=counts)
+    size = pool._ws.numel()
+    say(f"[case] compaction in a graph, then {later} sequences")
+    free = torch.full((later, 1), -1, dtype=torch.int32, device="cuda")
+    pool.extend(free, None, torch.zeros(later, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    others = [torch.full((size,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(6)]
+    for _ in range(3):
+        out.zero_(), counts.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(counts, want_counts)
+        assert all(bool((x == 0x5A).all()) for x in others)
+    assert _err(pool) == 0
