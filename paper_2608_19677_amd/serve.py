@@ -81,16 +81,35 @@ def _used_on(stream, *tensors):
             t.record_stream(stream)
 
 
-class Workspace:
+class _Memory:
+    """Device memory that calls on any stream use: once its owner is dropped, it is not handed out before the
+    work enqueued on each of them is done. (Not what a graph captured: its owner has to outlive the graph.)"""
+
+    def __init__(self, *tensors):
+        self._memory, self._seen = list(tensors), set()
+
+    def _on(self, stream) -> Optional[int]:
+        """Handle of the stream of a call: ``stream``, or the current one."""
+        handle = B._stream(stream)
+        if handle not in self._seen and not torch.cuda.is_current_stream_capturing():
+            s = torch.cuda.current_stream() if stream is None else stream
+            for t in self._memory:
+                t.record_stream(s)
+            self._seen.add(handle)
+        return handle
+
+
+class Workspace(_Memory):
     """Device scratch of an attention call and its error word."""
 
     def __init__(self, nbytes: int, device, err: Optional[torch.Tensor] = None):
         self.buf = torch.empty(max(16, nbytes), dtype=torch.uint8, device=device)
         self.err = torch.zeros(1, dtype=torch.int32, device=device) if err is None else err
         self.args = self.buf.data_ptr(), self.buf.numel(), _index(self.err, 1)
+        super().__init__(self.buf, self.err)
 
 
-class PagePool:
+class PagePool(_Memory):
     """Handle of a paged cache. ``k``, ``v``: [layers, pages, heads, tokens, dim] (``order``
     "head") or [layers, pages, tokens, heads, dim] ("token"), bfloat16 or float16, equal
     strides; ``refs``: int32 [pages], how many table entries name a page (0 = free)."""
@@ -111,7 +130,7 @@ class PagePool:
         self._ref, self._err = ctypes.byref(self.c), _index(self.err)
         self._ws = torch.empty(B.cr_pages_workspace_bytes(self.num_pages, 0), dtype=torch.uint8, device=k.device)
         self._ws_for = 0  # sequences that it is known to be large enough for
-        self._outgrown = []  # smaller ones before it: captured graphs may go on using them
+        super().__init__(k, v, refs, self.err, self._ws)
 
     @classmethod
     def empty(cls, layers: int, num_pages: int, heads: int, page_tokens: int, dim: int, dtype=torch.bfloat16, device="cuda",
@@ -128,11 +147,11 @@ class PagePool:
         if n > self._ws_for:
             nbytes = B.cr_pages_workspace_bytes(self.num_pages, n)
             if nbytes > self._ws.numel():
-                self._outgrown.append(self._ws)
                 self._ws = torch.empty(max(nbytes, 2 * self._ws.numel()), dtype=torch.uint8, device=self.k.device)
+                self._memory.append(self._ws)  # the smaller one stays: captured graphs may go on using it
+                self._seen.clear()
             self._ws_for = n
-        _used_on(stream, self._ws)
-        return self._ws.data_ptr(), self._ws.numel(), self._err, B._stream(stream)
+        return self._ws.data_ptr(), self._ws.numel(), self._err, self._on(stream)
 
     def pages_of(self, tokens: int) -> int:
         return -(-tokens // self.page_tokens)
@@ -155,7 +174,7 @@ class PagePool:
         """Gives the pages of every row's first length tokens back."""
         n = length.numel()
         p, width = _table(table, n)
-        B._check(B.load().cr_pages_free(self._ref, p, width, _index(length), n, self._err, B._stream(stream)), "cr_pages_free")
+        B._check(B.load().cr_pages_free(self._ref, p, width, _index(length), n, self._err, self._on(stream)), "cr_pages_free")
 
     def compact(self, table, length, table_out=None, refs_out=None, stream=None):
         """Moves the live pages to the front and renames the table's entries (in place, if no
@@ -172,7 +191,7 @@ class PagePool:
     def copy(self, src, dst, stream=None):
         """Contents of page src[i] to page dst[i], all layers."""
         n = src.numel()
-        B._check(B.load().cr_pages_copy(self._ref, _index(src), _index(dst, n), n, self._err, B._stream(stream)), "cr_pages_copy")
+        B._check(B.load().cr_pages_copy(self._ref, _index(src), _index(dst, n), n, self._err, self._on(stream)), "cr_pages_copy")
 
     def append(self, layer: int, k, v, off, length, table, stream=None):
         """Rows off[i]..off[i+1] of k and v ([total, heads, dim]) become the last tokens of the
@@ -182,7 +201,7 @@ class PagePool:
             raise B.CrError("new keys and values have the cache's heads, dim and type")
         p, width = _table(table, n)
         B._check(B.load().cr_kv_append(self._ref, layer, _pack_rows(*_rows(k)), _pack_rows(*_rows(v)), shape[0],
-                                       _index(off, n + 1), _index(length), n, p, width, self._err, B._stream(stream)), "cr_kv_append")
+                                       _index(off, n + 1), _index(length), n, p, width, self._err, self._on(stream)), "cr_kv_append")
 
 
 def _check_out(q, shape, out, lse):
@@ -222,8 +241,7 @@ def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, ca
         raise B.CrError(f"an argument is out of range: {e}") from None
     if ws is None:
         ws = prompt_workspace(q, k, q_off)
-        _used_on(stream, ws.buf, ws.err)
-    B._check(B.load().cr_attn_prompt(a, *ws.args, B._stream(stream)), "cr_attn_prompt")
+    B._check(B.load().cr_attn_prompt(a, *ws.args, ws._on(stream)), "cr_attn_prompt")
     return out
 
 
@@ -257,6 +275,6 @@ def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table,
         raise B.CrError(f"an argument is out of range: {e}") from None
     if ws is None:
         ws = shared_workspace(q, pool, group_off, prefix_table, own_table)
-        _used_on(stream, ws.buf)
-    B._check(B.load().cr_attn_shared(pool._ref, a, *ws.args, B._stream(stream)), "cr_attn_shared")
+    pool._on(stream)
+    B._check(B.load().cr_attn_shared(pool._ref, a, *ws.args, ws._on(stream)), "cr_attn_shared")
     return out
