@@ -18,6 +18,7 @@ skipped as the library documents.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import struct
 from typing import Optional
@@ -28,6 +29,7 @@ from . import binding as B
 
 _DTYPES = {torch.bfloat16: B.CR_BF16, torch.float16: B.CR_F16}
 _INT32, _FLOAT32 = torch.int32, torch.float32
+_HERE = contextlib.nullcontext()
 _pack_rows, _pack_prompt, _pack_shared, _RANGE = B.ROWS.pack, B.PROMPT_ARGS.pack, B.SHARED_ARGS.pack, (struct.error, OverflowError)
 
 
@@ -74,11 +76,18 @@ def _table(t: torch.Tensor, n: int):
     return _index(t), shape[1]
 
 
-def _used_on(stream, *tensors):
-    """Memory taken here from the current stream's pool and used on another stream."""
+def _taken_on(stream):
+    """Memory for a call is taken from the pool of the stream that it works on: a piece of the current stream's may
+    still be written to by what is enqueued there."""
+    return _HERE if stream is None else torch.cuda.stream(stream)
+
+
+def _new_out(q, stream):
+    with _taken_on(stream):
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if stream is not None:
-        for t in tensors:
-            t.record_stream(stream)
+        out.record_stream(torch.cuda.current_stream())  # the caller's, where it goes on with it
+    return out
 
 
 class _Memory:
@@ -147,7 +156,8 @@ class PagePool(_Memory):
         if n > self._ws_for:
             nbytes = B.cr_pages_workspace_bytes(self.num_pages, n)
             if nbytes > self._ws.numel():
-                self._ws = torch.empty(max(nbytes, 2 * self._ws.numel()), dtype=torch.uint8, device=self.k.device)
+                with _taken_on(stream):
+                    self._ws = torch.empty(max(nbytes, 2 * self._ws.numel()), dtype=torch.uint8, device=self.k.device)
                 self._memory.append(self._ws)  # the smaller one stays: captured graphs may go on using it
                 self._seen.clear()
             self._ws_for = n
@@ -230,8 +240,7 @@ def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, ca
         raise B.CrError("q, k and v have one type and dim, k and v one shape")
     code = _dtype(q)
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        _used_on(stream, out)
+        out = _new_out(q, stream)
     _check_out(q, shape, out, lse)
     n = q_off.numel()
     try:
@@ -240,7 +249,8 @@ def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, ca
     except _RANGE as e:
         raise B.CrError(f"an argument is out of range: {e}") from None
     if ws is None:
-        ws = prompt_workspace(q, k, q_off)
+        with _taken_on(stream):
+            ws = prompt_workspace(q, k, q_off)
     B._check(B.load().cr_attn_prompt(a, *ws.args, ws._on(stream)), "cr_attn_prompt")
     return out
 
@@ -262,8 +272,7 @@ def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table,
     if q.dtype is not pool.k.dtype or len(shape) != 3 or shape[2] != pool.dim:
         raise B.CrError("q has the cache's type and dim")
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        _used_on(stream, out)
+        out = _new_out(q, stream)
     _check_out(q, shape, out, lse)
     batch, groups = own_len.numel(), group_off.numel() - 1
     own, own_width = _table(own_table, batch)
@@ -274,7 +283,8 @@ def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table,
     except _RANGE as e:
         raise B.CrError(f"an argument is out of range: {e}") from None
     if ws is None:
-        ws = shared_workspace(q, pool, group_off, prefix_table, own_table)
+        with _taken_on(stream):
+            ws = shared_workspace(q, pool, group_off, prefix_table, own_table)
     pool._on(stream)
     B._check(B.load().cr_attn_shared(pool._ref, a, *ws.args, ws._on(stream)), "cr_attn_shared")
     return out

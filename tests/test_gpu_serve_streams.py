@@ -71,3 +71,45 @@ def test_a_dropped_workspace_is_kept_until_its_work_is_done(named):
     assert not side.query() and not taken
     side.synchronize()
     assert torch.equal(out, want)
+
+
+def _pool_of(t):
+    """Handle of the stream from whose memory a tensor was taken."""
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]:
+            return s["stream"]
+    raise AssertionError("not in any segment")
+
+
+def test_what_a_call_takes_is_its_streams():
+    """Outputs and workspaces made for a call on a named stream come from that stream's memory: the current
+    stream's may still be written to by work enqueued there. The output also stays whole for the current stream."""
+    q = torch.randn(3, 8, 64, device="cuda").to(torch.float16)
+    k = torch.randn(3, 4, 64, device="cuda").to(torch.float16)
+    off = _i32([0, 3])
+    side = torch.cuda.Stream()
+    say("[case] prompt attention on a named stream")
+    want = serve.attend_prompt(q, k, k, off, off, 0.1)
+    torch.cuda.synchronize()
+    out = serve.attend_prompt(q, k, k, off, off, 0.1, stream=side)
+    assert _pool_of(want) != side.cuda_stream and _pool_of(out) == side.cuda_stream
+    side.synchronize()
+    assert torch.equal(out, want)
+    say("[case] shared attention and a growing workspace on a named stream")
+    pool = serve.PagePool.empty(1, 300, 4, 16, 64, torch.float16)
+    table, n = torch.zeros(2000, 1, dtype=torch.int32, device="cuda"), torch.zeros(2000, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    pool.extend(table, None, n, stream=side)
+    assert _pool_of(pool._ws) == side.cuda_stream
+    pool.append(0, k, k, off, _i32([3]), table[:1])
+    torch.cuda.synchronize()
+    args = (q, pool, 0, off, _i32([0, 1]), table[:1], _i32([0]), table[:1], _i32([3]), 0.1)
+    torch.cuda.synchronize()
+    out = serve.attend_shared(*args, stream=side)
+    assert _pool_of(out) == side.cuda_stream
+    _busy(torch.cuda.current_stream())  # the caller goes on with it
+    at, size = out.data_ptr(), out.numel() * 2
+    del out
+    with torch.cuda.stream(side):
+        assert not _handed_out(size, at)
+    assert int(pool.err.item()) == 0
