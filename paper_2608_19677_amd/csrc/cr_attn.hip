@@ -234,6 +234,8 @@ template <int kDim, bool kPaged, uint32_t kTile, uint32_t kMovers>
 struct Loader {
     static constexpr uint32_t kPieces = kDim / 8, kStep = kMovers / kPieces, kPer = kTile / kStep;
     static constexpr uint32_t kWaveRows = kWave / kPieces;  // rows that a wavefront moves at once
+    // Longest stride whose lane offsets, up to kWaveRows - 1 rows and a piece, stay in 32 bits.
+    static constexpr uint32_t kLaneStride = (0xFFFFFFFFu - kDim) / (kWaveRows - 1u);
     const uint16_t *kb, *vb;  // of the key head (prompt: at the sequence's first key)
     uint32_t row, piece, end, lane_k, lane_v, bad;
     uint32_t page[kPer];      // of the next tile's rows
@@ -273,15 +275,17 @@ struct Loader {
         for (uint32_t p = 0; p < kPer; ++p) to[p] = table[min(first + p * kStep + row, last - 1u) >> a.pg.log_tokens];
     }
     __device__ __forceinline__ void pages(const Attn& a, const Seq& s, uint32_t k0) { pages_of_tile(a, s, k0, end, row, page); }
-    // Whole tiles whose rows of one wavefront and pass lie in one page: scalar addresses. Otherwise an
-    // address per lane; rows behind the last key repeat it: their weights are 0, and nothing foreign is
+    // Whole tiles whose rows of one wavefront and pass lie in one page and not too far apart: scalar addresses.
+    // Otherwise an address per lane; rows behind the last key repeat it: their weights are 0, and nothing foreign is
     // read.
     __device__ __forceinline__ void load(const Attn& a, const Seq& s, uint32_t k0)
     {
         const uint32_t mask = (1u << a.pg.log_tokens) - 1u;
         uint32_t first = k0, last = end;
         if (kPaged) place(s, k0, end, &first, &last);
-        if (first + kTile <= last && (!kPaged || mask >= kWaveRows - 1u)) {
+        const bool near = kPaged ? mask >= kWaveRows - 1u && (uint32_t)a.pg.token_stride <= kLaneStride
+                                 : max((uint32_t)a.k.token_stride, (uint32_t)a.v.token_stride) <= kLaneStride;
+        if (first + kTile <= last && near) {
             const uint32_t r0 = __builtin_amdgcn_readfirstlane(row);
 #pragma unroll
             for (uint32_t p = 0; p < kPer; ++p) {
