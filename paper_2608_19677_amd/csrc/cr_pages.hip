@@ -337,8 +337,9 @@ __global__ __launch_bounds__(256) void k_pages_free(uint32_t* __restrict__ refs,
                                                     const uint32_t* __restrict__ length, uint32_t n, uint32_t* __restrict__ err)
 {
     const uint64_t x = (uint64_t)blockIdx.x * kPgThreads + threadIdx.x;
-    if (x >= (uint64_t)n * width) return;
-    const uint32_t i = (uint32_t)(x / width), j = (uint32_t)(x % width);
+    const uint32_t per = max(width, 1u);  // threads per row; one looks at the length where there are no entries
+    if (x >= (uint64_t)n * per) return;
+    const uint32_t i = (uint32_t)(x / per), j = (uint32_t)(x % per);
     const uint32_t pages = pages_of(length[i], log_tokens);
     if (pages > width) {
         if (j == 0) atomicOr(err, CR_ERR_SEQ);
