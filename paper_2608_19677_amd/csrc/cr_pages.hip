@@ -470,6 +470,8 @@ __global__ __launch_bounds__(256) void k_pages_move(PgCopy c, PgWs w, uint32_t n
             }
             table_out[x] = g;
         }
+        if (width == 0u)  // no entries to go by
+            for (uint32_t i = x0; i < rows; i += stride) bad |= length[i] ? CR_ERR_SEQ : 0u;
         if (bad) atomicOr(err, bad);
         return;
     }

@@ -30,3 +30,12 @@ def test_free(length, bits):
     say(f"[case] free, no columns, {len(length)} rows")
     pool.free(_none(len(length)), _i32(length))
     assert int(pool.err.item()) == bits and pool.refs.tolist() == [1] * 3 + [0] * 7
+
+
+@pytest.mark.parametrize("length,bits", [([0, 0], 0), ([0, 5], B.CR_ERR_SEQ), ([1], B.CR_ERR_SEQ), ([0] * 300 + [2 ** 31 - 1], B.CR_ERR_SEQ)])
+def test_compact(length, bits):
+    pool = _pool()
+    pool.refs[8] = 2
+    say(f"[case] compact, no columns, {len(length)} rows")
+    pool.compact(_none(len(length)), _i32(length))
+    assert int(pool.err.item()) == bits and pool.refs.tolist() == [1, 1, 1, 2] + [0] * 6
