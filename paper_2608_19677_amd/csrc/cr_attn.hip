@@ -672,6 +672,12 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
         return;
     }
     if (a.lse && half == 0) a.lse[orow] = lse2 * kLn2;
+    if (none) {  // weights of 0 times values that are not finite
+#pragma unroll
+        for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    }
     uint16_t* op = (uint16_t*)a.out.p + (int64_t)tok * a.out.token_stride + (int64_t)head * a.out.head_stride;
 #pragma unroll
     for (int d = 0; d < kDim / 32; ++d)
@@ -995,6 +1001,7 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             }
             const bool none = total == 0.f;
             const float inv = none ? 0.f : 1.f / total_rounded, lse2 = none ? -INFINITY : mx + log2f(total);
+            if (none) acc = f32x4{0.f, 0.f, 0.f, 0.f};  // weights of 0 times values that are not finite
             const uint32_t ot = it.tok0 + mm / a.group, oh = head_kv * a.group + mm % a.group;
             const uint64_t orow = (uint64_t)ot * a.heads_q + oh;
             if (a.part_o) {
