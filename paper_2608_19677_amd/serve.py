@@ -13,8 +13,8 @@ library does the work.
 
 Tensors are on the GPU. Offsets, lengths and page tables are int32; a call enqueues kernels on
 ``stream`` (default: the current one) and returns. Problems that only the device sees set bits
-of ``pool.err`` or of the workspace's ``err`` (``CR_ERR_*``), and the sequence concerned is
-skipped as the library documents.
+of ``pool.err``, of the workspace's ``err`` or of an ``err`` given (``CR_ERR_*``), and the sequence
+concerned is skipped as the library documents.
 """
 from __future__ import annotations
 
@@ -231,10 +231,13 @@ def prompt_workspace(q, k, q_off, err: Optional[torch.Tensor] = None) -> Workspa
 
 
 def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, causal: bool = True,
-                  ws: Optional[Workspace] = None, stream=None):
+                  ws: Optional[Workspace] = None, err: Optional[torch.Tensor] = None, stream=None):
     """Attention of packed sequences: q [total_q, heads_q, dim], k, v [total_k, heads_kv, dim],
     sequence b at q_off[b]..q_off[b+1] and k_off[b]..k_off[b+1]. Returns out (and fills lse,
-    float32 [total_q, heads_q], if given)."""
+    float32 [total_q, heads_q], if given). Problems that only the device sees set bits of ``ws.err`` or,
+    where no workspace is given, of ``err`` (int32 [1]); with neither they show in no word."""
+    if ws is not None and err is not None:
+        raise B.CrError("a workspace has an error word of its own")
     shape, keys, dtype = q.shape, k.shape, q.dtype
     if keys != v.shape or len(keys) != 3 or len(shape) != 3 or keys[2] != shape[2] or k.dtype is not dtype or v.dtype is not dtype:
         raise B.CrError("q, k and v have one type and dim, k and v one shape")
@@ -250,7 +253,7 @@ def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, ca
         raise B.CrError(f"an argument is out of range: {e}") from None
     if ws is None:
         with _taken_on(stream):
-            ws = prompt_workspace(q, k, q_off)
+            ws = prompt_workspace(q, k, q_off, err)
     B._check(B.load().cr_attn_prompt(a, *ws.args, ws._on(stream)), "cr_attn_prompt")
     return out
 
