@@ -28,6 +28,7 @@ from typing import List
 import numpy as np
 import torch
 
+from . import binding as B
 from . import serve
 
 
@@ -76,6 +77,7 @@ class Destination:
         self.slots: "OrderedDict[int, int]" = OrderedDict()  # key -> row, least recent first
         self.project = project or Projection(heads_q, heads_kv, dim, dtype, device)
         self.counts = Counts()
+        self.prefilled = None  # the last batch's misses: keys, offsets, outputs of the last layer
 
     def _i32(self, v):
         return torch.tensor(np.asarray(v, dtype=np.int32), device=self.device)
@@ -88,7 +90,8 @@ class Destination:
         """A batch of requests in arrival order: their keys, prefix lengths and suffix lengths. Returns
         per request whether its prefix was cached, and the attention outputs of the last layer:
         [tokens, heads, dim] of the suffixes packed in the order of ``order`` with the offsets, and,
-        with ``samples``, of one decoded token per continuation."""
+        with ``samples``, of one decoded token per continuation. Raises where a call of the batch reported a
+        problem (bits of ``pool.err``)."""
         assert 0 < len(keys) <= self.batch
         hit, row, missed, gone = [], [], [], []
         for k, n in zip(keys, prefix_len):
@@ -110,6 +113,7 @@ class Destination:
             row.append(self.slots[k])
         self.counts.requests += len(keys)
         self.counts.prefill += int(np.sum(suffix_len, dtype=np.int64))
+        self.prefilled = None
         if missed:
             self._prefill(missed)
         order = np.argsort(np.asarray(row), kind="stable")  # requests of one prefix side by side
@@ -117,7 +121,13 @@ class Destination:
         for r in gone:
             self.pool.free(self.table[r:r + 1], self._i32([self.length[r]]))
             self.rows.append(r)
+        self._check()
         return hit, order, out
+
+    def _check(self):
+        bits = int(self.pool.err.item())
+        if bits:
+            raise B.CrError(f"a call on the cache reported {bits:#x}")
 
     def _prefill(self, missed):
         rows = torch.tensor([r for _, r in missed], device=self.device)
@@ -125,11 +135,13 @@ class Destination:
         table = torch.full((len(missed), self.width), -1, dtype=torch.int32, device=self.device)
         n, off = self._i32(lengths), self._i32(self._off(lengths))
         self.pool.extend(table, None, n)
+        out = None
         for layer in range(self.layers):
             q, k, v = self.project(layer, [key for key, _ in missed], lengths)
-            serve.attend_prompt(q, k, v, off, off, self.scale)
+            out = serve.attend_prompt(q, k, v, off, off, self.scale, err=self.pool.err)
             self.pool.append(layer, k, v, off, n, table)
         self.table[rows] = table
+        self.prefilled = [key for key, _ in missed], off, out
 
     def _attend(self, row, suffix, ids):
         starts = np.flatnonzero(np.concatenate([[True], row[1:] != row[:-1]]))
@@ -171,6 +183,7 @@ class Destination:
         for r in self.slots.values():
             n[r] = self.length[r]
         self.pool.compact(self.table, self._i32(n))
+        self._check()
 
 
 def main():

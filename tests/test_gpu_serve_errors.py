@@ -4,7 +4,9 @@ import torch
 
 from paper_2608_19677_amd import binding as B
 from paper_2608_19677_amd import serve
+from paper_2608_19677_amd.destination import Destination
 
+import serve_oracle as so
 from cr_check import say
 
 pytestmark = pytest.mark.gpu
@@ -24,3 +26,49 @@ def test_prompt_without_a_workspace():
     assert int(err.item()) == B.CR_ERR_SEQ
     with pytest.raises(B.CrError, match="word of its own"):
         serve.attend_prompt(q, q, q, good, good, 0.1, err=err, ws=serve.prompt_workspace(q, q, good))
+
+
+def _destination(project=None):
+    return Destination(2, 50, 12, 6, layers=2, heads_q=4, heads_kv=1, dim=64, page_tokens=8, project=project)
+
+
+def test_a_destination_raises_what_its_calls_report():
+    d = _destination()
+    d.serve([7], [33], [3])
+    real = d.project
+
+    class Short:
+        """A query too few for the prompts' offsets: their attention reports it, nothing else does."""
+
+        def __call__(self, layer, ids, lengths):
+            q, k, v = real(layer, ids, lengths)
+            return (q[:-1] if 9 in list(ids) else q), k, v
+
+    d.project = Short()
+    d.serve([7], [33], [4])
+    say("[case] a destination's prompt attention with a row too few")
+    with pytest.raises(B.CrError, match="0x10"):
+        d.serve([7, 9], [33, 20], [4, 4])
+
+
+def test_a_destinations_prompts():
+    d = _destination()
+    d.serve([7], [33], [3])
+    d.serve([7], [33], [5])
+    assert d.prefilled is None
+    say("[case] a destination's prompt attention")
+    d.serve([9, 7, 5], [50, 33, 17], [3, 4, 2])
+    keys, off, out = d.prefilled
+    assert keys == [9, 5] and off.tolist() == [0, 50, 67]
+    q, k, v = d.project(1, keys, [50, 17])
+    ref = so.flat(so.prompt(q, k, v, [0, 50, 67], [0, 50, 67], d.scale, True))
+    so.check(out.reshape(-1, 64), None, ref, torch.bfloat16)
+
+
+def test_a_destination_raises_what_compaction_reports():
+    d = _destination()
+    d.serve([7, 9], [33, 20], [3, 4])
+    d.table[d.slots[9], 1] = -1  # an entry that names no page
+    say("[case] a destination's compaction with an entry that names no page")
+    with pytest.raises(B.CrError, match="0x20"):
+        d.compact()
