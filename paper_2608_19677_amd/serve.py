@@ -14,7 +14,8 @@ library does the work.
 Tensors are on the GPU. Offsets, lengths and page tables are int32; a call enqueues kernels on
 ``stream`` (default: the current one) and returns. Problems that only the device sees set bits
 of ``pool.err``, of the workspace's ``err`` or of an ``err`` given (``CR_ERR_*``), and the sequence
-concerned is skipped as the library documents.
+concerned is skipped as the library documents. Nothing here is differentiable: tensors that require
+a gradient are refused where gradients are recorded.
 """
 from __future__ import annotations
 
@@ -51,6 +52,13 @@ def _rows(t: torch.Tensor):
     if not t.is_cuda:
         raise B.CrError("libcr takes device tensors")
     return t.data_ptr(), stride[0], stride[1]
+
+
+_grad_on = torch.is_grad_enabled
+
+
+def _refuse_grad():
+    raise B.CrError("the serving calls have no gradient: call them under torch.no_grad(), or detach what requires one")
 
 
 def _refuse(t, n):
@@ -209,6 +217,8 @@ class PagePool(_Memory):
         shape, n, dtype = k.shape, length.numel(), self.k.dtype
         if len(shape) != 3 or shape[1] != self.heads or shape[2] != self.dim or shape != v.shape or k.dtype is not dtype or v.dtype is not dtype:
             raise B.CrError("new keys and values have the cache's heads, dim and type")
+        if (k.requires_grad or v.requires_grad) and _grad_on():
+            _refuse_grad()
         p, width = _table(table, n)
         B._check(B.load().cr_kv_append(self._ref, layer, _pack_rows(*_rows(k)), _pack_rows(*_rows(v)), shape[0],
                                        _index(off, n + 1), _index(length), n, p, width, self._err, self._on(stream)), "cr_kv_append")
@@ -241,6 +251,8 @@ def attend_prompt(q, k, v, q_off, k_off, scale: float, *, out=None, lse=None, ca
     shape, keys, dtype = q.shape, k.shape, q.dtype
     if keys != v.shape or len(keys) != 3 or len(shape) != 3 or keys[2] != shape[2] or k.dtype is not dtype or v.dtype is not dtype:
         raise B.CrError("q, k and v have one type and dim, k and v one shape")
+    if (q.requires_grad or k.requires_grad or v.requires_grad) and _grad_on():
+        _refuse_grad()
     code = _dtype(q)
     if out is None:
         out = _new_out(q, stream)
@@ -274,6 +286,8 @@ def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table,
     shape = q.shape
     if q.dtype is not pool.k.dtype or len(shape) != 3 or shape[2] != pool.dim:
         raise B.CrError("q has the cache's type and dim")
+    if (q.requires_grad or pool.k.requires_grad or pool.v.requires_grad) and _grad_on():
+        _refuse_grad()
     if out is None:
         out = _new_out(q, stream)
     _check_out(q, shape, out, lse)

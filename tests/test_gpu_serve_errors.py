@@ -72,3 +72,32 @@ def test_a_destination_raises_what_compaction_reports():
     say("[case] a destination's compaction with an entry that names no page")
     with pytest.raises(B.CrError, match="0x20"):
         d.compact()
+
+
+def test_tensors_that_require_a_gradient_are_refused():
+    """Where gradients are recorded; under no_grad, or detached, the same tensors are taken."""
+    q, k, v = (torch.randn(20, 4, 64, device="cuda").to(torch.bfloat16) for _ in range(3))
+    off, n = _i32([0, 20]), _i32([20])
+    want = serve.attend_prompt(q, k, v, off, off, 0.1)
+    say("[case] gradients refused")
+    for name in "qkv":
+        x = dict(q=q, k=k, v=v)
+        x[name] = x[name].clone().requires_grad_()
+        with pytest.raises(B.CrError, match="no gradient"):
+            serve.attend_prompt(x["q"], x["k"], x["v"], off, off, 0.1)
+        with torch.no_grad():
+            assert torch.equal(serve.attend_prompt(x["q"], x["k"], x["v"], off, off, 0.1), want)
+    pool = serve.PagePool.empty(1, 4, 4, 8, 64)
+    table = _i32([[2, 0, 1]])
+    for x in ((k.clone().requires_grad_(), v), (k, v.clone().requires_grad_())):
+        with pytest.raises(B.CrError, match="no gradient"):
+            pool.append(0, *x, off, n, table)
+    pool.append(0, k, v, off, n, table)
+    args = (pool, 0, off, _i32([0, 1]), torch.empty((1, 0), dtype=torch.int32, device="cuda"), _i32([0]), table, n, 0.1)
+    with pytest.raises(B.CrError, match="no gradient"):
+        serve.attend_shared(q.clone().requires_grad_(), *args)
+    with torch.inference_mode():
+        assert (serve.attend_shared(q, *args).float() - want.float()).abs().max() <= 2 * so.UNIT[q.dtype] * want.float().abs().max()
+    pool.k.requires_grad_()
+    with pytest.raises(B.CrError, match="no gradient"):
+        serve.attend_shared(q, *args)

@@ -34,3 +34,15 @@ def test_join_of_more_rows_than_a_launch_takes(L):  # noqa: F811
         assert _attend_shared(L, **few, batch=batch, groups=batch, total_q=n) == B.CR_EINVAL
     n = (1 << 24) - 1
     assert _attend_shared(L, 64, **few, batch=n, groups=n, total_q=n) == B.CR_ESIZE
+
+
+def test_prompt_attention_has_no_gradient():
+    from paper_2608_19677_amd import serve
+    q, off = torch.zeros(3, 4, 64, dtype=torch.bfloat16), torch.tensor([0, 3], dtype=torch.int32)
+    for i in range(3):
+        x = [q, q, q]
+        x[i] = q.clone().requires_grad_()
+        with pytest.raises(B.CrError, match="no gradient"):
+            serve.attend_prompt(*x, off, off, 1.0)
+        with torch.no_grad(), pytest.raises(B.CrError, match="device tensors"):
+            serve.attend_prompt(*x, off, off, 1.0)
