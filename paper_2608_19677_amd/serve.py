@@ -31,6 +31,7 @@ from . import binding as B
 _DTYPES = {torch.bfloat16: B.CR_BF16, torch.float16: B.CR_F16}
 _INT32, _FLOAT32 = torch.int32, torch.float32
 _HERE = contextlib.nullcontext()
+_raw_stream, _device = B._raw_stream, B._device
 _pack_rows, _pack_prompt, _pack_shared, _RANGE = B.ROWS.pack, B.PROMPT_ARGS.pack, B.SHARED_ARGS.pack, (struct.error, OverflowError)
 
 
@@ -107,13 +108,17 @@ class _Memory:
 
     def _on(self, stream) -> Optional[int]:
         """Handle of the stream of a call: ``stream``, or the current one."""
-        handle = B._stream(stream)
-        if handle not in self._seen and not torch.cuda.is_current_stream_capturing():
+        handle = _raw_stream(_device()) if stream is None and _raw_stream else B._stream(stream)
+        if handle not in self._seen:
+            self._see(handle, stream)
+        return handle
+
+    def _see(self, handle, stream):
+        if not torch.cuda.is_current_stream_capturing():
             s = torch.cuda.current_stream() if stream is None else stream
             for t in self._memory:
                 t.record_stream(s)
             self._seen.add(handle)
-        return handle
 
 
 class Workspace(_Memory):
@@ -302,6 +307,8 @@ def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table,
     if ws is None:
         with _taken_on(stream):
             ws = shared_workspace(q, pool, group_off, prefix_table, own_table)
-    pool._on(stream)
-    B._check(B.load().cr_attn_shared(pool._ref, a, *ws.args, ws._on(stream)), "cr_attn_shared")
+    handle = pool._on(stream)
+    if handle not in ws._seen:
+        ws._see(handle, stream)
+    B._check(B.load().cr_attn_shared(pool._ref, a, *ws.args, handle), "cr_attn_shared")
     return out
