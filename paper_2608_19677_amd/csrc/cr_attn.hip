@@ -100,7 +100,6 @@ struct Attn {
     // `slots` + i.
     uint32_t chunk, slots, own_chunk, own_slots;
     uint32_t least_share;  // narrow kernel: tiles a block takes at least, so that no sequence needs more slots
-    uint32_t first;        // kind of the first slots (the others are kOwn's)
     float* part_o;         // f32 [slots + own_slots][total_q * heads_q][dim], NULL: results are final
     float* part_lse;       // f32 [slots + own_slots][total_q * heads_q], base 2
     uint32_t* err;
@@ -1104,7 +1103,7 @@ struct Wide {
 struct Shape {
     Wide wide[2];
     uint32_t wides, lists;  // lists of the narrow launch: 1 the first kind's, 2 own tokens
-    uint32_t first, chunk, slots, own_chunk, own_slots;
+    uint32_t chunk, slots, own_chunk, own_slots;
     uint32_t least;                                        // share of a narrow block, in tiles
     uint64_t blocks;                                       // of the narrow launch, per key head
     bool join;
@@ -1219,7 +1218,6 @@ inline bool good_shared_sizes(const cr_kv_cache* c, const cr_attn_shared_args* p
 inline Shape prompt_shape(const cr_attn_prompt_args* p)
 {
     Shape s{};
-    s.first = kPrompt;
     const uint64_t rows = (uint64_t)p->total_q * (p->heads_q / p->heads_kv), keys = p->total_k / p->batch;
     if (rows <= (uint64_t)kFewRows * p->batch && narrow_fits(rows, p->batch, p->total_k)) {
         s.lists = 1;
@@ -1253,12 +1251,10 @@ inline Shape shared_shape(const cr_kv_cache* c, const cr_attn_shared_args* p)
     const uint64_t rows = (uint64_t)p->total_q * (p->heads_q / c->heads);
     const uint64_t prefix = (uint64_t)p->prefix_width * c->page_tokens, own = (uint64_t)p->own_width * c->page_tokens;
     if (rows >= (uint64_t)kWholeRows * p->batch) {
-        s.first = kWhole;
         s.wide[s.wides++] = wide_shape(kWhole, rows, p->batch, c->heads, prefix + own, c->dim, &s.chunk, &s.slots);
         s.join = s.slots > 1;
         return s;
     }
-    s.first = kGroup;
     s.join = true;
     uint64_t units = 0, wides = 0;
     if (rows <= (uint64_t)kFewRows * p->groups && narrow_fits(rows, p->groups, prefix)) {
@@ -1337,7 +1333,6 @@ cr_status dispatch(Attn& a, const Shape& s, void* ws, uint32_t dtype, uint32_t d
         if ((rows / s.wide[i].rows + a.batch) * (s.wide[i].kind == kOwn ? s.own_slots : s.slots) * a.heads_kv >= (1ull << 32) / (8u * kWave))
             return CR_EINVAL;
     if (s.join && a.total_q >= (1ull << 32) / kThreads) return CR_EINVAL;  // a block of the join per token
-    a.first = s.first;
     a.chunk = s.chunk;
     a.slots = s.slots;
     a.own_chunk = s.own_chunk;
