@@ -476,7 +476,8 @@ cr_status cr_pages_free(const cr_kv_cache* c, const uint32_t* table, uint32_t wi
  * renamed into table_out (the same shape), the others copied; refs_out u32 [num_pages]
  * receives the counts (table_out and refs_out may be table and c->refs). Pages that moved
  * away keep their old contents. Several tables: rename them in one call by giving them as one
- * array, or call with rows = 0 last. A length beyond the width sets CR_ERR_SEQ (the row is
+ * array, or in one call each with refs_out other than c->refs, and then call with rows = 0 and
+ * refs_out = c->refs (as long as the counts are the old ones every call makes the same moves). A length beyond the width sets CR_ERR_SEQ (the row is
  * copied); an entry out of range or naming a free page sets CR_ERR_PAGE and is copied. */
 cr_status cr_pages_compact(const cr_kv_cache* c, const uint32_t* table, const uint32_t* length, uint32_t rows,
                            uint32_t width, uint32_t* table_out, uint32_t* refs_out, void* ws, size_t ws_bytes,

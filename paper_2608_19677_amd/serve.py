@@ -201,7 +201,8 @@ class PagePool(_Memory):
 
     def compact(self, table, length, table_out=None, refs_out=None, stream=None):
         """Moves the live pages to the front and renames the table's entries (in place, if no
-        other place is given)."""
+        other place is given). Of several tables, each but the last call's gives ``refs_out``
+        another place; the last may be None."""
         refs = _index(self.refs if refs_out is None else refs_out, self.num_pages)
         p = lengths = out = None
         rows = width = 0

@@ -218,3 +218,26 @@ def test_a_fork_in_a_graph():
         pool.extend(other, None, _i32([9]))
         pool.free(other, _i32([9]))
     assert _err(pool) == 0
+
+
+@pytest.mark.parametrize("pages", [60, PAGES])
+def test_several_tables_are_compacted_one_after_the_other(pages):
+    """One call per table with the counts put elsewhere, the last (without a table) puts them in place."""
+    pool = _pool(pages)
+    live = [pages - 1, 3, pages - 7, 20, pages - 2]
+    pool.refs[live] = _i32([1, 2, 1, 1, 1])
+    ref = so.Pages(pool.refs.tolist(), 4)
+    tables, lengths = [_i32([live[:2]]), _i32([live[2:], live[1:4]])], [[8], [9, 3]]
+    want = []
+    for t, n in zip(tables, lengths):
+        want.append(so.Pages(ref.refs, 4).compact(t.tolist(), n)[0])
+    k = pool.k.clone()
+    _, moves = ref.compact([], [])
+    for s, d in moves:
+        k[:, d] = k[:, s]
+    say(f"[case] two tables, {pages} pages")
+    aside = torch.empty_like(pool.refs)
+    for t, n in zip(tables, lengths):
+        pool.compact(t, _i32(n), refs_out=aside)
+    pool.compact(None, None)
+    assert [t.tolist() for t in tables] == want and pool.refs.tolist() == ref.refs and torch.equal(pool.k, k) and _err(pool) == 0
