@@ -504,9 +504,8 @@ cr_status cr_kv_append(const cr_kv_cache* c, uint32_t layer, const cr_rows* k, c
  *   out_i = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  lse_i = m + ln sum_j exp(s_j - m),
  * m the largest s_j. causal = 1: row i sees keys j <= i + nk - nq (the last query sees all
  * keys, so nk > nq continues earlier context); causal = 0: all keys. A row that sees no key
- * gives out 0 and lse -inf. Keys and values of other sequences never reach a row, whatever
- * bits they hold; within a sequence a value that is not finite may reach earlier rows of up to
- * 127 tokens before its own. */
+ * gives out 0 and lse -inf. Keys and values that a row does not see never reach it, whatever
+ * bits they hold, those of its own sequence included. */
 typedef struct {
     uint32_t dtype, heads_q, heads_kv, dim; /* dim 64 or 128; heads_q a multiple of heads_kv */
     uint32_t batch, causal;

@@ -41,6 +41,8 @@ constexpr float kSlack = 8.f;            // weights may reach 2^kSlack before th
 
 struct Bf16 {
     static constexpr float kLift = 0.f;
+    static constexpr uint32_t kInf = 0x7F80u;
+    static __device__ __forceinline__ float wide(uint32_t x) { return __uint_as_float(x << 16); }  // of 16 bits
     static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -59,6 +61,8 @@ struct Bf16 {
 // of it at least; around 1 those below 2^-24 would be lost, and many of them may add up.
 struct F16 {
     static constexpr float kLift = 6.f;
+    static constexpr uint32_t kInf = 0x7C00u;
+    static __device__ __forceinline__ float wide(uint32_t x) { return (float)__builtin_bit_cast(_Float16, (uint16_t)x); }
     static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -336,6 +340,125 @@ struct Loader {
     }
 };
 
+// Values that are not finite. A weight of 0 times such a value is not 0, so the products of a half tile that some
+// rows see in part carry it to rows that do not see it. Sums that are not finite show that it may have happened; the wave
+// then looks at the values from its first row's end on, and if there is one among them does its products once more,
+// straight from memory, with 0 in its place, and adds it to the rows that see it. Where all is finite that is the look at
+// the sums and a few registers: 24 prompts of about 300 tokens 39.9 -> 40.5 us, a decode step behind one prefix 35.1 -> 35.7,
+// long prompts within 0.5 %. (Checked on their way to LDS, the values of such tiles took 10 % of the short prompts.)
+template <int kDim>
+__device__ __forceinline__ bool all_finite(const f32x16 (&o)[kDim / 32])
+{
+    float top = 0.f;
+#pragma unroll
+    for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2)
+            top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top, __builtin_fabsf(o[d][i])), __builtin_fabsf(o[d][i + 1]));
+    return ballot(!(top < INFINITY)) == 0;
+}
+
+// The wave's rows are row .. last_row (repeated) of the sequence, its half tiles at first, first + step, ... below stop;
+// keys are read up to key_end, and all of its rows see `full` of them. The running maximum moves as it did in the first run,
+// so that all other sums come out the same, bit for bit.
+template <typename E, int kDim, bool kPaged>
+__device__ CR_INLINE void only_seen(const Attn& a, const Seq& it, uint32_t head_kv, uint32_t row, uint32_t last_row, uint32_t first, uint32_t step,
+                                    uint32_t stop, uint32_t key_end, uint32_t full, f32x16 (&o)[kDim / 32])
+{
+    uint32_t lane = lane_id();
+    stay(lane);  // what follows from it is computed again, not kept over the loop before
+    const uint32_t half = lane >> 5, col = lane & 31u, m = min(row + col, last_row);
+    const int32_t lim = (int32_t)min(row_limit(a, it, m), key_end);
+    const uint16_t* qp = (const uint16_t*)a.q.p + (int64_t)(it.tok0 + m / a.group) * a.q.token_stride +
+                         (int64_t)(head_kv * a.group + m % a.group) * a.q.head_stride;
+    // Row r of the half tile at k0, the last one repeated: its place in k or v.
+    auto at = [&](const uint16_t* k_or_v, const cr_rows& rows, uint32_t k0, uint32_t r) CR_INLINE {
+        uint32_t j = k0, last = key_end;
+        if (kPaged) {
+            const uint32_t* table = Loader<kDim, true, 32, kWave>::place(it, k0, key_end, &j, &last);
+            j = min(j + r, last - 1u);
+            const uint32_t g = min(table[j >> a.pg.log_tokens], a.pg.num_pages - 1u), mask = (1u << a.pg.log_tokens) - 1u;
+            return k_or_v + (int64_t)head_kv * a.pg.head_stride + (int64_t)g * a.pg.page_stride + (int64_t)(j & mask) * a.pg.token_stride;
+        }
+        return (const uint16_t*)rows.p + (int64_t)head_kv * rows.head_stride + ((int64_t)it.key0 + min(j + r, last - 1u)) * rows.token_stride;
+    };
+    auto not_finite = [&](uint32_t x) CR_INLINE { return (x & 0x7FFFu) >= E::kInf; };
+    const uint32_t part = first + (full >= first + 32u ? (full - first - 32u) / step + 1u : 0u) * step;  // the first half tile seen in part
+    bool any = false;
+    for (uint32_t k0 = part; k0 < key_end; k0 += step) {
+        const uint16_t* v = at(a.pg.v, a.v, k0, col);
+        for (uint32_t e = half * 8u; e < kDim; e += 16u) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(v + e);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) any |= not_finite(x[y]) || not_finite(x[y] >> 16);
+        }
+    }
+    if (__builtin_expect(!ballot(any), 1)) return;
+
+    float mc = kNoMax;
+#pragma unroll
+    for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    for (uint32_t k0 = first; k0 < stop; k0 += step) {
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        const uint16_t* k = at(a.pg.k, a.k, k0, col);
+#pragma unroll
+        for (int d = 0; d < kDim / 16; ++d)
+            s = E::mfma(*reinterpret_cast<const s16x8*>(k + d * 16 + half * 8u), *reinterpret_cast<const s16x8*>(qp + d * 16 + half * 8u), s);
+        const int32_t l = kPaged && k0 < it.gap_end ? min(lim, (int32_t)it.len0) : lim;
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if ((int32_t)(k0 + 8u * (i / 4) + 4u * half + (i & 3)) >= l) s[i] = -INFINITY;
+            top = __builtin_elementwise_maximum(top, s[i]);
+        }
+        top = both_max(top) * a.c;
+        if (ballot(top > mc + (kSlack + E::kLift))) {
+            const float up = fmaxf(mc, top - E::kLift), f = __builtin_amdgcn_exp2f(mc - up);
+            mc = up;
+#pragma unroll
+            for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        }
+        uint32_t pk[8];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2)
+            pk[i / 2] = E::pack(__builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c, -mc)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], a.c, -mc)));
+        const bool in_part = k0 >= part;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const u32x4 w = {pk[ks * 4], pk[ks * 4 + 1], pk[ks * 4 + 2], pk[ks * 4 + 3]};
+            s16x8 vf[kDim / 32];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+                const uint16_t* v = at(a.pg.v, a.v, k0, ks * 16u + (y / 4) * 8u + half * 4u + (y & 3)) + col;
+#pragma unroll
+                for (int d = 0; d < kDim / 32; ++d) {
+                    const uint16_t x = v[d * 32];
+                    vf[d][y] = (short)(in_part && not_finite(x) ? 0u : x);
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < kDim / 32; ++d) o[d] = E::mfma(vf[d], __builtin_bit_cast(s16x8, w), o[d]);
+        }
+    }
+    for (uint32_t k0 = part; k0 < stop; k0 += step)
+        for (uint32_t r = 0; r < 32u && (int32_t)(k0 + r) < lim; ++r) {
+            const uint16_t* v = at(a.pg.v, a.v, k0, r);
+#pragma unroll
+            for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t x = v[d * 32 + 8 * (i / 4) + 4u * half + (i & 3)];
+                    if (not_finite(x)) o[d][i] += E::wide(x);
+                }
+        }
+}
+
 // A wavefront keeps 32 rows, each in one column: S^T = K Q^T gives a lane its row's scores of 16 of 32
 // keys (the other half-wave has the other 16), so the row's maximum needs one exchange, and the
 // weights are the second operand of O^T = V^T P^T as they lie: the order of keys inside a
@@ -546,9 +669,9 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
             const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i + 1], a.c, -mc));
             part[0] = i ? part[0] + x : x;
             part[1] = i ? part[1] + y : y;
+            if (i) part_rounded = E::add(pk[h][i / 2 - 1], i > 2 ? part_rounded : 0.f);  // of the pair before: packed some cycles ago
             pk[h][i / 2] = E::pack(x, y);
             stay(pk[h][i / 2]);
-            part_rounded = E::add(pk[h][i / 2], i ? part_rounded : 0.f);
         };
         auto value = [&](s16x8 vf, int h, int n) CR_INLINE {
             const int ks = n / (kDim / 32), d = n % (kDim / 32);
@@ -594,7 +717,7 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
                 __builtin_amdgcn_sched_barrier(0);
             }
             sum += part[0] + part[1];
-            rounded += part_rounded;
+            rounded += E::add(pk[h ^ 1][7], part_rounded);
             stay(sum);
             stay(rounded);
             move_maximum();
@@ -652,6 +775,8 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
         ld.report(a);
     }
 
+    if (__builtin_expect(w_full < key_end && !all_finite<kDim>(o), 0))
+        only_seen<E, kDim, kPaged>(a, it, head_kv, row0 + wrow, row0 + rows - 1u, key_begin, 32u, w_end, key_end, w_full, o);
     const float total = both_sum(sum), total_rounded = both_sum(rounded);
     if (wrow + col >= rows) return;
     const bool none = total == 0.f;  // the largest weight of a row that sees a key is 2^kLift or more
@@ -671,12 +796,6 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
         return;
     }
     if (a.lse && half == 0) a.lse[orow] = lse2 * kLn2;
-    if (none) {  // weights of 0 times values that are not finite
-#pragma unroll
-        for (int d = 0; d < kDim / 32; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    }
     uint16_t* op = (uint16_t*)a.out.p + (int64_t)tok * a.out.token_stride + (int64_t)head * a.out.head_stride;
 #pragma unroll
     for (int d = 0; d < kDim / 32; ++d)
@@ -897,7 +1016,8 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
         float mc = kNoMax, sum = 0.f, rounded = 0.f;
-        uint32_t k0 = st.key_begin + (pairs ? wv >> 1 : wv) * kNarrowKeys;
+        const uint32_t first_key = st.key_begin + (pairs ? wv >> 1 : wv) * kNarrowKeys;
+        uint32_t k0 = first_key;
         if (k0 < key_end && wave_row < rows) {
             Loader<kDim, kPaged, kNarrowKeys, kWave> ld;
             ld.bad = 0;
@@ -970,6 +1090,8 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             }
             ld.report(a);
         }
+        if (__builtin_expect(full < key_end && !all_finite<kDim>(o), 0))
+            only_seen<E, kDim, kPaged>(a, it, head_kv, row0 + wave_row, row0 + rows - 1u, first_key, key_step, key_end, key_end, full, o);
         sum = both_sum(sum);
         rounded = both_sum(rounded);
         if (half == 0) {
@@ -1000,7 +1122,6 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             }
             const bool none = total == 0.f;
             const float inv = none ? 0.f : 1.f / total_rounded, lse2 = none ? -INFINITY : mx + log2f(total);
-            if (none) acc = f32x4{0.f, 0.f, 0.f, 0.f};  // weights of 0 times values that are not finite
             const uint32_t ot = it.tok0 + mm / a.group, oh = head_kv * a.group + mm % a.group;
             const uint64_t orow = (uint64_t)ot * a.heads_q + oh;
             if (a.part_o) {
