@@ -444,8 +444,8 @@ size_t cr_pages_workspace_bytes(uint32_t num_pages, uint32_t n);
  * ceil(len_old[i] / page_tokens) <= j < ceil(len_new[i] / page_tokens) become free pages, the
  * lowest ids first in the order of (i, j), with refs 1. len_old, len_new u32 [n] (len_old
  * NULL: all 0); table u32 [n][width]. A sequence that shrinks or passes the table's width
- * sets CR_ERR_SEQ and takes none. n * width < 2^32 here and in cr_pages_free. Too few free pages set CR_ERR_PAGES_OUT, and then nothing
- * is changed. */
+ * sets CR_ERR_SEQ and takes none. n * width < 2^32 here and in cr_pages_free. Too few free pages
+ * set CR_ERR_PAGES_OUT, and then nothing is changed. */
 cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_old, const uint32_t* len_new, uint32_t n,
                           uint32_t* table, uint32_t width, void* ws, size_t ws_bytes, uint32_t* err, void* stream);
 
@@ -517,11 +517,14 @@ typedef struct {
     const uint32_t* k_off;                  /* u32 [batch + 1], 0 .. total_k                */
 } cr_attn_prompt_args;
 
-/* total_q * heads_q < 2^31, total_k < CR_MAX_KEYS (CR_EINVAL otherwise; so are calls of more workgroups than
- * a launch takes). Offsets that do not fit, or do not cover all rows, set CR_ERR_SEQ; the rows of such a
- * sequence, or of none, are then unspecified, and all rows where q_off (or group_off) is out of order. The workspace holds partial results where
- * the keys of a call with few rows are split over more workgroups; its size follows from the
- * args' scalars alone (pointers and strides are not read). */
+/* total_q * heads_q < 2^31, total_k < CR_MAX_KEYS (CR_EINVAL otherwise; so are calls of more
+ * workgroups than a launch takes). Offsets that do not fit, or do not cover all rows, set
+ * CR_ERR_SEQ; the rows of such a sequence, or of none, are then unspecified, and all rows where
+ * q_off (or group_off) is out of order. The workspace holds partial results where the keys of a
+ * call with few rows are split over more workgroups; its size follows from the args' scalars
+ * alone (pointers and strides are not read). A batch of few rows on many keys is not split well:
+ * the host knows total_k but not the longest sequence (64 queries, one a sequence, on 2,000 keys
+ * each of 8 key heads of 128: 664 us; through pages of their own 117). */
 size_t cr_attn_prompt_workspace_bytes(const cr_attn_prompt_args* a);
 cr_status cr_attn_prompt(const cr_attn_prompt_args* a, void* ws, size_t ws_bytes, uint32_t* err, void* stream);
 
@@ -530,8 +533,8 @@ cr_status cr_attn_prompt(const cr_attn_prompt_args* a, void* ws, size_t ws_bytes
  * r of own_table holds request r's own own_len[r] tokens behind the prefix, its q_off[r+1] -
  * q_off[r] query tokens being the last of them (already appended). Query t of nq sees the
  * whole prefix and own tokens j <= own_len - nq + t. A group's prefix is read once for all its
- * requests' queries and query heads; the results over prefix and own tokens are joined by
- * their log-sum-exp. Definitions of out, lse and empty rows as cr_attn_prompt. One query per
+ * requests' queries and query heads (where requests bring many rows each, once for each
+ * request); the results over prefix and own tokens are joined by their log-sum-exp. Definitions of out, lse and empty rows as cr_attn_prompt. One query per
  * request is a decode step, several are the suffix of a hit or drafted tokens. prefix_len and
  * own_len may be 0, and a table of width 0 may be NULL. */
 typedef struct {
@@ -549,8 +552,12 @@ typedef struct {
     const uint32_t* own_len;                /* u32 [batch]                                  */
 } cr_attn_shared_args;
 
-/* Errors as cr_attn_prompt; groups that do not cover all requests and lengths beyond a table's width
- * set CR_ERR_SEQ, pages out of range CR_ERR_PAGE. The workspace size follows from the scalars of the cache and the args. */
+/* Errors as cr_attn_prompt; groups that do not cover all requests and lengths beyond a table's
+ * width set CR_ERR_SEQ, pages out of range CR_ERR_PAGE. The workspace size follows from the
+ * scalars of the cache and the args. So do the chunks that keys are cut into: the tables' widths
+ * stand for the lengths, and tables much wider than their longest rows leave most of the GPU idle
+ * (64 requests on 50 to 400 tokens behind one prefix: attention takes 35 us with tables as wide as
+ * the lengths, 68 with tables for 4,096 tokens, 261 with tables for 32,768). */
 size_t cr_attn_shared_workspace_bytes(const cr_kv_cache* c, const cr_attn_shared_args* a);
 cr_status cr_attn_shared(const cr_kv_cache* c, const cr_attn_shared_args* a, void* ws, size_t ws_bytes, uint32_t* err,
                          void* stream);

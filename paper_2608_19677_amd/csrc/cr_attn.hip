@@ -475,7 +475,7 @@ __device__ CR_INLINE void only_seen(const Attn& a, const Seq& it, uint32_t head_
 // unit to itself (one barrier per tile), else two and a barrier more.
 //
 // Bound by the matrix and vector units: one prompt of 16,384 tokens (64 heads of 128 on 8 key heads) runs at 990 to
-// 1,050 TFLOP/s on different cards, matrix units 49 % busy, no LDS conflicts; a tile of 64 keys takes 256 rows
+// 1,050 TFLOP/s on different cards, matrix units 48 % busy, no LDS conflicts; a tile of 64 keys takes 256 rows
 // 2.1 us, a block's start and end about 6 us: eight prompts of 1,000 to 4,100 tokens 830 to 850 TFLOP/s.
 struct Part {
     uint32_t kind, tiles, blocks;  // blocks: tiles x slots x key heads

@@ -288,7 +288,9 @@ def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table,
     """Attention of requests in groups that share a cached prefix: requests group_off[g] ..
     group_off[g+1] see the prefix_len[g] tokens of prefix_table[g] and, causally, their own
     own_len[r] tokens of own_table[r], the last of which are the queries' (append them first).
-    q [total_q, heads_q, dim], request r's at q_off[r]..q_off[r+1]. Returns out."""
+    q [total_q, heads_q, dim], request r's at q_off[r]..q_off[r+1]. Returns out. Tables about as
+    wide as their longest row keep the GPU busy: the widths stand for the lengths, which only the
+    device knows."""
     shape = q.shape
     if q.dtype is not pool.k.dtype or len(shape) != 3 or shape[2] != pool.dim:
         raise B.CrError("q has the cache's type and dim")
