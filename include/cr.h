@@ -454,9 +454,9 @@ cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_old, const u
  * multiple of page_tokens the tokens behind them are copied, in every layer, into a page of
  * its own (refs 1; lowest free ids first in the order of children), so that both may go on
  * writing. Entries of child behind its pages become CR_NO_PAGE. parent, length u32 [n]; table
- * u32 [rows][width]; child u32 [n][child_width] (not `table` itself). A parent >= rows or a
- * length beyond either width sets CR_ERR_SEQ and that child gets no pages; an entry that is out of
- * range or names a free page sets CR_ERR_PAGE and becomes CR_NO_PAGE (a tail's is copied from
+ * u32 [rows][width]; child u32 [n][child_width] (not `table` itself, and no row of it that a
+ * parent names). A parent >= rows or a length beyond either width sets CR_ERR_SEQ and that child
+ * gets no pages; an entry that is out of range or names a free page sets CR_ERR_PAGE and becomes CR_NO_PAGE (a tail's is copied from
  * nowhere). CR_ERR_PAGES_OUT as cr_pages_extend, and then no page is taken or shared and all
  * children's entries are CR_NO_PAGE. n + ceil(num_pages / 4096) + 1 < 2^24 (CR_EINVAL otherwise: blocks of a
  * launch). */

@@ -241,3 +241,15 @@ def test_several_tables_are_compacted_one_after_the_other(pages):
         pool.compact(t, _i32(n), refs_out=aside)
     pool.compact(None, None)
     assert [t.tolist() for t in tables] == want and pool.refs.tolist() == ref.refs and torch.equal(pool.k, k) and _err(pool) == 0
+
+
+@pytest.mark.parametrize("pages", [60, PAGES])
+def test_children_in_rows_of_the_parents_table(pages):
+    """Rows that no parent names take children of the same table."""
+    pool = _pool(pages)
+    pool.refs[:3] = 1
+    table = _i32([[0, 1, 2], [-7] * 3, [-7] * 3])
+    say(f"[case] children beside their parent, {pages} pages")
+    pool.fork(table, _i32([0, 0]), _i32([9, 4]), table[1:])
+    assert _err(pool) == 0 and table.tolist() == [[0, 1, 2], [0, 1, 3], [0, -1, -1]]
+    assert pool.refs[:5].tolist() == [3, 2, 1, 1, 0]
