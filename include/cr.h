@@ -562,6 +562,106 @@ size_t cr_attn_shared_workspace_bytes(const cr_kv_cache* c, const cr_attn_shared
 cr_status cr_attn_shared(const cr_kv_cache* c, const cr_attn_shared_args* a, void* ws, size_t ws_bytes, uint32_t* err,
                          void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * The same cache held in 8 bits: twice the prefixes per GPU, half the bytes of every pass over
+ * them. Each element is an 8-bit float (CR_E4M3: three bits behind the point, values to 448;
+ * CR_E5M2: two, to 57,344) times the power of two of its block, a block being block_tokens
+ * tokens of one key head, keys and values apart:
+ *   x = c 2^e.
+ * New tokens of a block choose e as the smallest integer, -126 at least, with
+ *   max |x| <= 1.75 * 2^8 * 2^e   (CR_E4M3; 1.75 * 2^15 for CR_E5M2)
+ * over their finite elements, or the block's e where it has tokens from before and theirs is
+ * larger; c is x 2^-e rounded to the nearest, ties to even. Where e grows, the codes from before become
+ * c 2^(e_old - e), rounded likewise (only codes that fall below the smallest normal one lose
+ * anything). Finite elements beyond the largest one that both types have (1.875 * 2^127 for CR_BF16,
+ * 1.875 * 2^15 for CR_F16 with CR_E4M3; 1.75 instead of 1.875 with CR_E5M2) are held as that one. A value
+ * that is not finite is held as NaN with CR_E4M3 and as itself with CR_E5M2.
+ * Powers of two, so that a code stands for an element of 16 bits exactly (CR_F16: but for those below 2^-24).
+ * ------------------------------------------------------------------------------------- */
+#define CR_E4M3 0u
+#define CR_E5M2 1u
+#define CR_MAX_BLOCK_TOKENS 128 /* tokens per scale: a power of two up to this, at most a page */
+
+/* As cr_kv_cache but for the codes (k, v: 1 byte each, 16-byte aligned), whose strides count
+ * bytes (multiples of 16, not negative, below 2^31 but for layer_stride), and the scales: u8
+ * [layers][num_pages][heads][page_tokens / block_tokens][2], the block's e + 127 of the keys and of the
+ * values (at least 1; those of blocks without tokens may be anything). */
+typedef struct {
+    uint32_t dtype;        /* CR_BF16 or CR_F16: queries, new keys and values, outputs   */
+    uint32_t code;         /* CR_E4M3 or CR_E5M2                                         */
+    uint32_t heads;        /* key heads, 1..CR_MAX_HEADS                                 */
+    uint32_t dim;          /* 64 or 128                                                  */
+    uint32_t page_tokens;  /* power of two, 1..CR_MAX_PAGE_TOKENS                        */
+    uint32_t block_tokens; /* power of two, 1..min(page_tokens, CR_MAX_BLOCK_TOKENS)     */
+    uint32_t num_pages;    /* 1..CR_MAX_PAGES                                            */
+    uint32_t layers;       /* 1..CR_MAX_LAYERS                                           */
+    void* k;
+    void* v;
+    int64_t layer_stride, page_stride, head_stride, token_stride;
+    uint8_t* scale;        /* 2-byte aligned                                             */
+    uint32_t* refs;
+} cr_kvq_cache;
+
+/* cr_pages_extend, _fork, _free, _compact and _copy for this cache, the workspace and all else as there: contents
+ * are codes and scales. A fork's tail takes the scales of its blocks along. */
+cr_status cr_kvq_extend(const cr_kvq_cache* c, const uint32_t* len_old, const uint32_t* len_new, uint32_t n,
+                        uint32_t* table, uint32_t width, void* ws, size_t ws_bytes, uint32_t* err, void* stream);
+cr_status cr_kvq_fork(const cr_kvq_cache* c, const uint32_t* table, uint32_t rows, uint32_t width,
+                      const uint32_t* parent, const uint32_t* length, uint32_t n, uint32_t* child,
+                      uint32_t child_width, void* ws, size_t ws_bytes, uint32_t* err, void* stream);
+cr_status cr_kvq_free(const cr_kvq_cache* c, const uint32_t* table, uint32_t width, const uint32_t* length,
+                      uint32_t n, uint32_t* err, void* stream);
+cr_status cr_kvq_compact(const cr_kvq_cache* c, const uint32_t* table, const uint32_t* length, uint32_t rows,
+                         uint32_t width, uint32_t* table_out, uint32_t* refs_out, void* ws, size_t ws_bytes,
+                         uint32_t* err, void* stream);
+cr_status cr_kvq_copy(const cr_kvq_cache* c, const uint32_t* src, const uint32_t* dst, uint32_t n, uint32_t* err,
+                      void* stream);
+
+/* cr_kv_append for this cache: rows off[i]..off[i+1] of k and v (type c->dtype) are rounded into the last of the
+ * length[i] tokens of sequence i, with scales as above; tokens from before are those of the sequence's first
+ * length[i] - (off[i+1] - off[i]). Errors as there (offsets out of order set CR_ERR_SEQ, and any
+ * sequence may then be skipped); sequences must not name the same page for the tokens they write, nor one that
+ * another table's row goes on reading. */
+cr_status cr_kvq_append(const cr_kvq_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, uint32_t total,
+                        const uint32_t* off, const uint32_t* length, uint32_t n, const uint32_t* table, uint32_t width,
+                        uint32_t* err, void* stream);
+
+/* The reverse: the last off[i+1] - off[i] of sequence i's first length[i] tokens into rows off[i]..off[i+1] of k and
+ * v (type c->dtype, [total][heads][dim]). Either may be NULL. off, length, table and errors as
+ * cr_kvq_append; rows of tokens that are skipped stay as they are. */
+cr_status cr_kvq_read(const cr_kvq_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, uint32_t total,
+                      const uint32_t* off, const uint32_t* length, uint32_t n, const uint32_t* table, uint32_t width,
+                      uint32_t* err, void* stream);
+
+/* cr_attn_shared over this cache: keys and values are what the codes stand for, everything else is as
+ * there, the workspace included. */
+size_t cr_kvq_attn_workspace_bytes(const cr_kvq_cache* c, const cr_attn_shared_args* a);
+cr_status cr_kvq_attn(const cr_kvq_cache* c, const cr_attn_shared_args* a, void* ws, size_t ws_bytes, uint32_t* err,
+                      void* stream);
+
+/* Rotary positions of packed queries and keys: in the first `rotated` elements of every head, pair i of
+ * rotated / 2 turns by t = positions[token] * freq[i] / 2^64 turns (the product modulo 2^64: only its fraction
+ * counts, so that far positions lose nothing),
+ *   x1' = m (x1 cos 2 pi t - x2 sin 2 pi t), x2' = m (x2 cos 2 pi t + x1 sin 2 pi t),
+ * m = magnitude; the pair is elements i and i + rotated / 2 (CR_ROTARY_HALF) or 2 i and 2 i + 1
+ * (CR_ROTARY_PAIRS). Other elements are copied. Computed in fp32 and rounded once; cosines and sines are
+ * within 2^-22. Positions are i32; negative ones turn back. freq u64 [rotated / 2], 8-byte aligned: radians per position / (2 pi)
+ * * 2^64, rounded. q_out and k_out are q and k (same pointer and strides), or do not overlap any input.
+ * heads_k may be 0. total * (heads_q + heads_k) < 2^31. */
+#define CR_ROTARY_HALF 0u
+#define CR_ROTARY_PAIRS 1u
+
+typedef struct {
+    uint32_t dtype, heads_q, heads_k, dim; /* CR_BF16 or CR_F16; dim 64 or 128           */
+    uint32_t rotated, layout, total;       /* rotated: a multiple of 16, 16..dim         */
+    float magnitude;                       /* finite                                     */
+    cr_rows q, k, q_out, k_out;
+    const int32_t* positions;              /* i32 [total]                                */
+    const uint64_t* freq;
+} cr_rotary_args;
+
+cr_status cr_rotary(const cr_rotary_args* a, void* stream);
+
 /* Library version string. */
 const char* cr_version(void);
 

@@ -32,7 +32,8 @@ EXPORTS = ("cr_count_rates", "cr_count_slice_workspace_bytes", "cr_count_slice",
            "cr_lru_reset", "cr_replay", "cr_replay_partition", "cr_replay_lru", "cr_replay_set_group_min_records",
            "cr_pages_workspace_bytes", "cr_pages_extend", "cr_pages_fork", "cr_pages_free", "cr_pages_compact",
            "cr_pages_copy", "cr_kv_append", "cr_attn_prompt_workspace_bytes", "cr_attn_prompt",
-           "cr_attn_shared_workspace_bytes", "cr_attn_shared", "cr_version")
+           "cr_attn_shared_workspace_bytes", "cr_attn_shared", "cr_kvq_extend", "cr_kvq_fork", "cr_kvq_free", "cr_kvq_compact",
+           "cr_kvq_copy", "cr_kvq_append", "cr_kvq_read", "cr_kvq_attn_workspace_bytes", "cr_kvq_attn", "cr_rotary", "cr_version")
 CR_WINDOW_SUM = 0xFFFFFFFFFFFFFFFF
 CR_PLAN_BUFFERS = 16
 CR_GROUP_MULTI, CR_GROUP_COLD = 0xFFFE, 0xFFFF
@@ -59,6 +60,8 @@ class CrPlanSet(ctypes.Structure):
 
 
 CR_BF16, CR_F16 = 0, 1
+CR_E4M3, CR_E5M2, CR_MAX_BLOCK_TOKENS = 0, 1, 128
+CR_ROTARY_HALF, CR_ROTARY_PAIRS = 0, 1
 CR_NO_PAGE = 0xFFFFFFFF
 CR_ERR_SEQ, CR_ERR_PAGE, CR_ERR_PAGES_OUT = 16, 32, 64
 
@@ -88,11 +91,25 @@ class CrAttnSharedArgs(ctypes.Structure):
                 ("own_len", _P)]
 
 
-# The same three laid out in one step (a ctypes structure takes ten times as long to fill); the calls take either.
+class CrKvqCache(ctypes.Structure):
+    _fields_ = [("dtype", _u32), ("code", _u32), ("heads", _u32), ("dim", _u32), ("page_tokens", _u32), ("block_tokens", _u32),
+                ("num_pages", _u32), ("layers", _u32), ("k", _P), ("v", _P), ("layer_stride", _i64), ("page_stride", _i64),
+                ("head_stride", _i64), ("token_stride", _i64), ("scale", _P), ("refs", _P)]
+
+
+class CrRotaryArgs(ctypes.Structure):
+    _fields_ = [("dtype", _u32), ("heads_q", _u32), ("heads_k", _u32), ("dim", _u32), ("rotated", _u32), ("layout", _u32),
+                ("total", _u32), ("magnitude", _f32), ("q", CrRows), ("k", CrRows), ("q_out", CrRows), ("k_out", CrRows),
+                ("positions", _P), ("freq", _P)]
+
+
+# The arguments laid out in one step (a ctypes structure takes ten times as long to fill); the calls take either.
 ROWS = struct.Struct("@Pqq")
 PROMPT_ARGS = struct.Struct("@8If" + "Pqq" * 4 + "PPP")
 SHARED_ARGS = struct.Struct("@7If" + "Pqq" * 2 + "PPPPPPP")
-assert [x.size for x in (ROWS, PROMPT_ARGS, SHARED_ARGS)] == [ctypes.sizeof(x) for x in (CrRows, CrAttnPromptArgs, CrAttnSharedArgs)]
+ROTARY_ARGS = struct.Struct("@7If" + "Pqq" * 4 + "PP")
+assert [x.size for x in (ROWS, PROMPT_ARGS, SHARED_ARGS, ROTARY_ARGS)] == \
+    [ctypes.sizeof(x) for x in (CrRows, CrAttnPromptArgs, CrAttnSharedArgs, CrRotaryArgs)]
 
 
 class CrError(RuntimeError):
@@ -160,13 +177,21 @@ def load(path: Optional[str] = None):
     L.cr_attn_prompt.argtypes = [_P, _P, size, _P, _P]
     L.cr_attn_shared_workspace_bytes.argtypes = [cache, _P]
     L.cr_attn_shared.argtypes = [cache, _P, _P, size, _P, _P]
-    for f in ("cr_pages_workspace_bytes", "cr_attn_prompt_workspace_bytes", "cr_attn_shared_workspace_bytes"):
+    coded = ctypes.POINTER(CrKvqCache)
+    for f in ("extend", "fork", "free", "compact", "copy"):
+        getattr(L, "cr_kvq_" + f).argtypes = [coded] + getattr(L, "cr_pages_" + f).argtypes[1:]
+    L.cr_kvq_append.argtypes = L.cr_kvq_read.argtypes = [coded, _u32, _P, _P, _u32, _P, _P, _u32, _P, _u32, _P, _P]
+    L.cr_kvq_attn_workspace_bytes.argtypes = [coded, _P]
+    L.cr_kvq_attn.argtypes = [coded, _P, _P, size, _P, _P]
+    L.cr_rotary.argtypes = [_P, _P]
+    for f in ("cr_pages_workspace_bytes", "cr_attn_prompt_workspace_bytes", "cr_attn_shared_workspace_bytes", "cr_kvq_attn_workspace_bytes"):
         getattr(L, f).restype = size
     L.cr_version.restype = ctypes.c_char_p
     for f in ("cr_count_rates", "cr_count_slice", "cr_lru_reset", "cr_admit", "cr_admit_noalloc", "cr_place_lpt", "cr_place_hash", "cr_route", "cr_route_live", "cr_plan_churn",
               "cr_keymap_build", "cr_keymap_lookup", "cr_keymap_scatter", "cr_replay",
               "cr_replay_partition", "cr_replay_lru", "cr_pages_extend", "cr_pages_fork", "cr_pages_free",
-              "cr_pages_compact", "cr_pages_copy", "cr_kv_append", "cr_attn_prompt", "cr_attn_shared"):
+              "cr_pages_compact", "cr_pages_copy", "cr_kv_append", "cr_attn_prompt", "cr_attn_shared", "cr_kvq_extend",
+              "cr_kvq_fork", "cr_kvq_free", "cr_kvq_compact", "cr_kvq_copy", "cr_kvq_append", "cr_kvq_read", "cr_kvq_attn", "cr_rotary"):
         getattr(L, f).restype = ctypes.c_int32
     _lib = L
     return L
@@ -412,6 +437,58 @@ def cr_attn_shared_workspace_bytes(cache: CrKvCache, args: CrAttnSharedArgs) -> 
 def cr_attn_shared(cache: CrKvCache, args: CrAttnSharedArgs, ws, err, stream=None):
     _check(load().cr_attn_shared(ctypes.byref(cache), _ref(args), _ptr(ws), 0 if ws is None else _nbytes(ws),
                                  _ptr(err), _stream(stream)), "cr_attn_shared")
+
+
+def cr_kvq_extend(cache: CrKvqCache, len_old, len_new, table, ws, err, stream=None):
+    _check(load().cr_kvq_extend(ctypes.byref(cache), _ptr(len_old), _ptr(len_new), len_new.numel(), _ptr(table),
+                                _table_width(table), _ptr(ws), _nbytes(ws), _ptr(err), _stream(stream)), "cr_kvq_extend")
+
+
+def cr_kvq_fork(cache: CrKvqCache, table, parent, length, child, ws, err, stream=None):
+    _check(load().cr_kvq_fork(ctypes.byref(cache), _ptr(table), table.shape[0], _table_width(table), _ptr(parent),
+                              _ptr(length), parent.numel(), _ptr(child), _table_width(child), _ptr(ws), _nbytes(ws),
+                              _ptr(err), _stream(stream)), "cr_kvq_fork")
+
+
+def cr_kvq_free(cache: CrKvqCache, table, length, err, stream=None):
+    _check(load().cr_kvq_free(ctypes.byref(cache), _ptr(table), _table_width(table), _ptr(length), length.numel(), _ptr(err),
+                              _stream(stream)), "cr_kvq_free")
+
+
+def cr_kvq_compact(cache: CrKvqCache, table, length, table_out, refs_out, ws, err, stream=None):
+    """table, table_out: int32 [rows, width] (or None); length: int32 [rows]."""
+    rows = 0 if table is None else table.shape[0]
+    _check(load().cr_kvq_compact(ctypes.byref(cache), _ptr(table), _ptr(length), rows, _table_width(table),
+                                 _ptr(table_out), _ptr(refs_out), _ptr(ws), _nbytes(ws), _ptr(err), _stream(stream)),
+           "cr_kvq_compact")
+
+
+def cr_kvq_copy(cache: CrKvqCache, src, dst, err, stream=None):
+    _check(load().cr_kvq_copy(ctypes.byref(cache), _ptr(src), _ptr(dst), src.numel(), _ptr(err), _stream(stream)), "cr_kvq_copy")
+
+
+def cr_kvq_append(cache: CrKvqCache, layer: int, k: CrRows, v: CrRows, total: int, off, length, table, err, stream=None):
+    _check(load().cr_kvq_append(ctypes.byref(cache), layer, _ref(k), _ref(v), total, _ptr(off), _ptr(length), length.numel(),
+                                _ptr(table), _table_width(table), _ptr(err), _stream(stream)), "cr_kvq_append")
+
+
+def cr_kvq_read(cache: CrKvqCache, layer: int, k: Optional[CrRows], v: Optional[CrRows], total: int, off, length, table, err, stream=None):
+    _check(load().cr_kvq_read(ctypes.byref(cache), layer, None if k is None else _ref(k), None if v is None else _ref(v), total,
+                              _ptr(off), _ptr(length), length.numel(), _ptr(table), _table_width(table), _ptr(err),
+                              _stream(stream)), "cr_kvq_read")
+
+
+def cr_kvq_attn_workspace_bytes(cache: CrKvqCache, args: CrAttnSharedArgs) -> int:
+    return int(load().cr_kvq_attn_workspace_bytes(ctypes.byref(cache), _ref(args)))
+
+
+def cr_kvq_attn(cache: CrKvqCache, args: CrAttnSharedArgs, ws, err, stream=None):
+    _check(load().cr_kvq_attn(ctypes.byref(cache), _ref(args), _ptr(ws), 0 if ws is None else _nbytes(ws), _ptr(err),
+                              _stream(stream)), "cr_kvq_attn")
+
+
+def cr_rotary(args: CrRotaryArgs, stream=None):
+    _check(load().cr_rotary(_ref(args), _stream(stream)), "cr_rotary")
 
 
 class PlanSet:

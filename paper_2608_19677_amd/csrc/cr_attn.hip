@@ -1,5 +1,5 @@
 // Attention of a destination: whole prompts (packed, causal, grouped heads) and requests that share a
-// cached prefix in pages.
+// cached prefix in pages, of 16-bit elements or of 8-bit codes with scales.
 //
 // Mathematics: scores s_j = scale q.k_j, running maximum m and sum l of exp(s_j - m) over the keys
 // in one pass, o = sum_j exp(s_j - m) v_j / l, lse = m + ln l. Results over disjoint sets of keys
@@ -10,7 +10,7 @@
 // before that; what o is divided by is the sum of the rounded weights, so that a row that leans on
 // few keys keeps their values exactly (divided by l, the rounding of one large weight would scale the
 // whole row, up to 2^-8).
-#include "cr_kv.h"
+#include "cr_codes.h"
 
 #include <type_traits>
 
@@ -22,13 +22,9 @@ namespace {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr uint32_t kWaves = 4;
@@ -40,6 +36,7 @@ constexpr float kNoMax = -3.0e38f;       // running maximum before the first key
 constexpr float kSlack = 8.f;            // weights may reach 2^kSlack before the maximum is moved
 
 struct Bf16 {
+    typedef bf16x2 Pair;
     static constexpr float kLift = 0.f;
     static constexpr uint32_t kInf = 0x7F80u;
     static __device__ __forceinline__ float wide(uint32_t x) { return __uint_as_float(x << 16); }  // of 16 bits
@@ -60,6 +57,7 @@ struct Bf16 {
 // The largest weight lies between 2^kLift and 2^(kLift + kSlack), so that 16 bits hold weights down to 2^-30
 // of it at least; around 1 those below 2^-24 would be lost, and many of them may add up.
 struct F16 {
+    typedef f16x2 Pair;
     static constexpr float kLift = 6.f;
     static constexpr uint32_t kInf = 0x7C00u;
     static __device__ __forceinline__ float wide(uint32_t x) { return (float)__builtin_bit_cast(_Float16, (uint16_t)x); }
@@ -77,6 +75,32 @@ struct F16 {
     }
 };
 
+// How the keys and values lie in memory. Codes become 16-bit elements, their scale with them, on the way to LDS (a power of
+// two: exact), one conversion for two elements; everything behind that is the same.
+struct Held16 {
+    static constexpr bool kCoded = false;
+    typedef uint16_t Elem;
+    typedef u32x4 Eight;
+    template <typename E>
+    static __device__ __forceinline__ u32x4 wide(u32x4 x, float) { return x; }
+    template <typename E>
+    static __device__ __forceinline__ uint32_t one(uint16_t x, float) { return x; }
+};
+
+template <typename C>
+struct HeldCodes {
+    static constexpr bool kCoded = true;
+    typedef uint8_t Elem;
+    typedef u32x2 Eight;
+    template <typename E>
+    static __device__ __forceinline__ u32x4 wide(u32x2 x, float scale) { return wide_of<C, typename E::Pair>(x, scale); }
+    template <typename E>
+    static __device__ __forceinline__ uint32_t one(uint8_t x, float scale)
+    {
+        return __builtin_bit_cast(uint32_t, C::template wide<false>(x, scale, typename E::Pair{})) & 0xFFFFu;
+    }
+};
+
 // The stretches of keys a call works on.
 enum Kind : uint32_t {
     kPrompt,  // a sequence's keys
@@ -88,7 +112,9 @@ enum Kind : uint32_t {
 struct Attn {
     cr_rows q, k, v, out;  // k, v: prompt only
     float* lse;
-    KvPages pg;            // shared only, k and v at the call's layer
+    KvPages pg;            // shared only, k and v at the call's layer (codes: strides in bytes)
+    const uint16_t* scale; // codes: the layer's scales
+    uint32_t log_block;
     const uint32_t* q_off;
     const uint32_t* k_off;         // prompt
     const uint32_t* group_off;     // shared
@@ -233,29 +259,33 @@ __device__ __forceinline__ float both_sum(float x)
 
 // Tiles of kTile keys and values on their way from memory to LDS, moved by kMovers threads: each
 // moves one 16-byte piece of every kStep-th row.
-template <int kDim, bool kPaged, uint32_t kTile, uint32_t kMovers>
+template <typename E, typename S, int kDim, bool kPaged, uint32_t kTile, uint32_t kMovers>
 struct Loader {
+    typedef typename S::Elem Elem;
+    typedef typename S::Eight Eight;
     static constexpr uint32_t kPieces = kDim / 8, kStep = kMovers / kPieces, kPer = kTile / kStep;
     static constexpr uint32_t kWaveRows = kWave / kPieces;  // rows that a wavefront moves at once
     // Longest stride whose lane offsets, up to kWaveRows - 1 rows and a piece, stay in 32 bits.
     static constexpr uint32_t kLaneStride = (0xFFFFFFFFu - kDim) / (kWaveRows - 1u);
-    const uint16_t *kb, *vb;  // of the key head (prompt: at the sequence's first key)
-    uint32_t row, piece, end, lane_k, lane_v, bad;
+    const Elem *kb, *vb;      // of the key head (prompt: at the sequence's first key)
+    uint32_t row, piece, end, lane_k, lane_v, bad, head;
     uint32_t page[kPer];      // of the next tile's rows
-    u32x4 rk[kPer], rv[kPer];
+    Eight rk[kPer], rv[kPer];
+    uint32_t rs[kPer];        // codes: the rows' scales
 
     __device__ __forceinline__ void init(const Attn& a, const Seq& s, uint32_t head_kv, uint32_t last, uint32_t mover)
     {
         piece = mover % kPieces;
         row = mover / kPieces;
         end = last;
+        head = head_kv;
         if (kPaged) {
-            kb = a.pg.k + (int64_t)head_kv * a.pg.head_stride;
-            vb = a.pg.v + (int64_t)head_kv * a.pg.head_stride;
+            kb = (const Elem*)a.pg.k + (int64_t)head_kv * a.pg.head_stride;
+            vb = (const Elem*)a.pg.v + (int64_t)head_kv * a.pg.head_stride;
             lane_k = lane_v = row % kWaveRows * (uint32_t)a.pg.token_stride + piece * 8u;
         } else {
-            kb = (const uint16_t*)a.k.p + (int64_t)head_kv * a.k.head_stride + (int64_t)s.key0 * a.k.token_stride;
-            vb = (const uint16_t*)a.v.p + (int64_t)head_kv * a.v.head_stride + (int64_t)s.key0 * a.v.token_stride;
+            kb = (const Elem*)a.k.p + (int64_t)head_kv * a.k.head_stride + (int64_t)s.key0 * a.k.token_stride;
+            vb = (const Elem*)a.v.p + (int64_t)head_kv * a.v.head_stride + (int64_t)s.key0 * a.v.token_stride;
             lane_k = row % kWaveRows * (uint32_t)a.k.token_stride + piece * 8u;
             lane_v = row % kWaveRows * (uint32_t)a.v.token_stride + piece * 8u;
         }
@@ -303,8 +333,11 @@ struct Loader {
                     ak = (int64_t)((uint64_t)j * (uint32_t)a.k.token_stride);
                     av = (int64_t)((uint64_t)j * (uint32_t)a.v.token_stride);
                 }
-                rk[p] = *reinterpret_cast<const u32x4*>(kb + ak + lane_k);
-                rv[p] = *reinterpret_cast<const u32x4*>(vb + av + lane_v);
+                rk[p] = *reinterpret_cast<const Eight*>(kb + ak + lane_k);
+                rv[p] = *reinterpret_cast<const Eight*>(vb + av + lane_v);
+                if constexpr (S::kCoded)
+                    rs[p] = a.scale[scale_at(min(__builtin_amdgcn_readfirstlane(page[p]), a.pg.num_pages - 1u), a.pg.heads, head,
+                                             (j & mask) + row % kWaveRows, a.pg.log_tokens, a.log_block)];
             }
         } else {
 #pragma unroll
@@ -320,8 +353,10 @@ struct Loader {
                     ak = (int64_t)((uint64_t)j * (uint32_t)a.k.token_stride);
                     av = (int64_t)((uint64_t)j * (uint32_t)a.v.token_stride);
                 }
-                rk[p] = *reinterpret_cast<const u32x4*>(kb + ak + piece * 8u);
-                rv[p] = *reinterpret_cast<const u32x4*>(vb + av + piece * 8u);
+                rk[p] = *reinterpret_cast<const Eight*>(kb + ak + piece * 8u);
+                rv[p] = *reinterpret_cast<const Eight*>(vb + av + piece * 8u);
+                if constexpr (S::kCoded)
+                    rs[p] = a.scale[scale_at(min(page[p], a.pg.num_pages - 1u), a.pg.heads, head, j & mask, a.pg.log_tokens, a.log_block)];
             }
         }
     }
@@ -334,8 +369,9 @@ struct Loader {
 #pragma unroll
         for (uint32_t p = 0; p < kPer; ++p) {
             const uint32_t r = p * kStep + row;
-            *reinterpret_cast<u32x4*>(lk + piece * key_run(kTile) + r * 8u) = rk[p];
-            *reinterpret_cast<u32x4*>(lv + (piece >> 2) * val_run(kTile) + r * 32u + (piece & 3u) * 8u) = rv[p];
+            const float ks = S::kCoded ? scale_of(rs[p] & 0xFFu) : 0.f, vs = S::kCoded ? scale_of(rs[p] >> 8) : 0.f;
+            *reinterpret_cast<u32x4*>(lk + piece * key_run(kTile) + r * 8u) = S::template wide<E>(rk[p], ks);
+            *reinterpret_cast<u32x4*>(lv + (piece >> 2) * val_run(kTile) + r * 32u + (piece & 3u) * 8u) = S::template wide<E>(rv[p], vs);
         }
     }
 };
@@ -361,7 +397,7 @@ __device__ __forceinline__ bool all_finite(const f32x16 (&o)[kDim / 32])
 // The wave's rows are row .. last_row (repeated) of the sequence, its half tiles at first, first + step, ... below stop;
 // keys are read up to key_end, and all of its rows see `full` of them. The running maximum moves as it did in the first run,
 // so that all other sums come out the same, bit for bit.
-template <typename E, int kDim, bool kPaged>
+template <typename E, typename S, int kDim, bool kPaged>
 __device__ CR_INLINE void only_seen(const Attn& a, const Seq& it, uint32_t head_kv, uint32_t row, uint32_t last_row, uint32_t first, uint32_t step,
                                     uint32_t stop, uint32_t key_end, uint32_t full, f32x16 (&o)[kDim / 32])
 {
@@ -371,24 +407,32 @@ __device__ CR_INLINE void only_seen(const Attn& a, const Seq& it, uint32_t head_
     const int32_t lim = (int32_t)min(row_limit(a, it, m), key_end);
     const uint16_t* qp = (const uint16_t*)a.q.p + (int64_t)(it.tok0 + m / a.group) * a.q.token_stride +
                          (int64_t)(head_kv * a.group + m % a.group) * a.q.head_stride;
-    // Row r of the half tile at k0, the last one repeated: its place in k or v.
+    typedef typename S::Elem Elem;
+    typedef typename S::Eight Eight;
+    // Row r of the half tile at k0, the last one repeated: its place in k or v, and its scale there.
+    float scale = 0.f;
     auto at = [&](const uint16_t* k_or_v, const cr_rows& rows, uint32_t k0, uint32_t r) CR_INLINE {
         uint32_t j = k0, last = key_end;
         if (kPaged) {
-            const uint32_t* table = Loader<kDim, true, 32, kWave>::place(it, k0, key_end, &j, &last);
+            const uint32_t* table = Loader<E, S, kDim, true, 32, kWave>::place(it, k0, key_end, &j, &last);
             j = min(j + r, last - 1u);
             const uint32_t g = min(table[j >> a.pg.log_tokens], a.pg.num_pages - 1u), mask = (1u << a.pg.log_tokens) - 1u;
-            return k_or_v + (int64_t)head_kv * a.pg.head_stride + (int64_t)g * a.pg.page_stride + (int64_t)(j & mask) * a.pg.token_stride;
+            if constexpr (S::kCoded) {
+                const uint32_t two = a.scale[scale_at(g, a.pg.heads, head_kv, j & mask, a.pg.log_tokens, a.log_block)];
+                scale = scale_of(&rows == &a.k ? two & 0xFFu : two >> 8);
+            }
+            return (const Elem*)k_or_v + (int64_t)head_kv * a.pg.head_stride + (int64_t)g * a.pg.page_stride + (int64_t)(j & mask) * a.pg.token_stride;
         }
-        return (const uint16_t*)rows.p + (int64_t)head_kv * rows.head_stride + ((int64_t)it.key0 + min(j + r, last - 1u)) * rows.token_stride;
+        return (const Elem*)rows.p + (int64_t)head_kv * rows.head_stride + ((int64_t)it.key0 + min(j + r, last - 1u)) * rows.token_stride;
     };
+    auto eight = [&](const Elem* p) CR_INLINE { return S::template wide<E>(*reinterpret_cast<const Eight*>(p), scale); };
     auto not_finite = [&](uint32_t x) CR_INLINE { return (x & 0x7FFFu) >= E::kInf; };
     const uint32_t part = first + (full >= first + 32u ? (full - first - 32u) / step + 1u : 0u) * step;  // the first half tile seen in part
     bool any = false;
     for (uint32_t k0 = part; k0 < key_end; k0 += step) {
-        const uint16_t* v = at(a.pg.v, a.v, k0, col);
+        const Elem* v = at(a.pg.v, a.v, k0, col);
         for (uint32_t e = half * 8u; e < kDim; e += 16u) {
-            const u32x4 x = *reinterpret_cast<const u32x4*>(v + e);
+            const u32x4 x = eight(v + e);
 #pragma unroll
             for (int y = 0; y < 4; ++y) any |= not_finite(x[y]) || not_finite(x[y] >> 16);
         }
@@ -404,10 +448,10 @@ __device__ CR_INLINE void only_seen(const Attn& a, const Seq& it, uint32_t head_
         f32x16 s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
-        const uint16_t* k = at(a.pg.k, a.k, k0, col);
+        const Elem* k = at(a.pg.k, a.k, k0, col);
 #pragma unroll
         for (int d = 0; d < kDim / 16; ++d)
-            s = E::mfma(*reinterpret_cast<const s16x8*>(k + d * 16 + half * 8u), *reinterpret_cast<const s16x8*>(qp + d * 16 + half * 8u), s);
+            s = E::mfma(__builtin_bit_cast(s16x8, eight(k + d * 16 + half * 8u)), *reinterpret_cast<const s16x8*>(qp + d * 16 + half * 8u), s);
         const int32_t l = kPaged && k0 < it.gap_end ? min(lim, (int32_t)it.len0) : lim;
         float top = -INFINITY;
 #pragma unroll
@@ -435,10 +479,10 @@ __device__ CR_INLINE void only_seen(const Attn& a, const Seq& it, uint32_t head_
             s16x8 vf[kDim / 32];
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
-                const uint16_t* v = at(a.pg.v, a.v, k0, ks * 16u + (y / 4) * 8u + half * 4u + (y & 3)) + col;
+                const Elem* v = at(a.pg.v, a.v, k0, ks * 16u + (y / 4) * 8u + half * 4u + (y & 3)) + col;
 #pragma unroll
                 for (int d = 0; d < kDim / 32; ++d) {
-                    const uint16_t x = v[d * 32];
+                    const uint32_t x = S::template one<E>(v[d * 32], scale);
                     vf[d][y] = (short)(in_part && not_finite(x) ? 0u : x);
                 }
             }
@@ -448,12 +492,12 @@ __device__ CR_INLINE void only_seen(const Attn& a, const Seq& it, uint32_t head_
     }
     for (uint32_t k0 = part; k0 < stop; k0 += step)
         for (uint32_t r = 0; r < 32u && (int32_t)(k0 + r) < lim; ++r) {
-            const uint16_t* v = at(a.pg.v, a.v, k0, r);
+            const Elem* v = at(a.pg.v, a.v, k0, r);
 #pragma unroll
             for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const uint32_t x = v[d * 32 + 8 * (i / 4) + 4u * half + (i & 3)];
+                    const uint32_t x = S::template one<E>(v[d * 32 + 8 * (i / 4) + 4u * half + (i & 3)], scale);
                     if (not_finite(x)) o[d][i] += E::wide(x);
                 }
         }
@@ -543,7 +587,7 @@ constexpr uint32_t wide_lds(uint32_t waves, uint32_t dim)  // elements
     return 2u * key_tile(kKeys, dim) + val_bufs(waves) * val_tile(kKeys, dim);
 }
 
-template <typename E, int kDim, bool kPaged, uint32_t kW>
+template <typename E, typename S, int kDim, bool kPaged, uint32_t kW>
 __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_t block, uint16_t* lds)
 {
     constexpr uint32_t kRows = kW * 32u;  // of the block
@@ -597,7 +641,7 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
     if (key_begin < key_end) {
-        Loader<kDim, kPaged, kKeys, kW * kWave> ld;
+        Loader<E, S, kDim, kPaged, kKeys, kW * kWave> ld;
         ld.bad = 0;
         ld.init(a, it, head_kv, key_end, threadIdx.x);
         ld.pages(a, it, key_begin);
@@ -776,7 +820,7 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
     }
 
     if (__builtin_expect(w_full < key_end && !all_finite<kDim>(o), 0))
-        only_seen<E, kDim, kPaged>(a, it, head_kv, row0 + wrow, row0 + rows - 1u, key_begin, 32u, w_end, key_end, w_full, o);
+        only_seen<E, S, kDim, kPaged>(a, it, head_kv, row0 + wrow, row0 + rows - 1u, key_begin, 32u, w_end, key_end, w_full, o);
     const float total = both_sum(sum), total_rounded = both_sum(rounded);
     if (wrow + col >= rows) return;
     const bool none = total == 0.f;  // the largest weight of a row that sees a key is 2^kLift or more
@@ -805,11 +849,11 @@ __device__ CR_INLINE void wide_block(const Attn& a, const Part& part_of, uint32_
                 uint2{E::pack(o[d][i] * inv, o[d][i + 1] * inv), E::pack(o[d][i + 2] * inv, o[d][i + 3] * inv)};
 }
 
-template <typename E, int kDim, bool kPaged>
+template <typename E, typename S, int kDim, bool kPaged>
 __global__ __launch_bounds__(8 * kWave, 2) void k_attn_wide(const Attn a, const Part p)
 {
     __shared__ __align__(16) uint16_t lds[wide_lds(8, kDim)];
-    wide_block<E, kDim, kPaged, 8>(a, p, blockIdx.x, lds);
+    wide_block<E, S, kDim, kPaged, 8>(a, p, blockIdx.x, lds);
 }
 
 // Few rows: up to 64 at a time. The block's wavefronts take tiles of 32 keys in turn, each with tiles of
@@ -846,7 +890,7 @@ struct NarrowLds {
     float row_max[kWaves][32], row_sum[kWaves][32], row_rounded[kWaves][32];
 };
 
-template <typename E, int kDim, bool kPaged>
+template <typename E, typename S, int kDim, bool kPaged>
 __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t block, uint32_t blocks, uint16_t* lds, NarrowLds& sh)
 {
     constexpr uint32_t kKeyRun = key_run(kNarrowKeys), kValRun = val_run(kNarrowKeys), kSumRow = kDim + 4u;
@@ -1019,7 +1063,7 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
         const uint32_t first_key = st.key_begin + (pairs ? wv >> 1 : wv) * kNarrowKeys;
         uint32_t k0 = first_key;
         if (k0 < key_end && wave_row < rows) {
-            Loader<kDim, kPaged, kNarrowKeys, kWave> ld;
+            Loader<E, S, kDim, kPaged, kNarrowKeys, kWave> ld;
             ld.bad = 0;
             ld.init(a, it, head_kv, key_end, lane);
             ld.pages(a, it, k0);
@@ -1091,7 +1135,7 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
             ld.report(a);
         }
         if (__builtin_expect(full < key_end && !all_finite<kDim>(o), 0))
-            only_seen<E, kDim, kPaged>(a, it, head_kv, row0 + wave_row, row0 + rows - 1u, first_key, key_step, key_end, key_end, full, o);
+            only_seen<E, S, kDim, kPaged>(a, it, head_kv, row0 + wave_row, row0 + rows - 1u, first_key, key_step, key_end, key_end, full, o);
         sum = both_sum(sum);
         rounded = both_sum(rounded);
         if (half == 0) {
@@ -1146,7 +1190,7 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
 // so that neither waits for the other's last.
 constexpr uint32_t kMixedPerCu = 2;  // blocks that share a compute unit
 
-template <typename E, int kDim, bool kPaged>
+template <typename E, typename S, int kDim, bool kPaged>
 __global__ __launch_bounds__(kThreads, kMixedPerCu) void k_attn_mixed(const Attn a, const Part p0, const Part p1, uint32_t lists)
 {
     constexpr uint32_t kWide = wide_lds(kWaves, kDim), kNarrow = kWaves * narrow_lds<kDim>();
@@ -1155,9 +1199,9 @@ __global__ __launch_bounds__(kThreads, kMixedPerCu) void k_attn_mixed(const Attn
     const uint32_t wides = p0.blocks + p1.blocks;
     if (blockIdx.x < wides) {
         const bool second = blockIdx.x >= p0.blocks;
-        wide_block<E, kDim, kPaged, kWaves>(a, second ? p1 : p0, second ? blockIdx.x - p0.blocks : blockIdx.x, lds);
+        wide_block<E, S, kDim, kPaged, kWaves>(a, second ? p1 : p0, second ? blockIdx.x - p0.blocks : blockIdx.x, lds);
     } else {
-        narrow_block<E, kDim, kPaged>(a, lists, blockIdx.x - wides, gridDim.x - wides, lds, sh);
+        narrow_block<E, S, kDim, kPaged>(a, lists, blockIdx.x - wides, gridDim.x - wides, lds, sh);
     }
 }
 
@@ -1327,7 +1371,8 @@ inline bool good_prompt_sizes(const cr_attn_prompt_args* p)
            p->total_k < CR_MAX_KEYS && p->batch <= (1u << 24) && (p->batch > 0 || p->total_q == 0);
 }
 
-inline bool good_shared_sizes(const cr_kv_cache* c, const cr_attn_shared_args* p)
+template <typename C>
+bool good_shared_sizes(const C* c, const cr_attn_shared_args* p)
 {
     return good_cache_sizes(c) && p && good_heads(p->heads_q, c->heads) && p->layer < c->layers && good_scale(p->scale) &&
            (uint64_t)p->total_q * p->heads_q < (1ull << 31) && p->batch <= (1u << 24) && p->groups <= p->batch &&
@@ -1366,7 +1411,8 @@ inline Shape prompt_shape(const cr_attn_prompt_args* p)
 }
 
 // Here the tables' widths stand for the lengths.
-inline Shape shared_shape(const cr_kv_cache* c, const cr_attn_shared_args* p)
+template <typename C>
+Shape shared_shape(const C* c, const cr_attn_shared_args* p)
 {
     Shape s{};
     const uint64_t rows = (uint64_t)p->total_q * (p->heads_q / c->heads);
@@ -1417,7 +1463,7 @@ inline size_t part_bytes(const Shape& s, uint64_t rows, uint32_t dim)
     return s.join ? ((uint64_t)s.slots + s.own_slots) * rows * (dim + 1u) * sizeof(float) : 0;
 }
 
-template <typename E, int kDim, bool kPaged>
+template <typename E, typename S, int kDim, bool kPaged>
 void launch(const Attn& a, const Shape& s, hipStream_t st)
 {
     const uint64_t rows = (uint64_t)a.total_q * a.group;
@@ -1429,12 +1475,12 @@ void launch(const Attn& a, const Shape& s, hipStream_t st)
         Part p{w.kind, (uint32_t)(rows / w.rows) + seqs, 0, 0};
         p.blocks = p.tiles * (w.kind == kOwn ? a.own_slots : a.slots) * a.heads_kv;
         p.sorted = seqs > 1u && seqs <= kSortSeqs && p.blocks > (w.rows == 256u ? 1u : kMixedPerCu) * (uint32_t)device_cus();
-        if (w.rows == 256u) hipLaunchKernelGGL((k_attn_wide<E, kDim, kPaged>), dim3(p.blocks), dim3(8 * kWave), 0, st, a, p);
+        if (w.rows == 256u) hipLaunchKernelGGL((k_attn_wide<E, S, kDim, kPaged>), dim3(p.blocks), dim3(8 * kWave), 0, st, a, p);
         else few[fews++] = p;
     }
     uint32_t blocks = few[0].blocks + few[1].blocks;
     if (s.lists) blocks += (uint32_t)s.blocks * a.heads_kv;
-    if (blocks) hipLaunchKernelGGL((k_attn_mixed<E, kDim, kPaged>), dim3(blocks), dim3(kThreads), 0, st, a, few[0], few[1], s.lists);
+    if (blocks) hipLaunchKernelGGL((k_attn_mixed<E, S, kDim, kPaged>), dim3(blocks), dim3(kThreads), 0, st, a, few[0], few[1], s.lists);
     if (s.join) {
         constexpr uint32_t kPer = kDim / 4;
         if (s.slots + s.own_slots > 8u)
@@ -1444,7 +1490,7 @@ void launch(const Attn& a, const Shape& s, hipStream_t st)
     }
 }
 
-template <bool kPaged>
+template <typename S, bool kPaged>
 cr_status dispatch(Attn& a, const Shape& s, void* ws, uint32_t dtype, uint32_t dim, void* stream)
 {
     const hipStream_t st = as_stream(stream);
@@ -1464,11 +1510,72 @@ cr_status dispatch(Attn& a, const Shape& s, void* ws, uint32_t dtype, uint32_t d
         a.part_lse = a.part_o + ((uint64_t)s.slots + s.own_slots) * a.total_q * a.heads_q * dim;
     }
     (void)hipGetLastError();
-    if (dtype == CR_BF16 && dim == 128) launch<Bf16, 128, kPaged>(a, s, st);
-    else if (dtype == CR_BF16) launch<Bf16, 64, kPaged>(a, s, st);
-    else if (dim == 128) launch<F16, 128, kPaged>(a, s, st);
-    else launch<F16, 64, kPaged>(a, s, st);
+    if (dtype == CR_BF16 && dim == 128) launch<Bf16, S, 128, kPaged>(a, s, st);
+    else if (dtype == CR_BF16) launch<Bf16, S, 64, kPaged>(a, s, st);
+    else if (dim == 128) launch<F16, S, 128, kPaged>(a, s, st);
+    else launch<F16, S, 64, kPaged>(a, s, st);
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
+}
+
+cr_status shared_dispatch(const cr_kv_cache* c, uint32_t layer, Attn& a, const Shape& s, void* ws, void* stream)
+{
+    a.pg = kv_pages(c);
+    a.pg.k += (int64_t)layer * c->layer_stride;
+    a.pg.v += (int64_t)layer * c->layer_stride;
+    return dispatch<Held16, true>(a, s, ws, c->dtype, c->dim, stream);
+}
+
+cr_status shared_dispatch(const cr_kvq_cache* c, uint32_t layer, Attn& a, const Shape& s, void* ws, void* stream)
+{
+    const KvqPages p = kvq_pages(c, layer);
+    a.pg = KvPages{(const uint16_t*)p.k, (const uint16_t*)p.v, p.layer_stride, p.page_stride, p.head_stride,
+                   p.token_stride, p.heads, p.dim, p.log_tokens, p.num_pages, c->layers};
+    a.scale = p.scale;
+    a.log_block = p.log_block;
+    return c->code == CR_E4M3 ? dispatch<HeldCodes<E4m3>, true>(a, s, ws, c->dtype, c->dim, stream)
+                              : dispatch<HeldCodes<E5m2>, true>(a, s, ws, c->dtype, c->dim, stream);
+}
+
+template <typename C>
+size_t shared_bytes(const C* c, const cr_attn_shared_args* p)
+{
+    if (!good_shared_sizes(c, p) || p->total_q == 0) return 0;
+    return part_bytes(shared_shape(c, p), (uint64_t)p->total_q * p->heads_q, c->dim);
+}
+
+template <typename C>
+cr_status attend_shared(const C* c, const cr_attn_shared_args* p, void* ws, size_t ws_bytes, uint32_t* err, void* stream)
+{
+    if (!good_cache(c) || !good_shared_sizes(c, p) || !err) return CR_EINVAL;
+    if (p->total_q == 0) return CR_OK;
+    if (!good_rows(p->q) || !good_rows(p->out) || !p->q_off || !p->group_off || !p->prefix_len || !p->own_len ||
+        (p->prefix_width && !p->prefix_table) || (p->own_width && !p->own_table) || (p->lse && !aligned4(p->lse)))
+        return CR_EINVAL;
+    const Shape s = shared_shape(c, p);
+    const size_t need = part_bytes(s, (uint64_t)p->total_q * p->heads_q, c->dim);
+    if (need && (!ws || !aligned16(ws))) return CR_EINVAL;
+    if (ws_bytes < need) return CR_ESIZE;
+    Attn a{};
+    a.q = p->q;
+    a.out = p->out;
+    a.lse = p->lse;
+    a.q_off = p->q_off;
+    a.group_off = p->group_off;
+    a.prefix_table = p->prefix_table;
+    a.prefix_len = p->prefix_len;
+    a.own_table = p->own_table;
+    a.own_len = p->own_len;
+    a.prefix_width = p->prefix_width;
+    a.own_width = p->own_width;
+    a.heads_q = p->heads_q;
+    a.heads_kv = c->heads;
+    a.group = p->heads_q / c->heads;
+    a.batch = p->batch;
+    a.groups = p->groups;
+    a.total_q = p->total_q;
+    a.c = p->scale * kLog2e;
+    a.err = err;
+    return shared_dispatch(c, p->layer, a, s, ws, stream);
 }
 
 }  // namespace
@@ -1510,51 +1617,27 @@ extern "C" cr_status cr_attn_prompt(const cr_attn_prompt_args* p, void* ws, size
     a.causal = p->causal;
     a.c = p->scale * kLog2e;
     a.err = err;
-    return dispatch<false>(a, s, ws, p->dtype, p->dim, stream);
+    return dispatch<Held16, false>(a, s, ws, p->dtype, p->dim, stream);
 }
 
 extern "C" size_t cr_attn_shared_workspace_bytes(const cr_kv_cache* c, const cr_attn_shared_args* p)
 {
-    using namespace cr;
-    if (!good_shared_sizes(c, p) || p->total_q == 0) return 0;
-    return part_bytes(shared_shape(c, p), (uint64_t)p->total_q * p->heads_q, c->dim);
+    return cr::shared_bytes(c, p);
 }
 
 extern "C" cr_status cr_attn_shared(const cr_kv_cache* c, const cr_attn_shared_args* p, void* ws, size_t ws_bytes,
                                     uint32_t* err, void* stream)
 {
-    using namespace cr;
-    if (!good_cache(c) || !good_shared_sizes(c, p) || !err) return CR_EINVAL;
-    if (p->total_q == 0) return CR_OK;
-    if (!good_rows(p->q) || !good_rows(p->out) || !p->q_off || !p->group_off || !p->prefix_len || !p->own_len ||
-        (p->prefix_width && !p->prefix_table) || (p->own_width && !p->own_table) || (p->lse && !aligned4(p->lse)))
-        return CR_EINVAL;
-    const Shape s = shared_shape(c, p);
-    const size_t need = part_bytes(s, (uint64_t)p->total_q * p->heads_q, c->dim);
-    if (need && (!ws || !aligned16(ws))) return CR_EINVAL;
-    if (ws_bytes < need) return CR_ESIZE;
-    Attn a{};
-    a.q = p->q;
-    a.out = p->out;
-    a.lse = p->lse;
-    a.pg = kv_pages(c);
-    a.pg.k += (int64_t)p->layer * c->layer_stride;
-    a.pg.v += (int64_t)p->layer * c->layer_stride;
-    a.q_off = p->q_off;
-    a.group_off = p->group_off;
-    a.prefix_table = p->prefix_table;
-    a.prefix_len = p->prefix_len;
-    a.own_table = p->own_table;
-    a.own_len = p->own_len;
-    a.prefix_width = p->prefix_width;
-    a.own_width = p->own_width;
-    a.heads_q = p->heads_q;
-    a.heads_kv = c->heads;
-    a.group = p->heads_q / c->heads;
-    a.batch = p->batch;
-    a.groups = p->groups;
-    a.total_q = p->total_q;
-    a.c = p->scale * kLog2e;
-    a.err = err;
-    return dispatch<true>(a, s, ws, c->dtype, c->dim, stream);
+    return cr::attend_shared(c, p, ws, ws_bytes, err, stream);
+}
+
+extern "C" size_t cr_kvq_attn_workspace_bytes(const cr_kvq_cache* c, const cr_attn_shared_args* p)
+{
+    return cr::shared_bytes(c, p);
+}
+
+extern "C" cr_status cr_kvq_attn(const cr_kvq_cache* c, const cr_attn_shared_args* p, void* ws, size_t ws_bytes,
+                                 uint32_t* err, void* stream)
+{
+    return cr::attend_shared(c, p, ws, ws_bytes, err, stream);
 }

@@ -1,0 +1,325 @@
+// The cache held in 8 bits: new tokens rounded into it, and tokens read back.
+//
+// Mathematics: a block (block_tokens tokens of one head, keys or values) holds codes c of an 8-bit float and one exponent
+// e, x = c 2^e. e is the smallest integer with max |x| <= 1.75 * 2^kTop * 2^e (1.75 * 2^kTop is the largest code), or the e the block has from
+// before if that is larger; c = x 2^-e rounded to the nearest. The products with powers of two are exact, so each element is
+// rounded once. Exponents come from the bits of the largest magnitude, which is found among the elements' bits
+// as integers (magnitudes of floats are ordered like their bits).
+#include "cr_codes.h"
+
+#include <type_traits>
+
+namespace cr {
+namespace {
+
+constexpr uint32_t kQThreads = 256;
+constexpr uint32_t kQWaves = kQThreads / kWave;
+constexpr uint32_t kQBlocks = 1u << 20;  // of a launch; waves take more work in turn
+
+// Magnitude bits of the largest element that both types have: the largest exponent, all of the code's bits set.
+template <typename T, typename C>
+constexpr uint32_t most_bits()
+{
+    return T::kInf - (1u << (T::kBits - C::kBits));
+}
+
+// Stored exponent for a largest magnitude (its bits in the element type, at most most_bits()).
+template <typename T, typename C>
+__device__ __forceinline__ uint32_t exponent_of(uint32_t top)
+{
+    const uint32_t f = __float_as_uint(T::first(top));  // f16's small ones are normal floats
+    const int e = (int)(f >> 23) - C::kTop + ((f & 0x7FFFFFu) > 0x600000u ? 1 : 0);  // 1.75 = 1 + 0x600000 / 2^23
+    return (uint32_t)max(e, 1);
+}
+
+// The larger magnitudes of two pairs of elements.
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b)
+{
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+struct QCall {
+    KvqPages c;
+    uint8_t* scale;        // bytes of the layer's scales
+    cr_rows k, v;
+    const uint32_t* off;
+    const uint32_t* length;
+    const uint32_t* table;
+    uint32_t total, n, width;
+    uint32_t log_span;     // append: tokens of a wave's piece of work
+    uint64_t items;        // append: spans x heads x 2
+    uint32_t* err;
+};
+
+// Whether sequence x's rows and length fit; o0, o1, len are filled.
+__device__ __forceinline__ bool q_fits(const QCall& a, uint32_t x, uint32_t* o0, uint32_t* o1, uint32_t* len)
+{
+    *o0 = a.off[x];
+    *o1 = a.off[x + 1u];
+    *len = a.length[x];
+    return *o0 <= *o1 && *o1 <= a.total && *o1 - *o0 <= *len && pages_of(*len, a.c.log_tokens) <= a.width;
+}
+
+// Every sequence's offsets and length are looked at by the wave of its number.
+__device__ __forceinline__ void q_check(const QCall& a, uint64_t x)
+{
+    uint32_t o0, o1, len;
+    if (x >= a.n || lane_id() != 0) return;
+    if (!q_fits(a, (uint32_t)x, &o0, &o1, &len) || (x == 0 && o0 != 0u) || (x + 1u == a.n && o1 != a.total)) atomicOr(a.err, CR_ERR_SEQ);
+}
+
+// New tokens. A wave takes a span of one head's keys or values: a block, or as many blocks as its lanes hold rows of (4 rows of
+// 128 elements, 8 of 64; a lane has 8 elements of a row). Spans of sequence x start at floor(first row / span) + 2 x: n rows touch at most
+// floor(n / span) + 2 of them, so no pass counts them. The magnitudes' maximum goes over the lanes of a block; rows from
+// before that share a block are rounded again only where its exponent grows.
+template <typename T, typename C, int kDim>
+__device__ __forceinline__ void append_span(const QCall& a, uint8_t* ck, uint8_t* cv, uint64_t item)
+{
+    constexpr uint32_t kPieces = kDim / 8, kRows = kWave / kPieces;  // lanes of a row, rows of a wave
+    constexpr uint32_t kHold = 8;                                    // steps of rows held in registers
+    constexpr uint32_t kMostBits = most_bits<T, C>();
+    const uint32_t lane = lane_id(), piece = lane % kPieces, row = lane / kPieces;
+    const uint32_t bl = a.c.log_block, mask = (1u << a.c.log_tokens) - 1u;
+    const uint32_t plane = (uint32_t)(item & 1u), head = (uint32_t)((item >> 1) % a.c.heads);
+    const uint64_t u = (item >> 1) / a.c.heads;
+    auto start = [&](uint32_t x) { return (uint64_t)(a.off[x] >> a.log_span) + 2u * x; };
+    const uint32_t x = wave_find(a.n, u, start);
+    uint32_t o0, o1, len;
+    if (!q_fits(a, x, &o0, &o1, &len) || o0 == o1 || u < start(x)) return;
+    const uint32_t p0 = len - (o1 - o0);  // place of the first new token
+    const uint64_t s0 = ((p0 >> a.log_span) + (u - start(x))) << a.log_span;
+    if (s0 >= len) return;
+    // The lane's rows are pos, pos + kRows, ...: in one block, or there is one step. A span ends below 2^32.
+    const uint32_t pos = (uint32_t)s0 + row, block = pos >> bl << bl, steps = ((1u << a.log_span) + kRows - 1u) / kRows;
+    const cr_rows& rows = plane ? a.v : a.k;
+    const uint16_t* src = (const uint16_t*)rows.p + (int64_t)head * rows.head_stride + piece * 8u;
+    const uint32_t page = a.table[(uint64_t)x * a.width + (min(pos, len - 1u) >> a.c.log_tokens)];
+
+    u32x4 r[kHold];
+    auto is_new = [&](uint32_t step) { return step < steps && pos + step * kRows >= p0 && pos + step * kRows < len; };
+    auto load = [&](uint32_t step0) {  // 0 where there is no new token
+#pragma unroll
+        for (uint32_t y = 0; y < kHold; ++y) {
+            r[y] = u32x4{0, 0, 0, 0};
+            if (is_new(step0 + y))
+                r[y] = *reinterpret_cast<const u32x4*>(src + (int64_t)(o0 + (pos + (step0 + y) * kRows - p0)) * rows.token_stride);
+        }
+    };
+    uint32_t top = 0;  // largest magnitudes of the lane's pairs
+    auto magnitudes = [&](auto finite) {
+#pragma unroll
+        for (uint32_t y = 0; y < kHold; ++y)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t m = r[y][i] & 0x7FFF7FFFu;
+                if (finite) {
+                    if ((m & 0xFFFFu) >= T::kInf) m &= 0xFFFF0000u;
+                    if ((m >> 16) >= T::kInf) m &= 0xFFFFu;
+                }
+                top = max_pair(top, m);
+            }
+    };
+    for (uint32_t step0 = 0; step0 < steps; step0 += kHold) {
+        load(step0);
+        magnitudes(std::false_type{});
+    }
+    const bool beyond = ballot((top & 0xFFFFu) > kMostBits || (top >> 16) > kMostBits) != 0;
+    if (beyond) {  // an element that is not finite, or larger than any code's
+        top = 0;
+        for (uint32_t step0 = 0; step0 < steps; step0 += kHold) {
+            if (steps > kHold) load(step0);
+            magnitudes(std::true_type{});
+        }
+    }
+    top = min(max(top & 0xFFFFu, top >> 16), kMostBits);
+    for (uint32_t y = min((uint32_t)kWave, kPieces << bl) >> 1; y; y >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, (int)y));
+
+    if (block >= len || block + ((1u << bl) - 1u) < p0) return;  // no new token in the lane's block
+    if (page >= a.c.num_pages) {
+        atomicOr(a.err, CR_ERR_PAGE);
+        return;
+    }
+    uint8_t* scale = a.scale + 2u * scale_at(page, a.c.heads, head, block & mask, a.c.log_tokens, bl) + plane;
+    uint8_t* codes = (plane ? cv : ck) + (int64_t)head * a.c.head_stride + (int64_t)page * a.c.page_stride + piece * 8u;
+    auto at = [&](uint32_t p) { return reinterpret_cast<u32x2*>(codes + (int64_t)(p & mask) * a.c.token_stride); };
+    uint32_t e = exponent_of<T, C>(top);
+    if (block < p0) {  // tokens from before
+        const uint32_t e_old = *scale;
+        if (e > e_old) {
+            const float down = scale_of((uint32_t)max((int)(e_old + 127u) - (int)e, 1));  // 2^(e_old - e); below 2^-126 no code is left anyway
+            for (uint32_t p = pos; p < p0; p += kRows) {
+                u32x2 w = *at(p);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const f32x2 lo = C::template floats<false>(w[i]), hi = C::template floats<true>(w[i]);
+                    w[i] = C::template code<true>(hi[0] * down, hi[1] * down, C::template code<false>(lo[0] * down, lo[1] * down, 0u));
+                }
+                *at(p) = w;
+            }
+        }
+        e = max(e, e_old);
+    }
+    const float up = scale_of(254u - e);  // 2^-(e - 127); e is at most 247
+    for (uint32_t step0 = 0; step0 < steps; step0 += kHold) {
+        if (steps > kHold) load(step0);
+#pragma unroll
+        for (uint32_t y = 0; y < kHold; ++y) {
+            if (!is_new(step0 + y)) continue;
+            u32x2 out;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float z[4] = {T::first(r[y][2 * i]), T::second(r[y][2 * i]), T::first(r[y][2 * i + 1]), T::second(r[y][2 * i + 1])};
+                if (beyond) {
+                    const float most = T::first(kMostBits);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)
+                        if (__builtin_fabsf(z[w]) < INFINITY) z[w] = fminf(fmaxf(z[w], -most), most);
+                }
+                out[i] = C::template code<true>(z[2] * up, z[3] * up, C::template code<false>(z[0] * up, z[1] * up, 0u));
+            }
+            *at(pos + (step0 + y) * kRows) = out;
+        }
+    }
+    if (piece == 0 && pos == block) *scale = (uint8_t)e;
+}
+
+template <typename T, typename C, int kDim>
+__global__ __launch_bounds__(256) void k_kvq_append(QCall a, uint8_t* ck, uint8_t* cv)
+{
+    const uint64_t waves = (uint64_t)gridDim.x * kQWaves;
+    for (uint64_t item = (uint64_t)blockIdx.x * kQWaves + wave_in_block(); item < a.items; item += waves) {
+        q_check(a, item);
+        append_span<T, C, kDim>(a, ck, cv, item);
+    }
+}
+
+// Tokens read back: a wave takes a token's keys and values of all heads, a lane 8 elements of a head at a time.
+template <typename T, typename C, int kDim>
+__global__ __launch_bounds__(256) void k_kvq_read(QCall a)
+{
+    constexpr uint32_t kPieces = kDim / 8, kAhead = 4;
+    const uint32_t per = a.c.heads * kPieces, first = a.k.p ? 0u : per, last = a.v.p ? 2u * per : per;
+    const uint32_t mask = (1u << a.c.log_tokens) - 1u;
+    const uint32_t waves = gridDim.x * kQWaves, me = blockIdx.x * kQWaves + wave_in_block();
+    for (uint64_t y = me; y < max(a.total, a.n); y += waves) {
+        q_check(a, y);
+        if (y >= a.total) continue;
+        const uint32_t tok = (uint32_t)y;
+        const uint32_t x = wave_find(a.n, tok, [&](uint32_t z) { return a.off[z]; });
+        uint32_t o0, o1, len;
+        if (!q_fits(a, x, &o0, &o1, &len) || tok < o0 || tok >= o1) continue;
+        const uint32_t pos = len - (o1 - tok), page = a.table[(uint64_t)x * a.width + (pos >> a.c.log_tokens)];
+        if (page >= a.c.num_pages) {
+            if (lane_id() == 0) atomicOr(a.err, CR_ERR_PAGE);
+            continue;
+        }
+        const int64_t from = (int64_t)page * a.c.page_stride + (int64_t)(pos & mask) * a.c.token_stride;
+        for (uint32_t z0 = first; z0 < last; z0 += kAhead * kWave) {
+            u32x2 w[kAhead];
+            uint32_t e[kAhead];
+#pragma unroll
+            for (uint32_t i = 0; i < kAhead; ++i) {
+                const uint32_t z = z0 + i * kWave + lane_id(), p = z < per ? z : z - per, h = p / kPieces;
+                if (z >= last) continue;
+                w[i] = *reinterpret_cast<const u32x2*>((z < per ? a.c.k : a.c.v) + from + (int64_t)h * a.c.head_stride + p % kPieces * 8u);
+                const uint32_t two = a.c.scale[scale_at(page, a.c.heads, h, pos & mask, a.c.log_tokens, a.c.log_block)];
+                e[i] = z < per ? two & 0xFFu : two >> 8;
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < kAhead; ++i) {
+                const uint32_t z = z0 + i * kWave + lane_id(), p = z < per ? z : z - per, h = p / kPieces;
+                if (z >= last) continue;
+                const cr_rows& rows = z < per ? a.k : a.v;
+                uint16_t* to = (uint16_t*)rows.p + (int64_t)tok * rows.token_stride + (int64_t)h * rows.head_stride + p % kPieces * 8u;
+                *reinterpret_cast<u32x4*>(to) = wide_of<C, typename T::Pair>(w[i], scale_of(e[i]));
+            }
+        }
+    }
+}
+
+// What both calls check; rows of NULL are not looked at where `optional`. CR_OK with a.total 0: nothing to do.
+cr_status q_call(const cr_kvq_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, bool optional, uint32_t total, const uint32_t* off,
+                 const uint32_t* length, uint32_t n, const uint32_t* table, uint32_t width, uint32_t* err, QCall* a)
+{
+    if (!good_cache(c) || layer >= c->layers || !err || total >= (1u << 31) || n > (1u << 24) || width > (1u << 28)) return CR_EINVAL;
+    *a = QCall{};
+    if (total == 0) return CR_OK;
+    if (n == 0 || !off || !length || (width > 0 && !table)) return CR_EINVAL;
+    if ((!k && !optional) || (!v && !optional) || (k && !good_rows(*k)) || (v && !good_rows(*v))) return CR_EINVAL;
+    a->c = kvq_pages(c, layer);
+    a->scale = c->scale + 2u * (uint64_t)layer * scales_of_layer(c);
+    if (k) a->k = *k;
+    if (v) a->v = *v;
+    a->off = off;
+    a->length = length;
+    a->table = table;
+    a->total = total;
+    a->n = n;
+    a->width = width;
+    a->err = err;
+    return CR_OK;
+}
+
+template <typename T, typename C>
+void append_launch(const QCall& a, uint32_t blocks, hipStream_t st)
+{
+    uint8_t *k = const_cast<uint8_t*>(a.c.k), *v = const_cast<uint8_t*>(a.c.v);
+    if (a.c.dim == 128) hipLaunchKernelGGL((k_kvq_append<T, C, 128>), dim3(blocks), dim3(kQThreads), 0, st, a, k, v);
+    else hipLaunchKernelGGL((k_kvq_append<T, C, 64>), dim3(blocks), dim3(kQThreads), 0, st, a, k, v);
+}
+
+template <typename T, typename C>
+void read_launch(const QCall& a, uint32_t blocks, hipStream_t st)
+{
+    if (a.c.dim == 128) hipLaunchKernelGGL((k_kvq_read<T, C, 128>), dim3(blocks), dim3(kQThreads), 0, st, a);
+    else hipLaunchKernelGGL((k_kvq_read<T, C, 64>), dim3(blocks), dim3(kQThreads), 0, st, a);
+}
+
+inline uint32_t q_blocks(uint64_t waves)
+{
+    const uint64_t blocks = (waves + kQWaves - 1u) / kQWaves;
+    return (uint32_t)(blocks < kQBlocks ? blocks : kQBlocks);
+}
+
+}  // namespace
+}  // namespace cr
+
+extern "C" cr_status cr_kvq_append(const cr_kvq_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, uint32_t total,
+                                   const uint32_t* off, const uint32_t* length, uint32_t n, const uint32_t* table,
+                                   uint32_t width, uint32_t* err, void* stream)
+{
+    using namespace cr;
+    QCall a;
+    const cr_status rc = q_call(c, layer, k, v, false, total, off, length, n, table, width, err, &a);
+    if (rc != CR_OK || a.total == 0) return rc;
+    const uint32_t rows = kWave * 8u / c->dim;  // of a wave
+    a.log_span = log2_of(c->block_tokens > rows ? c->block_tokens : rows);
+    a.items = ((uint64_t)(total >> a.log_span) + 2u * (uint64_t)n) * c->heads * 2u;
+    const hipStream_t st = as_stream(stream);
+    const uint32_t blocks = q_blocks(a.items);
+    (void)hipGetLastError();
+    if (c->dtype == CR_BF16 && c->code == CR_E4M3) append_launch<Bf16Rows, E4m3>(a, blocks, st);
+    else if (c->dtype == CR_BF16) append_launch<Bf16Rows, E5m2>(a, blocks, st);
+    else if (c->code == CR_E4M3) append_launch<F16Rows, E4m3>(a, blocks, st);
+    else append_launch<F16Rows, E5m2>(a, blocks, st);
+    return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
+}
+
+extern "C" cr_status cr_kvq_read(const cr_kvq_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, uint32_t total,
+                                 const uint32_t* off, const uint32_t* length, uint32_t n, const uint32_t* table,
+                                 uint32_t width, uint32_t* err, void* stream)
+{
+    using namespace cr;
+    QCall a;
+    const cr_status rc = q_call(c, layer, k, v, true, total, off, length, n, table, width, err, &a);
+    if (rc != CR_OK || a.total == 0) return rc;
+    const hipStream_t st = as_stream(stream);
+    const uint32_t blocks = q_blocks(total > n ? total : n);
+    (void)hipGetLastError();
+    if (c->dtype == CR_BF16 && c->code == CR_E4M3) read_launch<Bf16Rows, E4m3>(a, blocks, st);
+    else if (c->dtype == CR_BF16) read_launch<Bf16Rows, E5m2>(a, blocks, st);
+    else if (c->code == CR_E4M3) read_launch<F16Rows, E4m3>(a, blocks, st);
+    else read_launch<F16Rows, E5m2>(a, blocks, st);
+    return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
+}

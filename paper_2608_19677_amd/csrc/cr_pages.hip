@@ -200,18 +200,44 @@ struct PgGeom {
     int64_t head_stride, token_stride;
 };
 
-inline PgGeom pg_geom(const cr_kv_cache* c)
+// Rows of `dim` elements of 2 bytes; codes go by pairs.
+inline PgGeom pg_geom(uint32_t heads, uint32_t page_tokens, uint32_t dim, int64_t head_stride, int64_t token_stride)
 {
     PgGeom g;
-    g.row16 = c->dim / 8u;
-    g.heads = c->heads;
-    g.log_tokens = log2_of(c->page_tokens);
-    g.page16 = (c->heads * g.row16) << g.log_tokens;
-    g.head_stride = c->head_stride;
-    g.token_stride = c->token_stride;
-    const int64_t d = c->dim, pt = c->page_tokens, h = c->heads;
-    g.whole = (c->token_stride == d && c->head_stride == d * pt) || (c->head_stride == d && c->token_stride == d * h);
+    g.row16 = dim / 8u;
+    g.heads = heads;
+    g.log_tokens = log2_of(page_tokens);
+    g.page16 = (heads * g.row16) << g.log_tokens;
+    g.head_stride = head_stride;
+    g.token_stride = token_stride;
+    const int64_t d = dim, pt = page_tokens, h = heads;
+    g.whole = (token_stride == d && head_stride == d * pt) || (head_stride == d && token_stride == d * h);
     return g;
+}
+
+// Where the pages' contents lie: keys and values, and the pairs of scales of a cache held in 8 bits.
+struct PgPlanes {
+    uint16_t* k;
+    uint16_t* v;
+    int64_t layer_stride, page_stride;
+    PgGeom g;
+    uint32_t planes;
+    uint32_t log_block, scale_page;  // tokens per scale; pairs per page and layer
+    uint16_t* scale;                 // NULL: 16-bit elements
+    uint64_t scale_layer;
+};
+
+inline PgPlanes pg_planes(const cr_kv_cache* c)
+{
+    return PgPlanes{(uint16_t*)c->k, (uint16_t*)c->v, c->layer_stride, c->page_stride,
+                    pg_geom(c->heads, c->page_tokens, c->dim, c->head_stride, c->token_stride), 2u * c->layers, 0, 0, nullptr, 0};
+}
+
+inline PgPlanes pg_planes(const cr_kvq_cache* c)
+{
+    return PgPlanes{(uint16_t*)c->k, (uint16_t*)c->v, c->layer_stride / 2, c->page_stride / 2,
+                    pg_geom(c->heads, c->page_tokens, c->dim / 2u, c->head_stride / 2, c->token_stride / 2), 2u * c->layers,
+                    log2_of(c->block_tokens), scales_of_page(c), (uint16_t*)c->scale, scales_of_layer(c)};
 }
 
 // Offset in elements of piece x of a page.
@@ -225,14 +251,6 @@ __device__ __forceinline__ int64_t pg_piece(const PgGeom& g, uint32_t x)
 // A fork's tail: the tokens behind a child's full pages in one plane (keys or values of a layer), copied from page
 // src to page dst by `movers` threads. Bound by memory: 192 children's tails of 32 layers (336 MB read, from cache where children
 // share a parent, and 336 MB written) take 110 us.
-struct PgPlanes {
-    uint16_t* k;
-    uint16_t* v;
-    int64_t layer_stride, page_stride;
-    PgGeom g;
-    uint32_t planes;
-};
-
 __device__ __forceinline__ void pg_copy_tail(const PgPlanes& c, uint32_t src, uint32_t dst, uint32_t tail, uint32_t plane, uint32_t mover,
                                              uint32_t movers)
 {
@@ -246,6 +264,13 @@ __device__ __forceinline__ void pg_copy_tail(const PgPlanes& c, uint32_t src, ui
         const int64_t at =
             (int64_t)head * g.head_stride + (int64_t)(r / g.row16) * g.token_stride + (int64_t)(r % g.row16) * 8;
         *reinterpret_cast<uint4*>(d + at) = *reinterpret_cast<const uint4*>(s + at);
+    }
+    if (!c.scale || (plane & 1u)) return;  // with the keys: the scales of the tail's blocks
+    const uint32_t blocks = ((tail - 1u) >> c.log_block) + 1u, per = 1u << (g.log_tokens - c.log_block);
+    uint16_t* scale = c.scale + (uint64_t)(plane >> 1) * c.scale_layer;
+    for (uint32_t x = mover; x < blocks * g.heads; x += movers) {
+        const uint32_t at = x / blocks * per + x % blocks;
+        scale[(uint64_t)dst * c.scale_page + at] = scale[(uint64_t)src * c.scale_page + at];
     }
 }
 
@@ -415,28 +440,35 @@ __device__ __forceinline__ void pg_copy_unit(const uint16_t* __restrict__ s, uin
 // Contents of pages: of the `moves` pages behind the live ones into the holes (w.holes set), or src
 // to dst. A unit is one part of one plane (keys or values of a layer) of one page.
 struct PgCopy {
-    uint16_t* k;
-    uint16_t* v;
-    int64_t layer_stride, page_stride;
-    PgGeom g;
-    uint32_t planes, parts, num_pages, n;
+    PgPlanes c;
+    uint32_t parts, num_pages, n;
     const uint32_t* src;
     const uint32_t* dst;
 };
 
+// Part `part` of plane `plane` of page s copied to page d; the scales go with the keys' first part.
+__device__ __forceinline__ void pg_copy_part(const PgPlanes& c, uint32_t s, uint32_t d, uint32_t plane, uint32_t part)
+{
+    uint16_t* base = ((plane & 1u) ? c.v : c.k) + (int64_t)(plane >> 1) * c.layer_stride;
+    pg_copy_unit(base + (int64_t)s * c.page_stride, base + (int64_t)d * c.page_stride, c.g, part);
+    if (!c.scale || part != 0u || (plane & 1u)) return;
+    uint16_t* scale = c.scale + (uint64_t)(plane >> 1) * c.scale_layer;
+    for (uint32_t x = threadIdx.x; x < c.scale_page; x += kCopyThreads)
+        scale[(uint64_t)d * c.scale_page + x] = scale[(uint64_t)s * c.scale_page + x];
+}
+
 __global__ __launch_bounds__(256) void k_pages_copy(PgCopy c, uint32_t* __restrict__ err)
 {
-    const uint64_t units = (uint64_t)c.n * c.planes * c.parts;
+    const uint64_t units = (uint64_t)c.n * c.c.planes * c.parts;
     for (uint64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const uint32_t part = (uint32_t)(u % c.parts), plane = (uint32_t)(u / c.parts % c.planes);
-        const uint32_t i = (uint32_t)(u / c.parts / c.planes);
+        const uint32_t part = (uint32_t)(u % c.parts), plane = (uint32_t)(u / c.parts % c.c.planes);
+        const uint32_t i = (uint32_t)(u / c.parts / c.c.planes);
         const uint32_t s = c.src[i], d = c.dst[i];
         if (s >= c.num_pages || d >= c.num_pages) {
             if (threadIdx.x == 0) atomicOr(err, CR_ERR_PAGE);
             continue;
         }
-        uint16_t* base = ((plane & 1u) ? c.v : c.k) + (int64_t)(plane >> 1) * c.layer_stride;
-        pg_copy_unit(base + (int64_t)s * c.page_stride, base + (int64_t)d * c.page_stride, c.g, part);
+        pg_copy_part(c.c, s, d, plane, part);
     }
 }
 
@@ -475,13 +507,12 @@ __global__ __launch_bounds__(256) void k_pages_move(PgCopy c, PgWs w, uint32_t n
         if (bad) atomicOr(err, bad);
         return;
     }
-    const uint64_t units = (uint64_t)moves * c.planes * c.parts;
+    const uint64_t units = (uint64_t)moves * c.c.planes * c.parts;
     for (uint64_t u = blockIdx.x - name_blocks; u < units; u += gridDim.x - name_blocks) {
-        const uint32_t part = (uint32_t)(u % c.parts), plane = (uint32_t)(u / c.parts % c.planes);
-        const uint32_t i = (uint32_t)(u / c.parts / c.planes);
+        const uint32_t part = (uint32_t)(u % c.parts), plane = (uint32_t)(u / c.parts % c.c.planes);
+        const uint32_t i = (uint32_t)(u / c.parts / c.c.planes);
         const uint32_t s = w.by_rank[first + i], d = w.holes[i];
-        uint16_t* base = ((plane & 1u) ? c.v : c.k) + (int64_t)(plane >> 1) * c.layer_stride;
-        pg_copy_unit(base + (int64_t)s * c.page_stride, base + (int64_t)d * c.page_stride, c.g, part);
+        pg_copy_part(c.c, s, d, plane, part);
     }
 }
 
@@ -518,34 +549,21 @@ __global__ __launch_bounds__(256) void k_kv_append(KvPages c, uint16_t* __restri
     }
 }
 
-inline PgCopy pg_copy(const cr_kv_cache* c)
+template <typename C>
+PgCopy pg_copy(const C* c)
 {
     PgCopy m{};
-    m.k = (uint16_t*)c->k;
-    m.v = (uint16_t*)c->v;
-    m.layer_stride = c->layer_stride;
-    m.page_stride = c->page_stride;
-    m.g = pg_geom(c);
-    m.planes = 2u * c->layers;
-    m.parts = (m.g.page16 + kCopyUnit - 1) / kCopyUnit;
+    m.c = pg_planes(c);
+    m.parts = (m.c.g.page16 + kCopyUnit - 1) / kCopyUnit;
     m.num_pages = c->num_pages;
     return m;
 }
 
-}  // namespace
-}  // namespace cr
-
-extern "C" size_t cr_pages_workspace_bytes(uint32_t num_pages, uint32_t n)
+// The page calls, for a cache of either kind.
+template <typename C>
+cr_status pages_extend(const C* c, const uint32_t* len_old, const uint32_t* len_new, uint32_t n, uint32_t* table,
+                       uint32_t width, void* ws, size_t ws_bytes, uint32_t* err, void* stream)
 {
-    const size_t a = 2u * (size_t)n + 1u, b = 3u * (size_t)num_pages;
-    return ((size_t)cr::pg_chunks(num_pages) + 2u + (a > b ? a : b)) * sizeof(uint32_t);
-}
-
-extern "C" cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_old, const uint32_t* len_new, uint32_t n,
-                                     uint32_t* table, uint32_t width, void* ws, size_t ws_bytes, uint32_t* err,
-                                     void* stream)
-{
-    using namespace cr;
     if (!good_cache(c) || !c->refs || !err || !ws || !aligned4(ws) || (n > 0 && (!len_new || (width > 0 && !table))) ||
         n > (1u << 24) || width > (1u << 28))
         return CR_EINVAL;
@@ -573,11 +591,11 @@ extern "C" cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_o
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
 }
 
-extern "C" cr_status cr_pages_fork(const cr_kv_cache* c, const uint32_t* table, uint32_t rows, uint32_t width,
-                                   const uint32_t* parent, const uint32_t* length, uint32_t n, uint32_t* child,
-                                   uint32_t child_width, void* ws, size_t ws_bytes, uint32_t* err, void* stream)
+template <typename C>
+cr_status pages_fork(const C* c, const uint32_t* table, uint32_t rows, uint32_t width, const uint32_t* parent,
+                     const uint32_t* length, uint32_t n, uint32_t* child, uint32_t child_width, void* ws,
+                     size_t ws_bytes, uint32_t* err, void* stream)
 {
-    using namespace cr;
     if (!good_cache(c) || !c->refs || !err || !ws || !aligned4(ws) || n > (1u << 24) || width > (1u << 28) ||
         child_width > (1u << 28) ||
         (n > 0 && (!parent || !length || (rows > 0 && width > 0 && !table) || (child_width > 0 && !child) || child == table)))
@@ -600,7 +618,7 @@ extern "C" cr_status cr_pages_fork(const cr_kv_cache* c, const uint32_t* table, 
     t.num_pages = c->num_pages;
     const hipStream_t st = as_stream(stream);
     (void)hipGetLastError();
-    const PgPlanes planes{(uint16_t*)c->k, (uint16_t*)c->v, c->layer_stride, c->page_stride, pg_geom(c), 2u * c->layers};
+    const PgPlanes planes = pg_planes(c);
     const uint64_t units = (uint64_t)n * planes.planes;
     if (c->num_pages <= kOnePages && n <= kOneSeqs && (uint64_t)n * child_width <= kOneEntries && units * planes.g.page16 <= kOnePieces) {
         hipLaunchKernelGGL(k_pages_one, dim3(1), dim3(kOneThreads), 0, st, c->refs, t, planes, err);
@@ -612,10 +630,10 @@ extern "C" cr_status cr_pages_fork(const cr_kv_cache* c, const uint32_t* table, 
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
 }
 
-extern "C" cr_status cr_pages_free(const cr_kv_cache* c, const uint32_t* table, uint32_t width, const uint32_t* length,
-                                   uint32_t n, uint32_t* err, void* stream)
+template <typename C>
+cr_status pages_free(const C* c, const uint32_t* table, uint32_t width, const uint32_t* length, uint32_t n,
+                     uint32_t* err, void* stream)
 {
-    using namespace cr;
     if (!good_cache(c) || !c->refs || !err || n > (1u << 24) || width > (1u << 28) || (n > 0 && (!length || (width > 0 && !table))))
         return CR_EINVAL;
     if ((uint64_t)n * (width ? width : 1u) >= ((uint64_t)1 << 32) - kPgThreads) return CR_EINVAL;  // threads of a launch
@@ -627,11 +645,10 @@ extern "C" cr_status cr_pages_free(const cr_kv_cache* c, const uint32_t* table, 
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
 }
 
-extern "C" cr_status cr_pages_compact(const cr_kv_cache* c, const uint32_t* table, const uint32_t* length, uint32_t rows,
-                                      uint32_t width, uint32_t* table_out, uint32_t* refs_out, void* ws, size_t ws_bytes,
-                                      uint32_t* err, void* stream)
+template <typename C>
+cr_status pages_compact(const C* c, const uint32_t* table, const uint32_t* length, uint32_t rows, uint32_t width,
+                        uint32_t* table_out, uint32_t* refs_out, void* ws, size_t ws_bytes, uint32_t* err, void* stream)
 {
-    using namespace cr;
     if (!good_cache(c) || !c->refs || !refs_out || !err || !ws || !aligned4(ws) || rows > (1u << 24) || width > (1u << 28) ||
         (rows > 0 && (!length || (width > 0 && (!table || !table_out)))))
         return CR_EINVAL;
@@ -645,7 +662,7 @@ extern "C" cr_status cr_pages_compact(const cr_kv_cache* c, const uint32_t* tabl
     const uint32_t cus = (uint32_t)device_cus();
     const uint64_t want = (names + kPgThreads - 1) / kPgThreads;
     const uint32_t name_blocks = (uint32_t)(want < cus ? want : cus);
-    const uint64_t units = (uint64_t)(c->num_pages / 2u) * m.planes * m.parts;  // no more pages than that can move
+    const uint64_t units = (uint64_t)(c->num_pages / 2u) * m.c.planes * m.parts;  // no more pages than that can move
     const uint32_t copy_blocks = (uint32_t)(units < 8u * cus ? (units ? units : 1u) : 8u * cus);
     const hipStream_t st = as_stream(stream);
     (void)hipGetLastError();
@@ -660,21 +677,95 @@ extern "C" cr_status cr_pages_compact(const cr_kv_cache* c, const uint32_t* tabl
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
 }
 
-extern "C" cr_status cr_pages_copy(const cr_kv_cache* c, const uint32_t* src, const uint32_t* dst, uint32_t n,
-                                   uint32_t* err, void* stream)
+template <typename C>
+cr_status pages_copy(const C* c, const uint32_t* src, const uint32_t* dst, uint32_t n, uint32_t* err, void* stream)
 {
-    using namespace cr;
     if (!good_cache(c) || !err || (n > 0 && (!src || !dst)) || n > CR_MAX_PAGES) return CR_EINVAL;
     if (n == 0) return CR_OK;
     PgCopy m = pg_copy(c);
     m.n = n;
     m.src = src;
     m.dst = dst;
-    const uint64_t units = (uint64_t)n * m.planes * m.parts, cap = 8u * (uint64_t)device_cus();
+    const uint64_t units = (uint64_t)n * m.c.planes * m.parts, cap = 8u * (uint64_t)device_cus();
     (void)hipGetLastError();
     hipLaunchKernelGGL(k_pages_copy, dim3((uint32_t)(units < cap ? units : cap)), dim3(kCopyThreads), 0, as_stream(stream), m,
                        err);
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
+}
+
+}  // namespace
+}  // namespace cr
+
+extern "C" size_t cr_pages_workspace_bytes(uint32_t num_pages, uint32_t n)
+{
+    const size_t a = 2u * (size_t)n + 1u, b = 3u * (size_t)num_pages;
+    return ((size_t)cr::pg_chunks(num_pages) + 2u + (a > b ? a : b)) * sizeof(uint32_t);
+}
+
+extern "C" cr_status cr_pages_extend(const cr_kv_cache* c, const uint32_t* len_old, const uint32_t* len_new, uint32_t n,
+                                     uint32_t* table, uint32_t width, void* ws, size_t ws_bytes, uint32_t* err,
+                                     void* stream)
+{
+    return cr::pages_extend(c, len_old, len_new, n, table, width, ws, ws_bytes, err, stream);
+}
+
+extern "C" cr_status cr_kvq_extend(const cr_kvq_cache* c, const uint32_t* len_old, const uint32_t* len_new, uint32_t n,
+                                   uint32_t* table, uint32_t width, void* ws, size_t ws_bytes, uint32_t* err,
+                                   void* stream)
+{
+    return cr::pages_extend(c, len_old, len_new, n, table, width, ws, ws_bytes, err, stream);
+}
+
+extern "C" cr_status cr_pages_fork(const cr_kv_cache* c, const uint32_t* table, uint32_t rows, uint32_t width,
+                                   const uint32_t* parent, const uint32_t* length, uint32_t n, uint32_t* child,
+                                   uint32_t child_width, void* ws, size_t ws_bytes, uint32_t* err, void* stream)
+{
+    return cr::pages_fork(c, table, rows, width, parent, length, n, child, child_width, ws, ws_bytes, err, stream);
+}
+
+extern "C" cr_status cr_kvq_fork(const cr_kvq_cache* c, const uint32_t* table, uint32_t rows, uint32_t width,
+                                 const uint32_t* parent, const uint32_t* length, uint32_t n, uint32_t* child,
+                                 uint32_t child_width, void* ws, size_t ws_bytes, uint32_t* err, void* stream)
+{
+    return cr::pages_fork(c, table, rows, width, parent, length, n, child, child_width, ws, ws_bytes, err, stream);
+}
+
+extern "C" cr_status cr_pages_free(const cr_kv_cache* c, const uint32_t* table, uint32_t width, const uint32_t* length,
+                                   uint32_t n, uint32_t* err, void* stream)
+{
+    return cr::pages_free(c, table, width, length, n, err, stream);
+}
+
+extern "C" cr_status cr_kvq_free(const cr_kvq_cache* c, const uint32_t* table, uint32_t width, const uint32_t* length,
+                                 uint32_t n, uint32_t* err, void* stream)
+{
+    return cr::pages_free(c, table, width, length, n, err, stream);
+}
+
+extern "C" cr_status cr_pages_compact(const cr_kv_cache* c, const uint32_t* table, const uint32_t* length,
+                                      uint32_t rows, uint32_t width, uint32_t* table_out, uint32_t* refs_out, void* ws,
+                                      size_t ws_bytes, uint32_t* err, void* stream)
+{
+    return cr::pages_compact(c, table, length, rows, width, table_out, refs_out, ws, ws_bytes, err, stream);
+}
+
+extern "C" cr_status cr_kvq_compact(const cr_kvq_cache* c, const uint32_t* table, const uint32_t* length, uint32_t rows,
+                                    uint32_t width, uint32_t* table_out, uint32_t* refs_out, void* ws, size_t ws_bytes,
+                                    uint32_t* err, void* stream)
+{
+    return cr::pages_compact(c, table, length, rows, width, table_out, refs_out, ws, ws_bytes, err, stream);
+}
+
+extern "C" cr_status cr_pages_copy(const cr_kv_cache* c, const uint32_t* src, const uint32_t* dst, uint32_t n,
+                                   uint32_t* err, void* stream)
+{
+    return cr::pages_copy(c, src, dst, n, err, stream);
+}
+
+extern "C" cr_status cr_kvq_copy(const cr_kvq_cache* c, const uint32_t* src, const uint32_t* dst, uint32_t n,
+                                 uint32_t* err, void* stream)
+{
+    return cr::pages_copy(c, src, dst, n, err, stream);
 }
 
 extern "C" cr_status cr_kv_append(const cr_kv_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, uint32_t total,

@@ -1,7 +1,8 @@
 """A destination's serving operators on the device: a paged cache of keys and values, the calls
 that take, share, move and free its pages, attention over whole prompts (a miss) and attention
-of requests that share a cached prefix (a hit, and every decoded token). Marshalling only; the
-library does the work.
+of requests that share a cached prefix (a hit, and every decoded token). The cache holds 16-bit
+elements or 8-bit floats with scales, and queries and keys are turned by their positions before they go in.
+Marshalling only; the library does the work.
 
     pool = PagePool(k, v, refs)                       # k, v [layers, pages, heads, tokens, dim]
     pool.extend(table, None, length)                  # pages for new sequences
@@ -10,6 +11,11 @@ library does the work.
     pool.fork(table, parent, length, child)           # a request behind a cached prefix
     attend_shared(q, pool, 0, q_off, group_off, table, length, own_table, own_len, scale, out=o)
     pool.free(table, length)                          # an eviction
+
+    pool = QuantPagePool.empty(layers, pages, heads, tokens, dim)   # the same calls on a cache in 8 bits
+    pool.read(0, k, v, off, length, table)            # its tokens as 16-bit rows
+    rotary = Rotary(dim, base=500000.0)               # positions ...
+    rotary.apply(q, k, positions, q_out=q, k_out=k)   # ... of a step's queries and new keys
 
 Tensors are on the GPU. Offsets, lengths and page tables are int32; a call enqueues kernels on
 ``stream`` (default: the current one) and returns. Problems that only the device sees set bits
@@ -21,18 +27,22 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 import struct
-from typing import Optional
+from typing import Optional, Sequence
 
 import torch
 
 from . import binding as B
 
 _DTYPES = {torch.bfloat16: B.CR_BF16, torch.float16: B.CR_F16}
+_CODES = {torch.float8_e4m3fn: B.CR_E4M3, torch.float8_e5m2: B.CR_E5M2}
+_LAYOUTS = {"half": B.CR_ROTARY_HALF, "pairs": B.CR_ROTARY_PAIRS}
 _INT32, _FLOAT32 = torch.int32, torch.float32
 _HERE = contextlib.nullcontext()
 _raw_stream, _device = B._raw_stream, B._device
 _pack_rows, _pack_prompt, _pack_shared, _RANGE = B.ROWS.pack, B.PROMPT_ARGS.pack, B.SHARED_ARGS.pack, (struct.error, OverflowError)
+_pack_rotary = B.ROTARY_ARGS.pack
 
 
 def _dtype(t: torch.Tensor) -> int:
@@ -137,6 +147,14 @@ class PagePool(_Memory):
     strides; ``refs``: int32 [pages], how many table entries name a page (0 = free)."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, refs: torch.Tensor, order: str = "head"):
+        strides = self._take(k, v, refs, order)
+        self.dtype = k.dtype
+        self.c = B.CrKvCache(_dtype(k), self.heads, self.dim, self.page_tokens, self.num_pages, self.layers, k.data_ptr(),
+                             v.data_ptr(), *strides, _index(refs, self.num_pages))
+        self._ready("cr_pages_", "cr_kv_append", "cr_attn_shared")
+
+    def _take(self, k, v, refs, order):
+        """The tensors, and their strides of layers, pages, heads and tokens."""
         if order not in ("head", "token"):
             raise ValueError(f"unknown order {order!r}")
         if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.stride(4) != 1:
@@ -146,13 +164,18 @@ class PagePool(_Memory):
         h, t = (2, 3) if order == "head" else (3, 2)
         self.k, self.v, self.refs, self.order = k, v, refs, order
         self.layers, self.num_pages, self.heads, self.page_tokens, self.dim = k.shape[0], k.shape[1], k.shape[h], k.shape[t], k.shape[4]
-        self.err = torch.zeros(1, dtype=torch.int32, device=k.device)
-        self.c = B.CrKvCache(_dtype(k), self.heads, self.dim, self.page_tokens, self.num_pages, self.layers, k.data_ptr(),
-                             v.data_ptr(), k.stride(0), k.stride(1), k.stride(h), k.stride(t), _index(refs, self.num_pages))
+        return k.stride(0), k.stride(1), k.stride(h), k.stride(t)
+
+    def _ready(self, pages: str, append: str, attn: str, *held):
+        """The library's calls for this cache, and the memory that they use."""
+        L = B.load()
+        self._extend, self._fork, self._free, self._compact, self._copy = (getattr(L, pages + x) for x in ("extend", "fork", "free", "compact", "copy"))
+        self._append, self._attn, self._attn_bytes = getattr(L, append), getattr(L, attn), getattr(B, attn + "_workspace_bytes")
+        self.err = torch.zeros(1, dtype=torch.int32, device=self.k.device)
         self._ref, self._err = ctypes.byref(self.c), _index(self.err)
-        self._ws = torch.empty(B.cr_pages_workspace_bytes(self.num_pages, 0), dtype=torch.uint8, device=k.device)
+        self._ws = torch.empty(B.cr_pages_workspace_bytes(self.num_pages, 0), dtype=torch.uint8, device=self.k.device)
         self._ws_for = 0  # sequences that it is known to be large enough for
-        super().__init__(k, v, refs, self.err, self._ws)
+        _Memory.__init__(self, self.k, self.v, self.refs, self.err, self._ws, *held)
 
     @classmethod
     def empty(cls, layers: int, num_pages: int, heads: int, page_tokens: int, dim: int, dtype=torch.bfloat16, device="cuda",
@@ -184,20 +207,20 @@ class PagePool(_Memory):
         n = len_new.numel()
         new, old = _index(len_new), None if len_old is None else _index(len_old, n)
         p, width = _table(table, n)
-        B._check(B.load().cr_pages_extend(self._ref, old, new, n, p, width, *self._scratch(n, stream)), "cr_pages_extend")
+        B._check(self._extend(self._ref, old, new, n, p, width, *self._scratch(n, stream)), self._extend.__name__)
 
     def fork(self, table, parent, length, child, stream=None):
         """child[i]: the first length[i] tokens of table[parent[i]], the partial tail copied."""
         n, rows = parent.numel(), table.shape[0]
         (p, width), (c, child_width) = _table(table, rows), _table(child, n)
-        B._check(B.load().cr_pages_fork(self._ref, p, rows, width, _index(parent), _index(length, n), n, c, child_width,
-                                        *self._scratch(n, stream)), "cr_pages_fork")
+        B._check(self._fork(self._ref, p, rows, width, _index(parent), _index(length, n), n, c, child_width,
+                                        *self._scratch(n, stream)), self._fork.__name__)
 
     def free(self, table, length, stream=None):
         """Gives the pages of every row's first length tokens back."""
         n = length.numel()
         p, width = _table(table, n)
-        B._check(B.load().cr_pages_free(self._ref, p, width, _index(length), n, self._err, self._on(stream)), "cr_pages_free")
+        B._check(self._free(self._ref, p, width, _index(length), n, self._err, self._on(stream)), self._free.__name__)
 
     def compact(self, table, length, table_out=None, refs_out=None, stream=None):
         """Moves the live pages to the front and renames the table's entries (in place, if no
@@ -210,24 +233,193 @@ class PagePool(_Memory):
             rows = length.numel()
             p, width = _table(table, rows)
             lengths, out = _index(length), p if table_out is None else _index(table_out, rows * width)
-        B._check(B.load().cr_pages_compact(self._ref, p, lengths, rows, width, out, refs, *self._scratch(0, stream)), "cr_pages_compact")
+        B._check(self._compact(self._ref, p, lengths, rows, width, out, refs, *self._scratch(0, stream)), self._compact.__name__)
 
     def copy(self, src, dst, stream=None):
         """Contents of page src[i] to page dst[i], all layers."""
         n = src.numel()
-        B._check(B.load().cr_pages_copy(self._ref, _index(src), _index(dst, n), n, self._err, self._on(stream)), "cr_pages_copy")
+        B._check(self._copy(self._ref, _index(src), _index(dst, n), n, self._err, self._on(stream)), self._copy.__name__)
 
     def append(self, layer: int, k, v, off, length, table, stream=None):
         """Rows off[i]..off[i+1] of k and v ([total, heads, dim]) become the last tokens of the
         length[i] of sequence i."""
-        shape, n, dtype = k.shape, length.numel(), self.k.dtype
+        shape, n, dtype = k.shape, length.numel(), self.dtype
         if len(shape) != 3 or shape[1] != self.heads or shape[2] != self.dim or shape != v.shape or k.dtype is not dtype or v.dtype is not dtype:
             raise B.CrError("new keys and values have the cache's heads, dim and type")
         if (k.requires_grad or v.requires_grad) and _grad_on():
             _refuse_grad()
         p, width = _table(table, n)
-        B._check(B.load().cr_kv_append(self._ref, layer, _pack_rows(*_rows(k)), _pack_rows(*_rows(v)), shape[0],
-                                       _index(off, n + 1), _index(length), n, p, width, self._err, self._on(stream)), "cr_kv_append")
+        B._check(self._append(self._ref, layer, _pack_rows(*_rows(k)), _pack_rows(*_rows(v)), shape[0],
+                                       _index(off, n + 1), _index(length), n, p, width, self._err, self._on(stream)), self._append.__name__)
+
+
+class QuantPagePool(PagePool):
+    """Handle of a paged cache in 8 bits. ``k``, ``v``: as a PagePool's, float8_e4m3fn or float8_e5m2; ``scale``: uint8
+    [layers, pages, heads, page tokens / block tokens, 2], of each block of tokens the exponent + 127 of the power of two
+    that its keys' codes, and its values', are multiplied with (a scale of 127 is 1); ``dtype``: the type of queries, new keys and values and outputs.
+    All of PagePool's calls and ``attend_shared`` work on it: ``append`` rounds into it, with a block's scale chosen by
+    its largest element."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, scale: torch.Tensor, refs: torch.Tensor, dtype=torch.bfloat16, order: str = "head"):
+        strides = self._take(k, v, refs, order)
+        if k.dtype not in _CODES:
+            raise B.CrError(f"float8_e4m3fn or float8_e5m2 wanted, not {k.dtype}")
+        if dtype not in _DTYPES:
+            raise B.CrError(f"bfloat16 or float16 wanted, not {dtype}")
+        blocks = scale.shape[3] if scale.dim() == 5 else 0
+        if scale.dtype is not torch.uint8 or blocks == 0 or scale.shape != (self.layers, self.num_pages, self.heads, blocks, 2) or \
+                self.page_tokens % blocks or not scale.is_contiguous():
+            raise B.CrError("scale is uint8 [layers, pages, heads, page tokens / block tokens, 2], contiguous")
+        if not (k.device == v.device == scale.device == refs.device):
+            raise B.CrError("codes, scales and refs are on one device")
+        self.scale, self.dtype, self.block_tokens = scale, dtype, self.page_tokens // blocks
+        self.c = B.CrKvqCache(_DTYPES[dtype], _CODES[k.dtype], self.heads, self.dim, self.page_tokens, self.block_tokens, self.num_pages,
+                              self.layers, k.data_ptr(), v.data_ptr(), *strides, scale.data_ptr(), _index(refs, self.num_pages))
+        self._device = k.device.index
+        self._ready("cr_kvq_", "cr_kvq_append", "cr_kvq_attn", scale)
+        self._read = B.load().cr_kvq_read
+
+    @classmethod
+    def empty(cls, layers: int, num_pages: int, heads: int, page_tokens: int, dim: int, dtype=torch.bfloat16, device="cuda",
+              order: str = "head", codes=torch.float8_e4m3fn, block_tokens: Optional[int] = None) -> "QuantPagePool":
+        """A new cache, all pages free; blocks of 16 tokens (or of a page, if that is smaller) unless given."""
+        block = min(16, page_tokens) if block_tokens is None else block_tokens
+        if block < 1 or page_tokens % block:
+            raise B.CrError(f"a page of {page_tokens} tokens is not whole blocks of {block}")
+        shape = (layers, num_pages) + ((heads, page_tokens) if order == "head" else (page_tokens, heads)) + (dim,)
+        k, v = (torch.empty(shape, dtype=torch.uint8, device=device).view(codes) for _ in range(2))
+        scale = torch.full((layers, num_pages, heads, page_tokens // block, 2), 127, dtype=torch.uint8, device=device)
+        return cls(k, v, scale, torch.zeros(num_pages, dtype=torch.int32, device=device), dtype, order)
+
+    def _on(self, stream):
+        if _device() != self._device:
+            raise B.CrError(f"the cache is on cuda:{self._device}, the current device is cuda:{_device()}")
+        return super()._on(stream)
+
+    def read(self, layer: int, k, v, off, length, table, stream=None):
+        """The reverse of ``append``: the last tokens of the length[i] of sequence i into rows off[i]..off[i+1] of k and
+        v ([total, heads, dim], the cache's dtype; either may be None)."""
+        n, rows, shape = length.numel(), [None, None], None
+        for i, x in enumerate((k, v)):
+            if x is None:
+                continue
+            if x.dim() != 3 or x.shape[1] != self.heads or x.shape[2] != self.dim or x.dtype is not self.dtype or (shape or x.shape) != x.shape:
+                raise B.CrError("rows to read into have the cache's heads, dim and type")
+            if x.requires_grad and _grad_on():
+                _refuse_grad()
+            shape, rows[i] = x.shape, _pack_rows(*_rows(x))
+        if shape is None:
+            raise B.CrError("rows of keys or of values are wanted")
+        p, width = _table(table, n)
+        B._check(self._read(self._ref, layer, *rows, shape[0], _index(off, n + 1), _index(length), n, p, width, self._err,
+                            self._on(stream)), "cr_kvq_read")
+
+
+def rotary_frequencies(rotated: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0, length: Optional[int] = None,
+                       low: float = 1.0, high: float = 4.0) -> list:
+    """Radians per position of each pair i of ``rotated`` / 2: f_i = base^(-2i / rotated), for contexts that are
+    ``factor`` times as long as trained with ``scaling``
+
+    * "linear": f_i / factor;
+    * "base": base becomes base * factor^(rotated / (rotated - 2)), which divides the last frequency by the factor and keeps the first;
+    * "turns": frequencies that make ``high`` turns or more over ``length`` tokens stay, those of ``low`` or fewer are
+      divided by the factor, between them the share that stays goes by the turns;
+    * "index": the same with the share falling from pair to pair between the two that would make ``high`` and
+      ``low`` turns, rounded outwards.
+    """
+    if scaling not in (None, "linear", "base", "turns", "index"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if rotated < 2 or rotated % 2:
+        raise B.CrError(f"pairs of elements turn, not {rotated}")
+    if not (base > 1.0 and factor > 0.0 and math.isfinite(base) and math.isfinite(factor)):
+        raise B.CrError("base is above 1 and factor above 0")
+    if scaling in ("turns", "index") and not (length is not None and length > 0 and 0.0 < low < high):
+        raise B.CrError("this scaling goes by the turns over `length` tokens, 0 < low < high")
+    if scaling == "base":
+        if rotated == 2:
+            raise B.CrError("one pair alone has no other base")
+        base *= factor ** (rotated / (rotated - 2))
+    f = [base ** (-2.0 * i / rotated) for i in range(rotated // 2)]
+    if scaling == "linear":
+        return [x / factor for x in f]
+    if scaling in (None, "base"):
+        return f
+    if scaling == "turns":
+        stay = [(length * x / (2.0 * math.pi) - low) / (high - low) for x in f]
+    else:
+        pair = lambda turns: rotated * math.log(length / (2.0 * math.pi * turns)) / (2.0 * math.log(base))  # noqa: E731
+        a, b = max(math.floor(pair(high)), 0), min(math.ceil(pair(low)), rotated - 1)
+        stay = [1.0 - (i - a) / max(b - a, 0.001) for i in range(len(f))]
+    stay = [min(1.0, max(0.0, s)) for s in stay]
+    return [x * ((1.0 - s) / factor + s) for x, s in zip(f, stay)]
+
+
+class Rotary(_Memory):
+    """Rotary positions for heads of ``dim``: the first ``rotated`` elements (all, if not given) turn, pairs being elements i and
+    i + rotated / 2 (``layout`` "half") or 2i and 2i + 1 ("pairs"). Frequencies are rotary_frequencies(...) or given
+    (radians per position, one a pair); what turns is also multiplied with ``magnitude``. Far positions lose nothing: angles are exact
+    fractions of a turn."""
+
+    def __init__(self, dim: int, rotated: Optional[int] = None, *, base: float = 10000.0, layout: str = "half", scaling: Optional[str] = None,
+                 factor: float = 1.0, length: Optional[int] = None, low: float = 1.0, high: float = 4.0, magnitude: float = 1.0,
+                 frequencies: Optional[Sequence[float]] = None, device="cuda"):
+        if layout not in _LAYOUTS:
+            raise ValueError(f"unknown layout {layout!r}")
+        self.dim, self.rotated, self.layout, self.magnitude = dim, dim if rotated is None else rotated, layout, float(magnitude)
+        if dim not in (64, 128) or self.rotated not in range(16, dim + 1, 16):
+            raise B.CrError("heads are of 64 or 128 elements, of which a multiple of 16 turns")
+        if not abs(self.magnitude) <= 3.4e38:
+            raise B.CrError("magnitude is finite")
+        if frequencies is None:
+            frequencies = rotary_frequencies(self.rotated, base, scaling, factor, length, low, high)
+        self.frequencies = [float(f) for f in frequencies]
+        if len(self.frequencies) != self.rotated // 2 or not all(math.isfinite(f) for f in self.frequencies):
+            raise B.CrError(f"{self.rotated // 2} finite frequencies wanted")
+        turns = [int(round(f / (2.0 * math.pi) * 2.0 ** 64)) % (1 << 64) for f in self.frequencies]  # of 2^64 a turn
+        self.freq = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64).to(device)
+        if not self.freq.is_cuda:
+            raise B.CrError("libcr takes device tensors")
+        self._device, self._code = self.freq.device.index, _LAYOUTS[layout]
+        super().__init__(self.freq)
+
+    def apply(self, q, k, positions, q_out=None, k_out=None, stream=None):
+        """q [tokens, heads, dim] and k [tokens, key heads, dim] (or None) turned by ``positions`` (int32 [tokens]; negative ones
+        turn back) into q_out and k_out, new tensors if not given; q and k themselves may be given, other tensors must not overlap
+        q or k. Returns both."""
+        shape, dtype = q.shape, q.dtype
+        if len(shape) != 3 or shape[2] != self.dim:
+            raise B.CrError("rows are [tokens, heads, dim] with the dim of this handle")
+        code = _dtype(q)
+        if k is None:
+            if k_out is not None:
+                raise B.CrError("there are no keys to turn")
+            heads_k, keys, keys_out = 0, (0, 0, 0), (0, 0, 0)
+        else:
+            if k.dim() != 3 or k.shape[0] != shape[0] or k.shape[2] != self.dim or k.dtype is not dtype:
+                raise B.CrError("k has q's tokens, dim and type")
+            heads_k, keys = k.shape[1], _rows(k)
+        if _grad_on() and (q.requires_grad or (k is not None and k.requires_grad)):
+            _refuse_grad()
+        queries = _rows(q)
+        if q_out is None:
+            q_out = _new_out(q, stream)
+        if k is not None:
+            if k_out is None:
+                k_out = _new_out(k, stream)
+            if k_out.shape != k.shape or k_out.dtype is not dtype:
+                raise B.CrError("k_out has k's shape and type")
+            keys_out = _rows(k_out)
+        if q_out.shape != shape or q_out.dtype is not dtype:
+            raise B.CrError("q_out has q's shape and type")
+        if _device() != self._device:
+            raise B.CrError(f"the frequencies are on cuda:{self._device}, the current device is cuda:{_device()}")
+        try:
+            a = _pack_rotary(code, shape[1], heads_k, self.dim, self.rotated, self._code, shape[0], self.magnitude, *queries, *keys,
+                             *_rows(q_out), *keys_out, _index(positions, shape[0]), self.freq.data_ptr())
+        except _RANGE as e:
+            raise B.CrError(f"an argument is out of range: {e}") from None
+        B._check(B.load().cr_rotary(a, self._on(stream)), "cr_rotary")
+        return q_out, k_out
 
 
 def _check_out(q, shape, out, lse):
@@ -280,7 +472,7 @@ def shared_workspace(q, pool: PagePool, group_off, prefix_table, own_table, err:
     """Scratch for ``attend_shared`` of tensors of these shapes."""
     batch, own_width = own_table.shape
     a = B.CrAttnSharedArgs(q.shape[1], 0, batch, group_off.numel() - 1, q.shape[0], prefix_table.shape[1], own_width, 1.0)
-    return Workspace(B.cr_attn_shared_workspace_bytes(pool.c, a), q.device, pool.err if err is None else err)
+    return Workspace(pool._attn_bytes(pool.c, a), q.device, pool.err if err is None else err)
 
 
 def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table, prefix_len, own_table, own_len,
@@ -292,7 +484,7 @@ def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table,
     wide as their longest row keep the GPU busy: the widths stand for the lengths, which only the
     device knows."""
     shape = q.shape
-    if q.dtype is not pool.k.dtype or len(shape) != 3 or shape[2] != pool.dim:
+    if q.dtype is not pool.dtype or len(shape) != 3 or shape[2] != pool.dim:
         raise B.CrError("q has the cache's type and dim")
     if (q.requires_grad or pool.k.requires_grad or pool.v.requires_grad) and _grad_on():
         _refuse_grad()
@@ -313,5 +505,5 @@ def attend_shared(q, pool: PagePool, layer: int, q_off, group_off, prefix_table,
     handle = pool._on(stream)
     if handle not in ws._seen:
         ws._see(handle, stream)
-    B._check(B.load().cr_attn_shared(pool._ref, a, *ws.args, handle), "cr_attn_shared")
+    B._check(pool._attn(pool._ref, a, *ws.args, handle), pool._attn.__name__)
     return out
