@@ -617,21 +617,25 @@ cr_status cr_kvq_compact(const cr_kvq_cache* c, const uint32_t* table, const uin
 cr_status cr_kvq_copy(const cr_kvq_cache* c, const uint32_t* src, const uint32_t* dst, uint32_t n, uint32_t* err,
                       void* stream);
 
-/* cr_kv_append for this cache: rows off[i]..off[i+1] of k and v (type c->dtype) are rounded into the last of the
- * length[i] tokens of sequence i, with scales as above; tokens from before are those of the sequence's first
- * length[i] - (off[i+1] - off[i]). Errors as there (offsets out of order set CR_ERR_SEQ, and any
+/* Tokens of packed sequences in one layer: those of sequence i are rows off[i]..off[i+1] of k and v ([total][heads][dim], type
+ * c->dtype) and the last of its length[i] tokens in the cache. total < 2^31. */
+typedef struct {
+    uint32_t layer, total, n, width;
+    cr_rows k, v;
+    const uint32_t* off;     /* u32 [n + 1], 0 .. total, non-decreasing */
+    const uint32_t* length;  /* u32 [n]                                 */
+    const uint32_t* table;   /* u32 [n][width]                          */
+} cr_kvq_tokens;
+
+/* cr_kv_append for this cache: the rows are rounded into the tokens, with scales as above; tokens from before are those of the
+ * sequence's first length[i] - (off[i+1] - off[i]). Errors as there (offsets out of order set CR_ERR_SEQ, and any
  * sequence may then be skipped); sequences must not name the same page for the tokens they write, nor one that
  * another table's row goes on reading. */
-cr_status cr_kvq_append(const cr_kvq_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, uint32_t total,
-                        const uint32_t* off, const uint32_t* length, uint32_t n, const uint32_t* table, uint32_t width,
-                        uint32_t* err, void* stream);
+cr_status cr_kvq_append(const cr_kvq_cache* c, const cr_kvq_tokens* t, uint32_t* err, void* stream);
 
-/* The reverse: the last off[i+1] - off[i] of sequence i's first length[i] tokens into rows off[i]..off[i+1] of k and
- * v (type c->dtype, [total][heads][dim]). Either may be NULL. off, length, table and errors as
- * cr_kvq_append; rows of tokens that are skipped stay as they are. */
-cr_status cr_kvq_read(const cr_kvq_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, uint32_t total,
-                      const uint32_t* off, const uint32_t* length, uint32_t n, const uint32_t* table, uint32_t width,
-                      uint32_t* err, void* stream);
+/* The reverse: the tokens into the rows. k.p or v.p (or both) may be NULL. Errors as cr_kvq_append; rows of
+ * tokens that are skipped stay as they are. */
+cr_status cr_kvq_read(const cr_kvq_cache* c, const cr_kvq_tokens* t, uint32_t* err, void* stream);
 
 /* cr_attn_shared over this cache: keys and values are what the codes stand for, everything else is as
  * there, the workspace included. */

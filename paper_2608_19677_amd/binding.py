@@ -97,6 +97,11 @@ class CrKvqCache(ctypes.Structure):
                 ("head_stride", _i64), ("token_stride", _i64), ("scale", _P), ("refs", _P)]
 
 
+class CrKvqTokens(ctypes.Structure):
+    _fields_ = [("layer", _u32), ("total", _u32), ("n", _u32), ("width", _u32), ("k", CrRows), ("v", CrRows), ("off", _P), ("length", _P),
+                ("table", _P)]
+
+
 class CrRotaryArgs(ctypes.Structure):
     _fields_ = [("dtype", _u32), ("heads_q", _u32), ("heads_k", _u32), ("dim", _u32), ("rotated", _u32), ("layout", _u32),
                 ("total", _u32), ("magnitude", _f32), ("q", CrRows), ("k", CrRows), ("q_out", CrRows), ("k_out", CrRows),
@@ -108,8 +113,9 @@ ROWS = struct.Struct("@Pqq")
 PROMPT_ARGS = struct.Struct("@8If" + "Pqq" * 4 + "PPP")
 SHARED_ARGS = struct.Struct("@7If" + "Pqq" * 2 + "PPPPPPP")
 ROTARY_ARGS = struct.Struct("@7If" + "Pqq" * 4 + "PP")
-assert [x.size for x in (ROWS, PROMPT_ARGS, SHARED_ARGS, ROTARY_ARGS)] == \
-    [ctypes.sizeof(x) for x in (CrRows, CrAttnPromptArgs, CrAttnSharedArgs, CrRotaryArgs)]
+TOKENS_ARGS = struct.Struct("@4I" + "Pqq" * 2 + "PPP")
+assert [x.size for x in (ROWS, PROMPT_ARGS, SHARED_ARGS, ROTARY_ARGS, TOKENS_ARGS)] == \
+    [ctypes.sizeof(x) for x in (CrRows, CrAttnPromptArgs, CrAttnSharedArgs, CrRotaryArgs, CrKvqTokens)]
 
 
 class CrError(RuntimeError):
@@ -180,7 +186,7 @@ def load(path: Optional[str] = None):
     coded = ctypes.POINTER(CrKvqCache)
     for f in ("extend", "fork", "free", "compact", "copy"):
         getattr(L, "cr_kvq_" + f).argtypes = [coded] + getattr(L, "cr_pages_" + f).argtypes[1:]
-    L.cr_kvq_append.argtypes = L.cr_kvq_read.argtypes = [coded, _u32, _P, _P, _u32, _P, _P, _u32, _P, _u32, _P, _P]
+    L.cr_kvq_append.argtypes = L.cr_kvq_read.argtypes = [coded, _P, _P, _P]
     L.cr_kvq_attn_workspace_bytes.argtypes = [coded, _P]
     L.cr_kvq_attn.argtypes = [coded, _P, _P, size, _P, _P]
     L.cr_rotary.argtypes = [_P, _P]
@@ -467,15 +473,12 @@ def cr_kvq_copy(cache: CrKvqCache, src, dst, err, stream=None):
     _check(load().cr_kvq_copy(ctypes.byref(cache), _ptr(src), _ptr(dst), src.numel(), _ptr(err), _stream(stream)), "cr_kvq_copy")
 
 
-def cr_kvq_append(cache: CrKvqCache, layer: int, k: CrRows, v: CrRows, total: int, off, length, table, err, stream=None):
-    _check(load().cr_kvq_append(ctypes.byref(cache), layer, _ref(k), _ref(v), total, _ptr(off), _ptr(length), length.numel(),
-                                _ptr(table), _table_width(table), _ptr(err), _stream(stream)), "cr_kvq_append")
+def cr_kvq_append(cache: CrKvqCache, tokens: CrKvqTokens, err, stream=None):
+    _check(load().cr_kvq_append(ctypes.byref(cache), _ref(tokens), _ptr(err), _stream(stream)), "cr_kvq_append")
 
 
-def cr_kvq_read(cache: CrKvqCache, layer: int, k: Optional[CrRows], v: Optional[CrRows], total: int, off, length, table, err, stream=None):
-    _check(load().cr_kvq_read(ctypes.byref(cache), layer, None if k is None else _ref(k), None if v is None else _ref(v), total,
-                              _ptr(off), _ptr(length), length.numel(), _ptr(table), _table_width(table), _ptr(err),
-                              _stream(stream)), "cr_kvq_read")
+def cr_kvq_read(cache: CrKvqCache, tokens: CrKvqTokens, err, stream=None):
+    _check(load().cr_kvq_read(ctypes.byref(cache), _ref(tokens), _ptr(err), _stream(stream)), "cr_kvq_read")
 
 
 def cr_kvq_attn_workspace_bytes(cache: CrKvqCache, args: CrAttnSharedArgs) -> int:

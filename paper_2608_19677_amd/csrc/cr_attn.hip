@@ -397,7 +397,10 @@ __device__ __forceinline__ bool all_finite(const f32x16 (&o)[kDim / 32])
 // The wave's rows are row .. last_row (repeated) of the sequence, its half tiles at first, first + step, ... below stop;
 // keys are read up to key_end, and all of its rows see `full` of them. The running maximum moves as it did in the first run,
 // so that all other sums come out the same, bit for bit.
-template <typename E, typename S, int kDim, bool kPaged>
+template <int kDim>
+__device__ constexpr uint32_t few_dim(uint32_t e);  // where o has element e of a head: see FewLoader
+
+template <typename E, typename S, int kDim, bool kPaged, bool kFew = false>
 __device__ CR_INLINE void only_seen(const Attn& a, const Seq& it, uint32_t head_kv, uint32_t row, uint32_t last_row, uint32_t first, uint32_t step,
                                     uint32_t stop, uint32_t key_end, uint32_t full, f32x16 (&o)[kDim / 32])
 {
@@ -450,8 +453,10 @@ __device__ CR_INLINE void only_seen(const Attn& a, const Seq& it, uint32_t head_
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
         const Elem* k = at(a.pg.k, a.k, k0, col);
 #pragma unroll
-        for (int d = 0; d < kDim / 16; ++d)
-            s = E::mfma(__builtin_bit_cast(s16x8, eight(k + d * 16 + half * 8u)), *reinterpret_cast<const s16x8*>(qp + d * 16 + half * 8u), s);
+        for (int d = 0; d < kDim / 16; ++d) {
+            const uint32_t e = kFew ? few_dim<kDim>((2u * d + half) * 8u) : d * 16 + half * 8u;
+            s = E::mfma(__builtin_bit_cast(s16x8, eight(k + e)), *reinterpret_cast<const s16x8*>(qp + e), s);
+        }
         const int32_t l = kPaged && k0 < it.gap_end ? min(lim, (int32_t)it.len0) : lim;
         float top = -INFINITY;
 #pragma unroll
@@ -479,10 +484,10 @@ __device__ CR_INLINE void only_seen(const Attn& a, const Seq& it, uint32_t head_
             s16x8 vf[kDim / 32];
 #pragma unroll
             for (int y = 0; y < 8; ++y) {
-                const Elem* v = at(a.pg.v, a.v, k0, ks * 16u + (y / 4) * 8u + half * 4u + (y & 3)) + col;
+                const Elem* v = at(a.pg.v, a.v, k0, ks * 16u + (y / 4) * 8u + half * 4u + (y & 3)) + (kFew ? 0u : col);
 #pragma unroll
                 for (int d = 0; d < kDim / 32; ++d) {
-                    const uint32_t x = S::template one<E>(v[d * 32], scale);
+                    const uint32_t x = S::template one<E>(v[kFew ? few_dim<kDim>(d * 32 + col) : d * 32], scale);
                     vf[d][y] = (short)(in_part && not_finite(x) ? 0u : x);
                 }
             }
@@ -497,7 +502,7 @@ __device__ CR_INLINE void only_seen(const Attn& a, const Seq& it, uint32_t head_
             for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const uint32_t x = S::template one<E>(v[d * 32 + 8 * (i / 4) + 4u * half + (i & 3)], scale);
+                    const uint32_t e = d * 32 + 8 * (i / 4) + 4u * half + (i & 3), x = S::template one<E>(v[kFew ? few_dim<kDim>(e) : e], scale);
                     if (not_finite(x)) o[d][i] += E::wide(x);
                 }
         }
@@ -890,6 +895,45 @@ struct NarrowLds {
     float row_max[kWaves][32], row_sum[kWaves][32], row_rounded[kWaves][32];
 };
 
+// Sequence x of the lists (first_n of the first list, then own tokens): whether it fits. Where offsets of rows or groups are out
+// of order sequences may overlap, and the sum of their units passes what the host allowed for: *disorder, and no list is
+// worked on.
+template <bool kPaged>
+__device__ CR_INLINE bool list_seq(const Attn& a, uint32_t first_n, uint32_t x, uint32_t* tok0, uint32_t* nq, uint32_t* n, uint32_t* key0, bool* disorder)
+{
+    const bool own = x >= first_n;
+    const uint32_t y = own ? x - first_n : x;
+    uint32_t r0 = y, r1 = y + 1u;
+    if (kPaged && !own) {
+        r0 = a.group_off[y];
+        r1 = a.group_off[y + 1u];
+    }
+    const bool in_order = r0 <= r1 && r1 <= a.batch;
+    bool ok = in_order;
+    if (kPaged && !own && ((y == 0u && r0 != 0u) || (y + 1u == a.groups && r1 != a.batch))) atomicOr(a.err, CR_ERR_SEQ);
+    if (kPaged) {
+        *n = own ? a.own_len[y] : a.prefix_len[y];
+        ok = ok && pages_of(*n, a.pg.log_tokens) <= (own ? a.own_width : a.prefix_width);
+    } else {
+        const uint32_t k0 = a.k_off[y], k1 = a.k_off[y + 1u];
+        *key0 = k0;
+        *n = k1 - k0;
+        ok = ok && k0 <= k1 && k1 <= a.total_k;
+    }
+    *disorder |= !in_order;
+    if (in_order) {  // looked at whatever the keys are: the other sequences' sum depends on it
+        const uint32_t t0 = a.q_off[r0], t1 = a.q_off[r1];
+        const bool fits = t0 <= t1 && t1 <= a.total_q;
+        *disorder |= !fits;
+        ok = ok && fits;
+        *tok0 = t0;
+        *nq = t1 - t0;
+        if ((r0 == 0u && t0 != 0u) || (r1 == a.batch && t1 != a.total_q)) atomicOr(a.err, CR_ERR_SEQ);
+    }
+    if (!ok) atomicOr(a.err, CR_ERR_SEQ);
+    return ok;
+}
+
 template <typename E, typename S, int kDim, bool kPaged>
 __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t block, uint32_t blocks, uint16_t* lds, NarrowLds& sh)
 {
@@ -904,44 +948,10 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
     // Sequences 0 .. first_n of the first list, then those of the second.
     const uint32_t first_n = (lists & 1u) ? (kPaged ? a.groups : a.batch) : 0u;
     const uint32_t all_n = first_n + ((lists & 2u) ? a.batch : 0u);
-    // Units of sequence x; what does not fit has none. Where offsets of rows or groups are out of order
-    // sequences may overlap, and the sum of their units passes what the host allowed for: no list is worked on.
+    // Units of sequence x; what does not fit has none.
     bool disorder = false;
     auto units = [&](uint32_t x, uint32_t* tok0, uint32_t* nq, uint32_t* n, uint32_t* key0) CR_INLINE -> uint32_t {
-        if (x >= all_n) return 0u;
-        const bool own = x >= first_n;
-        const uint32_t y = own ? x - first_n : x;
-        uint32_t r0 = y, r1 = y + 1u;
-        if (kPaged && !own) {
-            r0 = a.group_off[y];
-            r1 = a.group_off[y + 1u];
-        }
-        const bool in_order = r0 <= r1 && r1 <= a.batch;
-        bool ok = in_order;
-        if (kPaged && !own && ((y == 0u && r0 != 0u) || (y + 1u == a.groups && r1 != a.batch))) atomicOr(a.err, CR_ERR_SEQ);
-        if (kPaged) {
-            *n = own ? a.own_len[y] : a.prefix_len[y];
-            ok = ok && pages_of(*n, a.pg.log_tokens) <= (own ? a.own_width : a.prefix_width);
-        } else {
-            const uint32_t k0 = a.k_off[y], k1 = a.k_off[y + 1u];
-            *key0 = k0;
-            *n = k1 - k0;
-            ok = ok && k0 <= k1 && k1 <= a.total_k;
-        }
-        disorder |= !in_order;
-        if (in_order) {  // looked at whatever the keys are: the other sequences' sum depends on it
-            const uint32_t t0 = a.q_off[r0], t1 = a.q_off[r1];
-            const bool fits = t0 <= t1 && t1 <= a.total_q;
-            disorder |= !fits;
-            ok = ok && fits;
-            *tok0 = t0;
-            *nq = t1 - t0;
-            if ((r0 == 0u && t0 != 0u) || (r1 == a.batch && t1 != a.total_q)) atomicOr(a.err, CR_ERR_SEQ);
-        }
-        if (!ok) {
-            atomicOr(a.err, CR_ERR_SEQ);
-            return 0u;
-        }
+        if (x >= all_n || !list_seq<kPaged>(a, first_n, x, tok0, nq, n, key0, &disorder)) return 0u;
         const uint32_t rows = *nq * a.group;
         return (rows + kNarrowRows - 1u) / kNarrowRows *
                ((*n + kNarrowKeys - 1u) / kNarrowKeys * (rows > 32u ? 2u : 1u) + kStart);
@@ -1186,6 +1196,454 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
     }
 }
 
+// Few rows over codes. Every wavefront works by itself: it takes an equal share of its key head's line of units, where a
+// sequence has kFewStart units and one for each tile of 32 keys for every 32 of its rows, keeps its rows' sums
+// in registers to the end of a stretch and writes them to a slot. No barrier, no sums through LDS; page ids are read two tiles ahead and
+// codes one, past the end of a stretch into the next one's.
+//
+// With half the bytes of 16-bit elements a block's start and join (8 us a stretch where four wavefronts share one) were most of
+// the time of many short sequences.
+constexpr uint32_t kFewRowTile = 32, kFewWindow = 512, kFewPart = kFewWindow / kWaves, kFewEntries = 256;
+constexpr uint32_t kFewStart = 3;  // tiles that a stretch's start and end cost
+
+template <int kDim>
+constexpr uint32_t few_lds()  // elements per wavefront
+{
+    return key_tile(kNarrowKeys, kDim) + val_tile(kNarrowKeys, kDim);
+}
+
+// Sequences that the block looks at: up to kFewWindow of them all wavefronts together, of more each a part of its own; and
+// the units of all windows (of `per` windows each).
+struct FewLds {
+    u32x4 seq[kFewWindow];  // units before it, first query token, query tokens, keys
+    uint32_t entry[kFewEntries];
+    uint32_t sums[16];
+    uint32_t disorder[kWaves];
+};
+
+// A tile of 32 keys on its way from memory to LDS: a lane moves 16 codes of every kStep-th row. In LDS the first eight of all
+// lanes' codes come before the second: neighbouring lanes write to neighbouring banks. So element e of a row there is element
+// few_dim(e) of the head, of keys (the queries' fragments follow) and of values (the outputs' do).
+template <int kDim>
+__device__ constexpr uint32_t few_dim(uint32_t e)
+{
+    return e / 8u % (kDim / 16u) * 16u + e / 8u / (kDim / 16u) * 8u + e % 8u;
+}
+
+template <typename E, typename S, int kDim>
+struct FewLoader {
+    static constexpr uint32_t kLanes = kDim / 16, kStep = kWave / kLanes, kPer = kNarrowKeys / kStep;
+    const uint8_t *kb, *vb;  // of the key head and the lane's piece
+    const uint16_t* sb;
+    uint32_t row, piece, bad;
+    uint32_t page[kPer];
+    u32x4 rk[kPer], rv[kPer];
+    uint32_t rs[kPer];
+
+    __device__ __forceinline__ void init(const Attn& a, uint32_t head_kv)
+    {
+        const uint32_t lane = lane_id();
+        piece = lane % kLanes;
+        row = lane / kLanes;
+        bad = 0;
+        kb = (const uint8_t*)a.pg.k + (int64_t)head_kv * a.pg.head_stride + piece * 16u;
+        vb = (const uint8_t*)a.pg.v + (int64_t)head_kv * a.pg.head_stride + piece * 16u;
+        sb = a.scale + ((uint64_t)head_kv << (a.pg.log_tokens - a.log_block));
+    }
+    // Rows behind the last key that a row of the stretch sees repeat it: their weights are 0, and nothing foreign is read.
+    __device__ __forceinline__ void pages(const Attn& a, const uint32_t* table, uint32_t k0, uint32_t end)
+    {
+#pragma unroll
+        for (uint32_t p = 0; p < kPer; ++p) page[p] = table[min(k0 + p * kStep + row, end - 1u) >> a.pg.log_tokens];
+    }
+    __device__ __forceinline__ void load(const Attn& a, uint32_t k0, uint32_t end)
+    {
+        const uint32_t mask = (1u << a.pg.log_tokens) - 1u, page_scales = a.pg.heads << (a.pg.log_tokens - a.log_block);
+#pragma unroll
+        for (uint32_t p = 0; p < kPer; ++p) {
+            const uint32_t tok = min(k0 + p * kStep + row, end - 1u) & mask, g = min(page[p], a.pg.num_pages - 1u);
+            bad |= page[p] >= a.pg.num_pages;
+            const uint64_t at = (uint64_t)g * (uint32_t)a.pg.page_stride + (uint64_t)tok * (uint32_t)a.pg.token_stride;
+            rk[p] = *reinterpret_cast<const u32x4*>(kb + at);
+            rv[p] = *reinterpret_cast<const u32x4*>(vb + at);
+            rs[p] = sb[(uint64_t)g * page_scales + (tok >> a.log_block)];
+        }
+    }
+    __device__ __forceinline__ void store(uint16_t* lk, uint16_t* lv) const
+    {
+#pragma unroll
+        for (uint32_t p = 0; p < kPer; ++p) {
+            const uint32_t r = p * kStep + row;
+            const float ks = scale_of(rs[p] & 0xFFu), vs = scale_of(rs[p] >> 8);
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i) {
+                const uint32_t at = piece + i * kLanes;
+                *reinterpret_cast<u32x4*>(lk + at * key_run(kNarrowKeys) + r * 8u) = S::template wide<E>(u32x2{rk[p][2 * i], rk[p][2 * i + 1]}, ks);
+                *reinterpret_cast<u32x4*>(lv + (at >> 2) * val_run(kNarrowKeys) + r * 32u + (at & 3u) * 8u) =
+                    S::template wide<E>(u32x2{rv[p][2 * i], rv[p][2 * i + 1]}, vs);
+            }
+        }
+    }
+};
+
+template <typename E, typename S, int kDim>
+__device__ CR_INLINE void few_block(const Attn& a, uint32_t lists, uint32_t block, uint32_t blocks, uint16_t* lds, FewLds& sh)
+{
+    // All heads of a share on one XCD, side by side: where heads lie next to each other in a token a head's row may be less than a line of
+    // the L2.
+    if (blocks % kXcds == 0u) block = xcd_tile(block, blocks);
+    constexpr uint32_t kKeyRun = key_run(kNarrowKeys), kValRun = val_run(kNarrowKeys);
+    const uint32_t lane = lane_id(), wv = wave_in_block(), half = lane >> 5, col = lane & 31u;
+    const uint32_t head_kv = block % a.heads_kv;
+    uint16_t* lk = lds + wv * few_lds<kDim>();
+    uint16_t* lv = lk + key_tile(kNarrowKeys, kDim);
+
+    const uint32_t first_n = (lists & 1u) ? a.groups : 0u, all_n = first_n + ((lists & 2u) ? a.batch : 0u);
+    const bool together = all_n <= kFewWindow;
+    const uint32_t slot0 = together ? 0u : wv * kFewPart;  // of the wavefront's sequences in LDS
+    bool disorder = false;
+    // Units of two sequences a lane: 2 i and 2 i + 1 from x on, i the thread of the block or the lane. Sum of the lane's; kept where
+    // the wavefront looks for its own.
+    struct Pair {
+        uint32_t v[2], tok0[2], nq[2], n[2];
+    };
+    auto pair_at = [&](uint32_t x) CR_INLINE {
+        Pair r;
+        uint32_t key0;
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+            r.v[j] = r.tok0[j] = r.nq[j] = r.n[j] = 0;
+            if (x + j >= all_n) continue;
+            if (!list_seq<true>(a, first_n, x + j, &r.tok0[j], &r.nq[j], &r.n[j], &key0, &disorder)) r.nq[j] = 0;  // no rows
+            r.v[j] = (r.nq[j] * a.group + kFewRowTile - 1u) / kFewRowTile * ((r.n[j] + kNarrowKeys - 1u) / kNarrowKeys + kFewStart);
+        }
+        return r;
+    };
+    auto keep = [&](const Pair& r, uint32_t i, uint32_t before) CR_INLINE {
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+            sh.seq[i + j] = u32x4{before + (j ? r.v[0] : 0u), r.tok0[j], r.nq[j], r.n[j]};
+        }
+    };
+    const uint32_t index = block / a.heads_kv * kWaves + wv, of = blocks / a.heads_kv * kWaves;
+    uint32_t all, base = 0, x0 = 0, here, share;
+    auto window = [&](uint32_t x) CR_INLINE {  // a wavefront's own
+        const Pair r = pair_at(x + lane * 2u);
+        const uint32_t upto = wave_incl_scan_u32(r.v[0] + r.v[1]);
+        wave_lds_fence();
+        keep(r, slot0 + lane * 2u, upto - r.v[0] - r.v[1]);
+        wave_lds_fence();
+        return rdlane(upto, 63u);
+    };
+    if (together) {
+        const Pair r = pair_at(threadIdx.x * 2u);
+        const uint64_t wrong = ballot(disorder);
+        if (lane == 0) sh.disorder[wv] = wrong != 0;
+        const uint32_t before = block_exscan_u32(r.v[0] + r.v[1], sh.sums, &all);
+        keep(r, threadIdx.x * 2u, before);
+        __syncthreads();
+        all = here = __builtin_amdgcn_readfirstlane(all);
+    } else {
+        const uint32_t windows = (all_n + kFewPart - 1u) / kFewPart, per = (windows + kFewEntries - 1u) / kFewEntries;
+        const uint32_t entries = (windows + per - 1u) / per;
+        for (uint32_t e = threadIdx.x; e < kFewEntries; e += kThreads) sh.entry[e] = 0;
+        __syncthreads();
+        for (uint32_t e = wv; e < entries; e += kWaves) {
+            uint32_t sum = 0;
+            for (uint32_t w = e * per; w < min(windows, (e + 1u) * per); ++w) {
+                const Pair r = pair_at(w * kFewPart + lane * 2u);
+                sum += r.v[0] + r.v[1];
+            }
+            sum = wave_incl_scan_u32(sum);
+            if (lane == 63u) sh.entry[e] = sum;
+        }
+        const uint64_t wrong = ballot(disorder);
+        if (lane == 0) sh.disorder[wv] = wrong != 0;
+        __syncthreads();
+        uint32_t mine[4], sum = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            mine[j] = sum;
+            sum += sh.entry[lane * 4u + j];
+        }
+        const uint32_t upto = wave_incl_scan_u32(sum);
+        all = rdlane(upto, 63u);
+        here = 0;
+        const uint32_t u0 = index * max(all / of + 1u, a.least_share);
+        uint32_t at_or_before = 0;  // entries that start at or before the wavefront's first unit
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) at_or_before += (uint32_t)__popcll(ballot(upto - sum + mine[j] <= u0));
+        const uint32_t e = at_or_before - 1u;
+        uint32_t from = upto - sum;  // of the lane's entry e & 3
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+            if ((e & 3u) == j) from += mine[j];
+        base = rdlane(from, e >> 2);
+        x0 = e * per * kFewPart - kFewPart;  // the window before: next() goes on from it
+    }
+    for (uint32_t w = 0; w < kWaves; ++w)
+        if (sh.disorder[w]) return;
+    share = max(all / of + 1u, a.least_share);
+    if ((uint64_t)index * share >= all) return;
+    uint32_t u = index * share;
+    const uint32_t u_end = min(all - u, share) + u;
+
+    // A stretch: up to 32 rows of a sequence over the tiles of it that fall into the wavefront's share.
+    struct Stretch {
+        uint32_t y, tok0, nq, n, row0, key_begin, key_end, slot;  // y: its number in its list
+        bool own, ends, valid;
+    };
+    auto rows_of = [&](const Stretch& st) CR_INLINE { return min(kFewRowTile, st.nq * a.group - st.row0); };
+    auto limit_of = [&](const Stretch& st, uint32_t m) CR_INLINE {  // keys that row m sees
+        return st.own ? (uint32_t)max(0, (int32_t)st.n - (int32_t)st.nq + 1 + (int32_t)(m / a.group)) : st.n;
+    };
+    uint32_t seq_i = slot0 - 1u, seq_end = 0, seq[4];
+    auto read_seq = [&]() CR_INLINE {
+        const u32x4 r = sh.seq[seq_i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) seq[i] = __builtin_amdgcn_readfirstlane(r[i]);
+        seq_end = base + seq[0] + (seq[2] * a.group + kFewRowTile - 1u) / kFewRowTile * ((seq[3] + kNarrowKeys - 1u) / kNarrowKeys + kFewStart);
+    };
+    if (together) {  // the sequence before the wavefront's first unit's
+        uint32_t i = 0;
+        for (uint32_t y = 0; y < all_n; y += 64u) i += (uint32_t)__popcll(ballot(sh.seq[y + lane][0] <= u));
+        seq_i = __builtin_amdgcn_readfirstlane(i - 2u);
+    }
+    auto next = [&]() CR_INLINE {
+        Stretch st;
+        st.valid = false;
+        st.key_begin = 0;
+        while (u < u_end && !st.valid) {
+            if (u >= seq_end) {  // the sequence behind, mostly: those without units are passed over
+                while (u >= base + here) {  // all > u: there is a window behind
+                    base += here;
+                    x0 += kFewPart;
+                    here = window(x0);
+                    seq_i = slot0 - 1u;
+                }
+                ++seq_i;
+                read_seq();
+                if (u >= seq_end) {
+                    uint32_t i = 0;  // the sequence of unit u
+                    for (uint32_t y = 0; y < (together ? all_n : kFewPart); y += 64u) i += (uint32_t)__popcll(ballot(sh.seq[slot0 + y + lane][0] <= u - base));
+                    seq_i = __builtin_amdgcn_readfirstlane(slot0 + i - 1u);
+                    read_seq();
+                }
+            }
+            const uint32_t x = x0 + seq_i - slot0;
+            st.own = x >= first_n;
+            st.y = st.own ? x - first_n : x;
+            st.tok0 = seq[1];
+            st.nq = seq[2];
+            st.n = seq[3];
+            const uint32_t tiles = (st.n + kNarrowKeys - 1u) / kNarrowKeys;
+            const uint32_t from = base + seq[0], step = tiles + kFewStart;
+            const uint32_t row_tile = u - from < step ? 0u : __builtin_amdgcn_readfirstlane((u - from) / step);
+            const uint32_t first = from + row_tile * step, keys = first + kFewStart, last = first + step;  // the rows' units
+            uint32_t t0 = 0, t1 = tiles;
+            st.slot = 0;
+            st.ends = true;
+            st.valid = u == first;
+            if ((st.own ? a.own_slots : a.slots) > 1u && tiles != 0u) {
+                // every wavefront whose share has a unit of the keys has a slot, though it may come without a tile
+                st.valid = u_end > keys;
+                t0 = u > keys ? u - keys : 0u;
+                t1 = u_end < last ? (st.valid ? u_end - keys : 0u) : tiles;
+                if (keys < index * share) st.slot = index - __builtin_amdgcn_readfirstlane(keys / share);
+                st.ends = last <= u_end;
+            }
+            u = last;
+            st.row0 = row_tile * kFewRowTile;
+            st.key_begin = t0 * kNarrowKeys;
+            st.key_end = min(limit_of(st, st.row0 + rows_of(st) - 1u), t1 * kNarrowKeys);
+        }
+        return st;
+    };
+    constexpr bool kAhead = kDim == 64;  // a stretch's queries are read a tile ahead; of 128 elements there is no room for them
+    FewLoader<E, S, kDim> ld;
+    ld.init(a, head_kv);
+    const uint32_t k_lane = half * kKeyRun + col * 8u;
+    const uint32_t v_lane = (half * 4u + (lane & 15u) / 4u) * 32u + ((lane >> 4) & 1u) * 16u + (lane & 3u) * 4u;
+    s16x8 qf[kDim / 16], q_next[kAhead ? kDim / 16 : 1];
+    f32x16 o[kDim / 32];
+    float mc = kNoMax, sum = 0.f, rounded = 0.f;
+    int32_t lim = 0;
+    uint32_t full = 0, m = 0;
+    // Tiles in their order: page ids of the tile at (ps, pk), codes of the one before it at (ls, lk0), work on the one before that at (st, k0).
+    // A stretch without keys is one tile of none.
+    Stretch ps, ls;
+    ps.valid = ls.valid = false;
+    ps.key_begin = ps.key_end = ls.key_begin = ls.key_end = 0;
+    uint32_t pk = 0, lk0 = 0;
+    auto table_of = [&](const Stretch& st) CR_INLINE {
+        return st.own ? a.own_table + (uint64_t)st.y * a.own_width : a.prefix_table + (uint64_t)st.y * a.prefix_width;
+    };
+    auto load_rows = [&](const Stretch& st, auto& q) CR_INLINE {
+        const uint32_t x = st.row0 + min(col, rows_of(st) - 1u);
+        const uint16_t* qp = (const uint16_t*)a.q.p + (int64_t)(st.tok0 + x / a.group) * a.q.token_stride +
+                             (int64_t)(head_kv * a.group + x % a.group) * a.q.head_stride;
+#pragma unroll
+        for (int d = 0; d < (int)(sizeof(q) / sizeof(q[0])); ++d) q[d] = *reinterpret_cast<const s16x8*>(qp + few_dim<kDim>((2u * d + half) * 8u));
+    };
+    // The tile in LDS, keys from k0 on. Fragments of keys are read before the first product, and of values before the weights.
+    auto work = [&](uint32_t k0) CR_INLINE {
+        s16x8 kf[kDim / 16];
+#pragma unroll
+        for (int d = 0; d < kDim / 16; ++d) kf[d] = *reinterpret_cast<const s16x8*>(lk + k_lane + d * 2u * kKeyRun);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int d = 0; d < kDim / 16; ++d) s = E::mfma(kf[d], qf[d], s);
+        auto values = [&](int ks, int d) CR_INLINE {
+            const uint16_t* p = lv + v_lane + d * kValRun + ks * 16u * 32u;
+            const s16x4 x = read_tr(p), y = read_tr(p + 8u * 32u);
+            return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        s16x8 vf[kDim / 32];
+#pragma unroll
+        for (int d = 0; d < kDim / 32; ++d) vf[d] = values(0, d);
+        __builtin_amdgcn_sched_barrier(0);
+        if (k0 + kNarrowKeys > full) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if ((int32_t)(k0 + 8u * (i / 4) + 4u * half + (i & 3)) >= lim) s[i] = -INFINITY;
+        }
+        float top = __builtin_elementwise_maximum(s[0], s[1]);
+#pragma unroll
+        for (int i = 2; i < 16; i += 2)
+            top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top, s[i]), s[i + 1]);
+        top = both_max(top) * a.c;
+        if (ballot(top > mc + (kSlack + E::kLift))) {
+            const float up = fmaxf(mc, top - E::kLift), f = __builtin_amdgcn_exp2f(mc - up);
+            mc = up;
+            sum *= f;
+            rounded *= f;
+#pragma unroll
+            for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        }
+        uint32_t w2[8];
+        float t[4], part_rounded = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c, -mc));
+            const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i + 1], a.c, -mc));
+            t[i & 3] = i < 4 ? x : t[i & 3] + x;
+            t[(i & 3) + 1] = i < 4 ? y : t[(i & 3) + 1] + y;
+            w2[i / 2] = E::pack(x, y);
+            part_rounded = E::add(w2[i / 2], part_rounded);
+        }
+        sum += (t[0] + t[1]) + (t[2] + t[3]);
+        rounded += part_rounded;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const u32x4 w = {w2[ks * 4], w2[ks * 4 + 1], w2[ks * 4 + 2], w2[ks * 4 + 3]};
+#pragma unroll
+            for (int d = 0; d < kDim / 32; ++d) {
+                o[d] = E::mfma(vf[d], __builtin_bit_cast(s16x8, w), o[d]);
+                if (ks == 0) vf[d] = values(1, d);
+            }
+        }
+        wave_lds_fence();
+    };
+    for (;;) {
+        if (ls.valid && ps.valid && lk0 != ls.key_begin && pk != ps.key_begin) {
+            // Inside a stretch: the tile loaded and the one whose page ids are here are of the stretch that is worked on.
+            const uint32_t* table = table_of(ps);
+            for (; pk + kNarrowKeys < ps.key_end; pk += kNarrowKeys) {
+                ld.store(lk, lv);
+                wave_lds_fence();
+                ld.load(a, pk, ps.key_end);
+                ld.pages(a, table, pk + kNarrowKeys, ps.key_end);
+                work(pk - kNarrowKeys);
+            }
+            lk0 = pk - kNarrowKeys;
+        }
+        const Stretch st = ls;
+        const uint32_t k0 = lk0;
+        const bool keys = st.valid && k0 < st.key_end;
+        if (keys) {
+            ld.store(lk, lv);
+            wave_lds_fence();
+        }
+        if (st.valid && k0 == st.key_begin) {
+            if (kAhead) {
+#pragma unroll
+                for (int d = 0; d < kDim / 16; ++d) qf[d] = q_next[d];
+            } else {
+                load_rows(st, qf);
+            }
+        }
+        ls = ps;
+        lk0 = pk;
+        if (ls.valid) {
+            if (kAhead && lk0 == ls.key_begin) load_rows(ls, q_next);
+            if (lk0 < ls.key_end) ld.load(a, lk0, ls.key_end);
+        }
+        pk += kNarrowKeys;
+        if (pk >= ps.key_end || !ps.valid) {
+            ps = next();
+            pk = ps.key_begin;
+        }
+        if (ps.valid && pk < ps.key_end) ld.pages(a, table_of(ps), pk, ps.key_end);
+        if (!st.valid) {  // nothing loaded yet
+            if (!ls.valid && !ps.valid) break;
+            continue;
+        }
+        if (k0 == st.key_begin) {
+            full = min(limit_of(st, st.row0), st.key_end);  // keys that all rows see
+            m = st.row0 + min(col, rows_of(st) - 1u);
+            lim = (int32_t)min(limit_of(st, m), st.key_end);
+#pragma unroll
+            for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+            mc = kNoMax;
+            sum = rounded = 0.f;
+        }
+        if (keys) work(k0);
+        if (k0 + kNarrowKeys < st.key_end) continue;
+
+        // The stretch's end.
+        const uint32_t rows = rows_of(st);
+        if (__builtin_expect(full < st.key_end && !all_finite<kDim>(o), 0)) {  // own tokens: all rows see a prefix
+            Seq it{};
+            it.tok0 = st.tok0;
+            it.nq = st.nq;
+            it.n = st.n;
+            it.causal = 1;
+            it.first_lim = (int32_t)st.n - (int32_t)st.nq + 1;
+            it.table1 = a.own_table + (uint64_t)st.y * a.own_width;
+            only_seen<E, S, kDim, true, true>(a, it, head_kv, st.row0, st.row0 + rows - 1u, st.key_begin, kNarrowKeys, st.key_end, st.key_end, full, o);
+        }
+        const float total = both_sum(sum), total_rounded = both_sum(rounded);
+        if (col < rows) {
+            const bool none = total == 0.f;
+            const float inv = none ? 0.f : 1.f / total_rounded;
+            const uint64_t stride = (uint64_t)a.total_q * a.heads_q;  // of slots
+            const uint64_t to = (uint64_t)(st.slot + (st.own ? a.slots : 0u)) * stride + (uint64_t)(st.tok0 + m / a.group) * a.heads_q + head_kv * a.group + m % a.group;
+            if (half == 0) {
+                a.part_lse[to] = none ? -INFINITY : mc + log2f(total);
+                if (st.ends)  // slots that are left
+                    for (uint32_t z = st.slot + 1u; z < (st.own ? a.own_slots : a.slots); ++z) a.part_lse[to + (uint64_t)(z - st.slot) * stride] = -INFINITY;
+            }
+            if (!none) {
+#pragma unroll
+                for (int d = 0; d < kDim / 32; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        *reinterpret_cast<f32x4*>(a.part_o + to * kDim + few_dim<kDim>(d * 32 + 2 * i) + half * 4u) =
+                            f32x4{o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
+            }
+        }
+        if (!ls.valid) break;
+    }
+    if (ld.bad) atomicOr(a.err, CR_ERR_PAGE);
+}
+
 // One launch of what is not wide: tiles of 128 rows (up to two parts) and the narrow lists' blocks,
 // so that neither waits for the other's last.
 constexpr uint32_t kMixedPerCu = 2;  // blocks that share a compute unit
@@ -1193,16 +1651,28 @@ constexpr uint32_t kMixedPerCu = 2;  // blocks that share a compute unit
 template <typename E, typename S, int kDim, bool kPaged>
 __global__ __launch_bounds__(kThreads, kMixedPerCu) void k_attn_mixed(const Attn a, const Part p0, const Part p1, uint32_t lists)
 {
-    constexpr uint32_t kWide = wide_lds(kWaves, kDim), kNarrow = kWaves * narrow_lds<kDim>();
+    constexpr uint32_t kWide = wide_lds(kWaves, kDim), kNarrow = kWaves * (S::kCoded ? few_lds<kDim>() : narrow_lds<kDim>());
     __shared__ __align__(16) uint16_t lds[kWide > kNarrow ? kWide : kNarrow];
-    __shared__ NarrowLds sh;
+    __shared__ std::conditional_t<S::kCoded, FewLds, NarrowLds> sh;
     const uint32_t wides = p0.blocks + p1.blocks;
     if (blockIdx.x < wides) {
         const bool second = blockIdx.x >= p0.blocks;
         wide_block<E, S, kDim, kPaged, kWaves>(a, second ? p1 : p0, second ? blockIdx.x - p0.blocks : blockIdx.x, lds);
     } else {
-        narrow_block<E, S, kDim, kPaged>(a, lists, blockIdx.x - wides, gridDim.x - wides, lds, sh);
+        if constexpr (S::kCoded) few_block<E, S, kDim>(a, lists, blockIdx.x - wides, gridDim.x - wides, lds, sh);
+        else narrow_block<E, S, kDim, kPaged>(a, lists, blockIdx.x - wides, gridDim.x - wides, lds, sh);
     }
+}
+
+// Lists of few rows over codes alone.
+constexpr uint32_t few_per_cu(int dim) { return dim == 64 ? 3u : 2u; }  // blocks that share a compute unit
+
+template <typename E, typename S, int kDim>
+__global__ __launch_bounds__(kThreads, few_per_cu(kDim)) void k_attn_few(const Attn a, uint32_t lists)
+{
+    __shared__ __align__(16) uint16_t lds[kWaves * few_lds<kDim>()];
+    __shared__ FewLds sh;
+    few_block<E, S, kDim>(a, lists, blockIdx.x, gridDim.x, lds, sh);
 }
 
 // Joins the partial results of a token's rows: 4 elements of a row per thread, kPar threads share the
@@ -1281,6 +1751,7 @@ constexpr uint32_t kSplitMax = 32;
 constexpr uint32_t kLongKeys = 1024;     // mean keys from which blocks of 256 rows pay
 constexpr uint32_t kNarrowParts = 63;    // shares a sequence's keys may fall into
 constexpr uint32_t kShareLeast = 8;      // tiles a narrow block should have
+constexpr uint32_t kFewLeast = 4;        // tiles a wavefront over codes should have
 
 inline uint32_t up_to(uint64_t x, uint32_t m) { return (uint32_t)((x + m - 1u) / m * m); }
 
@@ -1347,6 +1818,43 @@ inline bool narrow_fits(uint64_t rows, uint32_t seqs, uint64_t keys)
     return narrow_most(rows, seqs, keys) < (1ull << 31);
 }
 
+// The same for wavefronts over codes: units are tiles of 32 rows, and a share is a wavefront's.
+constexpr uint32_t kFewParts = 127;
+
+inline uint32_t few_slots(uint64_t keys, uint64_t share, uint32_t* least)
+{
+    const uint64_t tiles = (keys + kNarrowKeys - 1u) / kNarrowKeys;
+    if (tiles * 2u <= share) return 1u;
+    uint64_t parts = (tiles + share - 1u) / share;
+    parts = parts < kFewParts ? parts : kFewParts;
+    const uint32_t need = (uint32_t)((tiles + parts - 1u) / parts);
+    *least = need > *least ? need : *least;
+    return (uint32_t)parts + 1u;
+}
+
+inline uint64_t few_units(uint64_t rows, uint32_t seqs, uint64_t keys)
+{
+    return tiles_of(rows, kFewRowTile, seqs) * (keys / (2u * kNarrowKeys) + kFewStart);
+}
+
+inline uint64_t few_most(uint64_t rows, uint32_t seqs, uint64_t keys)
+{
+    return (rows / kFewRowTile + seqs) * (keys / kNarrowKeys + 1u + kFewStart);
+}
+
+// How a cache's lists of few rows are cut.
+struct Line {
+    bool coded;
+    uint64_t units(uint64_t rows, uint32_t seqs, uint64_t keys) const { return coded ? few_units(rows, seqs, keys) : narrow_units(rows, seqs, keys); }
+    uint64_t most(uint64_t rows, uint32_t seqs, uint64_t keys) const { return coded ? few_most(rows, seqs, keys) : narrow_most(rows, seqs, keys); }
+    bool fits(uint64_t rows, uint32_t seqs, uint64_t keys) const { return most(rows, seqs, keys) < (1ull << 31); }
+    uint32_t slots(uint64_t keys, uint64_t share, uint32_t* least) const { return coded ? few_slots(keys, share, least) : narrow_slots(keys, share, least); }
+    uint64_t shares() const { return coded ? kWaves : 1u; }  // of a block
+    uint32_t least() const { return coded ? kFewLeast : kShareLeast; }
+};
+inline Line line_of(const cr_kv_cache*) { return Line{false}; }
+inline Line line_of(const cr_kvq_cache*) { return Line{true}; }
+
 // Whether every sequence can have a block to itself: shares of kStart units hold one sequence's first
 // unit at most, so with whole sequences (one slot) and as many blocks none works on two. For short ones:
 // a block's wavefronts take four tiles at a time.
@@ -1354,9 +1862,9 @@ constexpr uint32_t kAloneKeys = 512;
 inline bool narrow_alone(uint64_t most, uint64_t keys, uint64_t blocks) { return keys <= kAloneKeys && most <= blocks * kStart; }
 
 // Blocks per key head: what the wide parts of the launch leave of the GPU, at least half of it.
-inline uint64_t narrow_blocks(uint32_t heads_kv, uint64_t wides)
+inline uint64_t narrow_blocks(uint32_t heads_kv, uint64_t wides, uint32_t per_cu = kMixedPerCu)
 {
-    const uint64_t room = kMixedPerCu * (uint64_t)device_cus();
+    const uint64_t room = per_cu * (uint64_t)device_cus();
     return ((wides < room / 2u ? room - wides : room / 2u) + heads_kv - 1u) / heads_kv;
 }
 
@@ -1423,36 +1931,38 @@ Shape shared_shape(const C* c, const cr_attn_shared_args* p)
         return s;
     }
     s.join = true;
+    const Line line = line_of(c);
     uint64_t units = 0, wides = 0;
-    if (rows <= (uint64_t)kFewRows * p->groups && narrow_fits(rows, p->groups, prefix)) {
+    if (rows <= (uint64_t)kFewRows * p->groups && line.fits(rows, p->groups, prefix)) {
         s.lists |= 1u;
-        units += narrow_units(rows, p->groups, prefix);
+        units += line.units(rows, p->groups, prefix);
     } else {
         const Wide w = wide_shape(kGroup, rows, p->groups, c->heads, prefix, c->dim, &s.chunk, &s.slots);
         if (w.rows == 128u) wides += tiles_of(rows, w.rows, p->groups) * s.slots * c->heads;
         s.wide[s.wides++] = w;
     }
-    if (rows <= (uint64_t)kFewRows * p->batch && narrow_fits(rows, p->batch, own)) {
+    if (rows <= (uint64_t)kFewRows * p->batch && line.fits(rows, p->batch, own)) {
         s.lists |= 2u;
-        units += narrow_units(rows, p->batch, own);
+        units += line.units(rows, p->batch, own);
     } else {
         s.wide[s.wides++] = wide_shape(kOwn, rows, p->batch, c->heads, own, c->dim, &s.own_chunk, &s.own_slots);
     }
     if (s.lists) {
-        s.blocks = narrow_blocks(c->heads, wides);
-        s.least = kShareLeast;
-        const uint64_t equal = units / s.blocks, share = equal > kShareLeast ? equal : kShareLeast;
-        if (s.lists & 1u) s.slots = narrow_slots(prefix, share, &s.least);
-        if (s.lists & 2u) s.own_slots = narrow_slots(own, share, &s.least);
-        const uint64_t most = (2u * units + s.least - 1u) / s.least;  // more blocks would have no share
-        const uint64_t all = ((s.lists & 1u) ? narrow_most(rows, p->groups, prefix) : 0u) + ((s.lists & 2u) ? narrow_most(rows, p->batch, own) : 0u);
-        if (narrow_alone(all, (s.lists & 1u) && prefix > own ? prefix : own, s.blocks)) {
+        s.blocks = narrow_blocks(c->heads, wides, line.coded && wides == 0 ? few_per_cu(c->dim) : kMixedPerCu);
+        s.least = line.least();
+        const uint64_t shares = s.blocks * line.shares();
+        const uint64_t equal = units / shares, share = equal > s.least ? equal : s.least;
+        if (s.lists & 1u) s.slots = line.slots(prefix, share, &s.least);
+        if (s.lists & 2u) s.own_slots = line.slots(own, share, &s.least);
+        const uint64_t most = (2u * units + s.least - 1u) / s.least;  // more shares would be empty
+        const uint64_t all = ((s.lists & 1u) ? line.most(rows, p->groups, prefix) : 0u) + ((s.lists & 2u) ? line.most(rows, p->batch, own) : 0u);
+        if (!line.coded && narrow_alone(all, (s.lists & 1u) && prefix > own ? prefix : own, shares)) {
             if (s.lists & 1u) s.slots = 1u;
             if (s.lists & 2u) s.own_slots = 1u;
             s.least = 1u;
             s.blocks = (all + kStart - 1u) / kStart;
-        } else if (most < s.blocks) {
-            s.blocks = most ? most : 1u;
+        } else if (most < shares) {
+            s.blocks = most ? (most + line.shares() - 1u) / line.shares() : 1u;
         }
     }
     return s;
@@ -1480,6 +1990,12 @@ void launch(const Attn& a, const Shape& s, hipStream_t st)
     }
     uint32_t blocks = few[0].blocks + few[1].blocks;
     if (s.lists) blocks += (uint32_t)s.blocks * a.heads_kv;
+    if constexpr (S::kCoded) {
+        if (blocks && !fews) {
+            hipLaunchKernelGGL((k_attn_few<E, S, kDim>), dim3(blocks), dim3(kThreads), 0, st, a, s.lists);
+            blocks = 0;
+        }
+    }
     if (blocks) hipLaunchKernelGGL((k_attn_mixed<E, S, kDim, kPaged>), dim3(blocks), dim3(kThreads), 0, st, a, few[0], few[1], s.lists);
     if (s.join) {
         constexpr uint32_t kPer = kDim / 4;

@@ -41,14 +41,14 @@ __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b)
 
 struct QCall {
     KvqPages c;
-    uint8_t* scale;        // bytes of the layer's scales
+    uint16_t* scale;       // the layer's scales, by pairs
     cr_rows k, v;
     const uint32_t* off;
     const uint32_t* length;
     const uint32_t* table;
     uint32_t total, n, width;
     uint32_t log_span;     // append: tokens of a wave's piece of work
-    uint64_t items;        // append: spans x heads x 2
+    uint64_t items;        // append: spans x heads
     uint32_t* err;
 };
 
@@ -69,128 +69,157 @@ __device__ __forceinline__ void q_check(const QCall& a, uint64_t x)
     if (!q_fits(a, (uint32_t)x, &o0, &o1, &len) || (x == 0 && o0 != 0u) || (x + 1u == a.n && o1 != a.total)) atomicOr(a.err, CR_ERR_SEQ);
 }
 
-// New tokens. A wave takes a span of one head's keys or values: a block, or as many blocks as its lanes hold rows of (4 rows of
-// 128 elements, 8 of 64; a lane has 8 elements of a row). Spans of sequence x start at floor(first row / span) + 2 x: n rows touch at most
-// floor(n / span) + 2 of them, so no pass counts them. The magnitudes' maximum goes over the lanes of a block; rows from
-// before that share a block are rounded again only where its exponent grows.
+// First span of sequence x whose rows start at `first`. n rows touch no more than n spans, nor more than floor(n / span) + 2, so
+// no pass counts them; a decode step has one for each row.
+__host__ __device__ __forceinline__ uint64_t span_start(uint32_t first, uint32_t x, uint32_t log_span)
+{
+    const uint64_t few = (uint64_t)(first >> log_span) + 2u * (uint64_t)x;
+    return few < first ? few : first;
+}
+
+// New tokens. A wave takes a span of one head's keys and values: a block, or as many blocks as its lanes hold rows of (4 rows of
+// 128 elements, 8 of 64; a lane has 8 elements of a row). The magnitudes' maximum goes over the lanes of a block; rows from before that
+// share a block are rounded again only where its exponent grows.
+//
+// Bound by memory: 20,000 new tokens of 8 heads of 128 (104 MB) take 20 us, 5.2 TB/s; by the chain of dependent loads where there are
+// few: a token for each of 256 requests 6 us.
 template <typename T, typename C, int kDim>
 __device__ __forceinline__ void append_span(const QCall& a, uint8_t* ck, uint8_t* cv, uint64_t item)
 {
     constexpr uint32_t kPieces = kDim / 8, kRows = kWave / kPieces;  // lanes of a row, rows of a wave
-    constexpr uint32_t kHold = 8;                                    // steps of rows held in registers
+    constexpr uint32_t kHold = 4;                                    // steps of rows held in registers
     constexpr uint32_t kMostBits = most_bits<T, C>();
     const uint32_t lane = lane_id(), piece = lane % kPieces, row = lane / kPieces;
     const uint32_t bl = a.c.log_block, mask = (1u << a.c.log_tokens) - 1u;
-    const uint32_t plane = (uint32_t)(item & 1u), head = (uint32_t)((item >> 1) % a.c.heads);
-    const uint64_t u = (item >> 1) / a.c.heads;
-    auto start = [&](uint32_t x) { return (uint64_t)(a.off[x] >> a.log_span) + 2u * x; };
+    const uint32_t head = (uint32_t)(item % a.c.heads);
+    const uint64_t u = item / a.c.heads;
+    auto start = [&](uint32_t x) { return span_start(a.off[x], x, a.log_span); };
     const uint32_t x = wave_find(a.n, u, start);
     uint32_t o0, o1, len;
-    if (!q_fits(a, x, &o0, &o1, &len) || o0 == o1 || u < start(x)) return;
+    const bool fits = q_fits(a, x, &o0, &o1, &len);
+    const uint64_t s = span_start(o0, x, a.log_span);
+    if (!fits || o0 == o1 || u < s) return;
     const uint32_t p0 = len - (o1 - o0);  // place of the first new token
-    const uint64_t s0 = ((p0 >> a.log_span) + (u - start(x))) << a.log_span;
+    const uint64_t s0 = ((p0 >> a.log_span) + (u - s)) << a.log_span;
     if (s0 >= len) return;
     // The lane's rows are pos, pos + kRows, ...: in one block, or there is one step. A span ends below 2^32.
     const uint32_t pos = (uint32_t)s0 + row, block = pos >> bl << bl, steps = ((1u << a.log_span) + kRows - 1u) / kRows;
-    const cr_rows& rows = plane ? a.v : a.k;
-    const uint16_t* src = (const uint16_t*)rows.p + (int64_t)head * rows.head_stride + piece * 8u;
     const uint32_t page = a.table[(uint64_t)x * a.width + (min(pos, len - 1u) >> a.c.log_tokens)];
 
-    u32x4 r[kHold];
+    u32x4 r[2][kHold];
     auto is_new = [&](uint32_t step) { return step < steps && pos + step * kRows >= p0 && pos + step * kRows < len; };
     auto load = [&](uint32_t step0) {  // 0 where there is no new token
 #pragma unroll
-        for (uint32_t y = 0; y < kHold; ++y) {
-            r[y] = u32x4{0, 0, 0, 0};
-            if (is_new(step0 + y))
-                r[y] = *reinterpret_cast<const u32x4*>(src + (int64_t)(o0 + (pos + (step0 + y) * kRows - p0)) * rows.token_stride);
+        for (int j = 0; j < 2; ++j) {
+            const cr_rows& rows = j ? a.v : a.k;
+            const uint16_t* src = (const uint16_t*)rows.p + (int64_t)head * rows.head_stride + piece * 8u;
+#pragma unroll
+            for (uint32_t y = 0; y < kHold; ++y) {
+                r[j][y] = u32x4{0, 0, 0, 0};
+                if (is_new(step0 + y))
+                    r[j][y] = *reinterpret_cast<const u32x4*>(src + (int64_t)(o0 + (pos + (step0 + y) * kRows - p0)) * rows.token_stride);
+            }
         }
     };
-    uint32_t top = 0;  // largest magnitudes of the lane's pairs
+    uint32_t top[2] = {0, 0};  // largest magnitudes of the lane's pairs
     auto magnitudes = [&](auto finite) {
 #pragma unroll
-        for (uint32_t y = 0; y < kHold; ++y)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t m = r[y][i] & 0x7FFF7FFFu;
-                if (finite) {
-                    if ((m & 0xFFFFu) >= T::kInf) m &= 0xFFFF0000u;
-                    if ((m >> 16) >= T::kInf) m &= 0xFFFFu;
+            for (uint32_t y = 0; y < kHold; ++y)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t m = r[j][y][i] & 0x7FFF7FFFu;
+                    if (finite) {
+                        if ((m & 0xFFFFu) >= T::kInf) m &= 0xFFFF0000u;
+                        if ((m >> 16) >= T::kInf) m &= 0xFFFFu;
+                    }
+                    top[j] = max_pair(top[j], m);
                 }
-                top = max_pair(top, m);
-            }
     };
     for (uint32_t step0 = 0; step0 < steps; step0 += kHold) {
         load(step0);
         magnitudes(std::false_type{});
     }
-    const bool beyond = ballot((top & 0xFFFFu) > kMostBits || (top >> 16) > kMostBits) != 0;
+    const uint32_t both = max_pair(top[0], top[1]);
+    const bool beyond = ballot((both & 0xFFFFu) > kMostBits || (both >> 16) > kMostBits) != 0;
     if (beyond) {  // an element that is not finite, or larger than any code's
-        top = 0;
+        top[0] = top[1] = 0;
         for (uint32_t step0 = 0; step0 < steps; step0 += kHold) {
             if (steps > kHold) load(step0);
             magnitudes(std::true_type{});
         }
     }
-    top = min(max(top & 0xFFFFu, top >> 16), kMostBits);
-    for (uint32_t y = min((uint32_t)kWave, kPieces << bl) >> 1; y; y >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, (int)y));
+    // of keys in the lower half, of values in the upper
+    uint32_t two = min(max(top[0] & 0xFFFFu, top[0] >> 16), kMostBits) | min(max(top[1] & 0xFFFFu, top[1] >> 16), kMostBits) << 16;
+    for (uint32_t y = min((uint32_t)kWave, kPieces << bl) >> 1; y; y >>= 1) two = max_pair(two, (uint32_t)__shfl_xor((int)two, (int)y));
 
     if (block >= len || block + ((1u << bl) - 1u) < p0) return;  // no new token in the lane's block
     if (page >= a.c.num_pages) {
         atomicOr(a.err, CR_ERR_PAGE);
         return;
     }
-    uint8_t* scale = a.scale + 2u * scale_at(page, a.c.heads, head, block & mask, a.c.log_tokens, bl) + plane;
-    uint8_t* codes = (plane ? cv : ck) + (int64_t)head * a.c.head_stride + (int64_t)page * a.c.page_stride + piece * 8u;
-    auto at = [&](uint32_t p) { return reinterpret_cast<u32x2*>(codes + (int64_t)(p & mask) * a.c.token_stride); };
-    uint32_t e = exponent_of<T, C>(top);
-    if (block < p0) {  // tokens from before
-        const uint32_t e_old = *scale;
-        if (e > e_old) {
-            const float down = scale_of((uint32_t)max((int)(e_old + 127u) - (int)e, 1));  // 2^(e_old - e); below 2^-126 no code is left anyway
-            for (uint32_t p = pos; p < p0; p += kRows) {
-                u32x2 w = *at(p);
+    uint16_t* scale = a.scale + scale_at(page, a.c.heads, head, block & mask, a.c.log_tokens, bl);
+    const uint32_t scale_old = block < p0 ? *scale : 0u;  // tokens from before
+    uint32_t e[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const f32x2 lo = C::template floats<false>(w[i]), hi = C::template floats<true>(w[i]);
-                    w[i] = C::template code<true>(hi[0] * down, hi[1] * down, C::template code<false>(lo[0] * down, lo[1] * down, 0u));
+    for (int j = 0; j < 2; ++j) {
+        uint8_t* codes = (j ? cv : ck) + (int64_t)head * a.c.head_stride + (int64_t)page * a.c.page_stride + piece * 8u;
+        auto at = [&](uint32_t p) { return reinterpret_cast<u32x2*>(codes + (int64_t)(p & mask) * a.c.token_stride); };
+        e[j] = exponent_of<T, C>(j ? two >> 16 : two & 0xFFFFu);
+        if (block < p0) {
+            const uint32_t e_old = j ? scale_old >> 8 : scale_old & 0xFFu;
+            if (e[j] > e_old) {
+                const float down = scale_of((uint32_t)max((int)(e_old + 127u) - (int)e[j], 1));  // 2^(e_old - e); below 2^-126 no code is left anyway
+                for (uint32_t p = pos; p < p0; p += kRows) {
+                    u32x2 w = *at(p);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const f32x2 lo = C::template floats<false>(w[i]), hi = C::template floats<true>(w[i]);
+                        w[i] = C::template code<true>(hi[0] * down, hi[1] * down, C::template code<false>(lo[0] * down, lo[1] * down, 0u));
+                    }
+                    *at(p) = w;
                 }
-                *at(p) = w;
             }
+            e[j] = max(e[j], e_old);
         }
-        e = max(e, e_old);
     }
-    const float up = scale_of(254u - e);  // 2^-(e - 127); e is at most 247
     for (uint32_t step0 = 0; step0 < steps; step0 += kHold) {
         if (steps > kHold) load(step0);
 #pragma unroll
-        for (uint32_t y = 0; y < kHold; ++y) {
-            if (!is_new(step0 + y)) continue;
-            u32x2 out;
+        for (int j = 0; j < 2; ++j) {
+            uint8_t* codes = (j ? cv : ck) + (int64_t)head * a.c.head_stride + (int64_t)page * a.c.page_stride + piece * 8u;
+            const float up = scale_of(254u - e[j]);  // 2^-(e - 127); e is at most 247
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float z[4] = {T::first(r[y][2 * i]), T::second(r[y][2 * i]), T::first(r[y][2 * i + 1]), T::second(r[y][2 * i + 1])};
-                if (beyond) {
-                    const float most = T::first(kMostBits);
+            for (uint32_t y = 0; y < kHold; ++y) {
+                if (!is_new(step0 + y)) continue;
+                u32x2 out;
 #pragma unroll
-                    for (int w = 0; w < 4; ++w)
-                        if (__builtin_fabsf(z[w]) < INFINITY) z[w] = fminf(fmaxf(z[w], -most), most);
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t x0 = r[j][y][2 * i], x1 = r[j][y][2 * i + 1];
+                    float z[4] = {T::first(x0), T::second(x0), T::first(x1), T::second(x1)};
+                    if (beyond) {
+                        const float most = T::first(kMostBits);
+#pragma unroll
+                        for (int w = 0; w < 4; ++w)
+                            if (__builtin_fabsf(z[w]) < INFINITY) z[w] = fminf(fmaxf(z[w], -most), most);
+                    }
+                    out[i] = C::template code<true>(z[2] * up, z[3] * up, C::template code<false>(z[0] * up, z[1] * up, 0u));
                 }
-                out[i] = C::template code<true>(z[2] * up, z[3] * up, C::template code<false>(z[0] * up, z[1] * up, 0u));
+                *reinterpret_cast<u32x2*>(codes + (int64_t)((pos + (step0 + y) * kRows) & mask) * a.c.token_stride) = out;
             }
-            *at(pos + (step0 + y) * kRows) = out;
         }
     }
-    if (piece == 0 && pos == block) *scale = (uint8_t)e;
+    if (piece == 0 && pos == block) *scale = (uint16_t)(e[0] | e[1] << 8);
 }
 
 template <typename T, typename C, int kDim>
 __global__ __launch_bounds__(256) void k_kvq_append(QCall a, uint8_t* ck, uint8_t* cv)
 {
-    const uint64_t waves = (uint64_t)gridDim.x * kQWaves;
-    for (uint64_t item = (uint64_t)blockIdx.x * kQWaves + wave_in_block(); item < a.items; item += waves) {
+    const uint64_t waves = (uint64_t)gridDim.x * kQWaves, end = a.items > a.n ? a.items : a.n;
+    for (uint64_t item = (uint64_t)blockIdx.x * kQWaves + wave_in_block(); item < end; item += waves) {
         q_check(a, item);
-        append_span<T, C, kDim>(a, ck, cv, item);
+        if (item < a.items) append_span<T, C, kDim>(a, ck, cv, item);
     }
 }
 
@@ -239,24 +268,23 @@ __global__ __launch_bounds__(256) void k_kvq_read(QCall a)
 }
 
 // What both calls check; rows of NULL are not looked at where `optional`. CR_OK with a.total 0: nothing to do.
-cr_status q_call(const cr_kvq_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, bool optional, uint32_t total, const uint32_t* off,
-                 const uint32_t* length, uint32_t n, const uint32_t* table, uint32_t width, uint32_t* err, QCall* a)
+cr_status q_call(const cr_kvq_cache* c, const cr_kvq_tokens* t, bool optional, uint32_t* err, QCall* a)
 {
-    if (!good_cache(c) || layer >= c->layers || !err || total >= (1u << 31) || n > (1u << 24) || width > (1u << 28)) return CR_EINVAL;
+    if (!good_cache(c) || !t || t->layer >= c->layers || !err || t->total >= (1u << 31) || t->n > (1u << 24) || t->width > (1u << 28)) return CR_EINVAL;
     *a = QCall{};
-    if (total == 0) return CR_OK;
-    if (n == 0 || !off || !length || (width > 0 && !table)) return CR_EINVAL;
-    if ((!k && !optional) || (!v && !optional) || (k && !good_rows(*k)) || (v && !good_rows(*v))) return CR_EINVAL;
-    a->c = kvq_pages(c, layer);
-    a->scale = c->scale + 2u * (uint64_t)layer * scales_of_layer(c);
-    if (k) a->k = *k;
-    if (v) a->v = *v;
-    a->off = off;
-    a->length = length;
-    a->table = table;
-    a->total = total;
-    a->n = n;
-    a->width = width;
+    if (t->total == 0) return CR_OK;
+    if (t->n == 0 || !t->off || !t->length || (t->width > 0 && !t->table)) return CR_EINVAL;
+    if (((t->k.p || !optional) && !good_rows(t->k)) || ((t->v.p || !optional) && !good_rows(t->v))) return CR_EINVAL;
+    a->c = kvq_pages(c, t->layer);
+    a->scale = const_cast<uint16_t*>(a->c.scale);
+    a->k = t->k;
+    a->v = t->v;
+    a->off = t->off;
+    a->length = t->length;
+    a->table = t->table;
+    a->total = t->total;
+    a->n = t->n;
+    a->width = t->width;
     a->err = err;
     return CR_OK;
 }
@@ -285,19 +313,17 @@ inline uint32_t q_blocks(uint64_t waves)
 }  // namespace
 }  // namespace cr
 
-extern "C" cr_status cr_kvq_append(const cr_kvq_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, uint32_t total,
-                                   const uint32_t* off, const uint32_t* length, uint32_t n, const uint32_t* table,
-                                   uint32_t width, uint32_t* err, void* stream)
+extern "C" cr_status cr_kvq_append(const cr_kvq_cache* c, const cr_kvq_tokens* t, uint32_t* err, void* stream)
 {
     using namespace cr;
     QCall a;
-    const cr_status rc = q_call(c, layer, k, v, false, total, off, length, n, table, width, err, &a);
+    const cr_status rc = q_call(c, t, false, err, &a);
     if (rc != CR_OK || a.total == 0) return rc;
     const uint32_t rows = kWave * 8u / c->dim;  // of a wave
     a.log_span = log2_of(c->block_tokens > rows ? c->block_tokens : rows);
-    a.items = ((uint64_t)(total >> a.log_span) + 2u * (uint64_t)n) * c->heads * 2u;
+    a.items = span_start(a.total, a.n, a.log_span) * c->heads;
     const hipStream_t st = as_stream(stream);
-    const uint32_t blocks = q_blocks(a.items);
+    const uint32_t blocks = q_blocks(a.items > a.n ? a.items : a.n);
     (void)hipGetLastError();
     if (c->dtype == CR_BF16 && c->code == CR_E4M3) append_launch<Bf16Rows, E4m3>(a, blocks, st);
     else if (c->dtype == CR_BF16) append_launch<Bf16Rows, E5m2>(a, blocks, st);
@@ -306,16 +332,14 @@ extern "C" cr_status cr_kvq_append(const cr_kvq_cache* c, uint32_t layer, const 
     return hipGetLastError() == hipSuccess ? CR_OK : CR_EHIP;
 }
 
-extern "C" cr_status cr_kvq_read(const cr_kvq_cache* c, uint32_t layer, const cr_rows* k, const cr_rows* v, uint32_t total,
-                                 const uint32_t* off, const uint32_t* length, uint32_t n, const uint32_t* table,
-                                 uint32_t width, uint32_t* err, void* stream)
+extern "C" cr_status cr_kvq_read(const cr_kvq_cache* c, const cr_kvq_tokens* t, uint32_t* err, void* stream)
 {
     using namespace cr;
     QCall a;
-    const cr_status rc = q_call(c, layer, k, v, true, total, off, length, n, table, width, err, &a);
+    const cr_status rc = q_call(c, t, true, err, &a);
     if (rc != CR_OK || a.total == 0) return rc;
     const hipStream_t st = as_stream(stream);
-    const uint32_t blocks = q_blocks(total > n ? total : n);
+    const uint32_t blocks = q_blocks(a.total > a.n ? a.total : a.n);
     (void)hipGetLastError();
     if (c->dtype == CR_BF16 && c->code == CR_E4M3) read_launch<Bf16Rows, E4m3>(a, blocks, st);
     else if (c->dtype == CR_BF16) read_launch<Bf16Rows, E5m2>(a, blocks, st);

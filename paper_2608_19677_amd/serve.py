@@ -42,7 +42,7 @@ _INT32, _FLOAT32 = torch.int32, torch.float32
 _HERE = contextlib.nullcontext()
 _raw_stream, _device = B._raw_stream, B._device
 _pack_rows, _pack_prompt, _pack_shared, _RANGE = B.ROWS.pack, B.PROMPT_ARGS.pack, B.SHARED_ARGS.pack, (struct.error, OverflowError)
-_pack_rotary = B.ROTARY_ARGS.pack
+_pack_rotary, _pack_tokens = B.ROTARY_ARGS.pack, B.TOKENS_ARGS.pack
 
 
 def _dtype(t: torch.Tensor) -> int:
@@ -278,6 +278,7 @@ class QuantPagePool(PagePool):
         self._device = k.device.index
         self._ready("cr_kvq_", "cr_kvq_append", "cr_kvq_attn", scale)
         self._read = B.load().cr_kvq_read
+        self._head = [self.heads, self.dim]
 
     @classmethod
     def empty(cls, layers: int, num_pages: int, heads: int, page_tokens: int, dim: int, dtype=torch.bfloat16, device="cuda",
@@ -296,23 +297,42 @@ class QuantPagePool(PagePool):
             raise B.CrError(f"the cache is on cuda:{self._device}, the current device is cuda:{_device()}")
         return super()._on(stream)
 
+    def _tokens(self, layer, k, v, off, length, table):
+        """A cr_kvq_tokens of rows [total, heads, dim] of both."""
+        shape, sk, sv, dtype = k.shape, k.stride(), v.stride(), self.dtype
+        if k.dtype is not dtype or v.dtype is not dtype or shape != v.shape or [*shape[1:]] != self._head or sk[2] != 1 or sv[2] != 1:
+            raise B.CrError("rows of keys and values have the cache's heads, dim and type, with dim contiguous")
+        if not (k.is_cuda and v.is_cuda):
+            raise B.CrError("libcr takes device tensors")
+        if (k.requires_grad or v.requires_grad) and _grad_on():
+            _refuse_grad()
+        n = length.numel()
+        p, width = _table(table, n)
+        try:
+            return _pack_tokens(layer, shape[0], n, width, k.data_ptr(), sk[0], sk[1], v.data_ptr(), sv[0], sv[1], _index(off, n + 1), _index(length), p)
+        except _RANGE as e:
+            raise B.CrError(f"an argument is out of range: {e}") from None
+
+    def append(self, layer: int, k, v, off, length, table, stream=None):
+        """Rows off[i]..off[i+1] of k and v ([total, heads, dim]) are rounded into the last tokens of the
+        length[i] of sequence i."""
+        rc = self._append(self._ref, self._tokens(layer, k, v, off, length, table), self._err, self._on(stream))
+        if rc:
+            B._check(rc, "cr_kvq_append")
+
     def read(self, layer: int, k, v, off, length, table, stream=None):
         """The reverse of ``append``: the last tokens of the length[i] of sequence i into rows off[i]..off[i+1] of k and
         v ([total, heads, dim], the cache's dtype; either may be None)."""
-        n, rows, shape = length.numel(), [None, None], None
-        for i, x in enumerate((k, v)):
-            if x is None:
-                continue
-            if x.dim() != 3 or x.shape[1] != self.heads or x.shape[2] != self.dim or x.dtype is not self.dtype or (shape or x.shape) != x.shape:
-                raise B.CrError("rows to read into have the cache's heads, dim and type")
-            if x.requires_grad and _grad_on():
-                _refuse_grad()
-            shape, rows[i] = x.shape, _pack_rows(*_rows(x))
-        if shape is None:
+        if k is None and v is None:
             raise B.CrError("rows of keys or of values are wanted")
-        p, width = _table(table, n)
-        B._check(self._read(self._ref, layer, *rows, shape[0], _index(off, n + 1), _index(length), n, p, width, self._err,
-                            self._on(stream)), "cr_kvq_read")
+        t = self._tokens(layer, v if k is None else k, k if v is None else v, off, length, table)
+        if k is None or v is None:  # the other one's rows have no place
+            f = list(B.TOKENS_ARGS.unpack(t))
+            f[4 if k is None else 7] = 0
+            t = _pack_tokens(*f)
+        rc = self._read(self._ref, t, self._err, self._on(stream))
+        if rc:
+            B._check(rc, "cr_kvq_read")
 
 
 def rotary_frequencies(rotated: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0, length: Optional[int] = None,
@@ -380,45 +400,52 @@ class Rotary(_Memory):
         if not self.freq.is_cuda:
             raise B.CrError("libcr takes device tensors")
         self._device, self._code = self.freq.device.index, _LAYOUTS[layout]
+        self._freq, self._call = self.freq.data_ptr(), B.load().cr_rotary
         super().__init__(self.freq)
 
     def apply(self, q, k, positions, q_out=None, k_out=None, stream=None):
         """q [tokens, heads, dim] and k [tokens, key heads, dim] (or None) turned by ``positions`` (int32 [tokens]; negative ones
         turn back) into q_out and k_out, new tensors if not given; q and k themselves may be given, other tensors must not overlap
         q or k. Returns both."""
-        shape, dtype = q.shape, q.dtype
-        if len(shape) != 3 or shape[2] != self.dim:
+        shape, dtype, dim = q.shape, q.dtype, self.dim
+        code = _DTYPES.get(dtype)
+        if code is None:
+            _dtype(q)
+        if len(shape) != 3 or shape[2] != dim:
             raise B.CrError("rows are [tokens, heads, dim] with the dim of this handle")
-        code = _dtype(q)
+        if q_out is None:
+            q_out = _new_out(q, stream)
+        elif q_out.shape != shape or q_out.dtype is not dtype:
+            raise B.CrError("q_out has q's shape and type")
         if k is None:
             if k_out is not None:
                 raise B.CrError("there are no keys to turn")
             heads_k, keys, keys_out = 0, (0, 0, 0), (0, 0, 0)
         else:
-            if k.dim() != 3 or k.shape[0] != shape[0] or k.shape[2] != self.dim or k.dtype is not dtype:
+            key_shape = k.shape
+            if len(key_shape) != 3 or key_shape[0] != shape[0] or key_shape[2] != dim or k.dtype is not dtype:
                 raise B.CrError("k has q's tokens, dim and type")
-            heads_k, keys = k.shape[1], _rows(k)
-        if _grad_on() and (q.requires_grad or (k is not None and k.requires_grad)):
-            _refuse_grad()
-        queries = _rows(q)
-        if q_out is None:
-            q_out = _new_out(q, stream)
-        if k is not None:
             if k_out is None:
                 k_out = _new_out(k, stream)
-            if k_out.shape != k.shape or k_out.dtype is not dtype:
+            elif k_out.shape != key_shape or k_out.dtype is not dtype:
                 raise B.CrError("k_out has k's shape and type")
-            keys_out = _rows(k_out)
-        if q_out.shape != shape or q_out.dtype is not dtype:
-            raise B.CrError("q_out has q's shape and type")
-        if _device() != self._device:
-            raise B.CrError(f"the frequencies are on cuda:{self._device}, the current device is cuda:{_device()}")
+            if k.requires_grad and _grad_on():
+                _refuse_grad()
+            heads_k, keys = key_shape[1], _rows(k)
+            keys_out = keys if k_out is k else _rows(k_out)
+        if q.requires_grad and _grad_on():
+            _refuse_grad()
+        queries = _rows(q)
         try:
-            a = _pack_rotary(code, shape[1], heads_k, self.dim, self.rotated, self._code, shape[0], self.magnitude, *queries, *keys,
-                             *_rows(q_out), *keys_out, _index(positions, shape[0]), self.freq.data_ptr())
+            a = _pack_rotary(code, shape[1], heads_k, dim, self.rotated, self._code, shape[0], self.magnitude, *queries, *keys,
+                             *(queries if q_out is q else _rows(q_out)), *keys_out, _index(positions, shape[0]), self._freq)
         except _RANGE as e:
             raise B.CrError(f"an argument is out of range: {e}") from None
-        B._check(B.load().cr_rotary(a, self._on(stream)), "cr_rotary")
+        if _device() != self._device:
+            raise B.CrError(f"the frequencies are on cuda:{self._device}, the current device is cuda:{_device()}")
+        rc = self._call(a, self._on(stream))
+        if rc:
+            B._check(rc, "cr_rotary")
         return q_out, k_out
 
 

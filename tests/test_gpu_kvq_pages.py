@@ -171,12 +171,13 @@ def test_binding():
             rows = lambda t: B.CrRows(t.data_ptr(), t.stride(0), t.stride(1))  # noqa: E731
             ws = torch.empty(B.cr_pages_workspace_bytes(30, 2), dtype=torch.uint8, device="cuda")
             B.cr_kvq_extend(pool.c, None, length, table, ws, pool.err)
-            B.cr_kvq_append(pool.c, 0, rows(k), rows(v), 40, off, length, table, pool.err)
+            B.cr_kvq_append(pool.c, B.CrKvqTokens(0, 40, 2, 4, rows(k), rows(v), off.data_ptr(), length.data_ptr(), table.data_ptr()), pool.err)
             B.cr_kvq_fork(pool.c, table, parent, at, child, ws, pool.err)
             B.cr_kvq_free(pool.c, table, length, pool.err)
             B.cr_kvq_compact(pool.c, child, at, child, pool.refs, ws, pool.err)
             B.cr_kvq_copy(pool.c, _i32([0]), _i32([29]), pool.err)
-            B.cr_kvq_read(pool.c, 0, rows(back), None, 27, _i32([0, 20, 27]), at, child, pool.err)
+            some = _i32([0, 20, 27])
+            B.cr_kvq_read(pool.c, B.CrKvqTokens(0, 27, 2, 4, rows(back), B.CrRows(), some.data_ptr(), at.data_ptr(), child.data_ptr()), pool.err)
             a = B.CrAttnSharedArgs(8, 0, 2, 1, 4, 4, 4, 0.1, rows(q), rows(out), None, qo.data_ptr(), go.data_ptr(), child.data_ptr(),
                                    none.data_ptr(), child.data_ptr(), at.data_ptr())
             ws = torch.empty(B.cr_kvq_attn_workspace_bytes(pool.c, a), dtype=torch.uint8, device="cuda")

@@ -31,14 +31,14 @@ BAD_CACHES = [dict(dtype=2), dict(code=2), dict(heads=0), dict(heads=1025), dict
 
 @pytest.mark.parametrize("kw", BAD_CACHES, ids=[str(k) for k in BAD_CACHES])
 def test_every_call_refuses_a_bad_cache(L, kw):  # noqa: F811
-    c, r = ctypes.byref(_cache(**kw)), ctypes.byref(_rows())
+    c = ctypes.byref(_cache(**kw))
     assert L.cr_kvq_extend(c, None, FAKE, 1, FAKE, 4, FAKE, 1 << 20, FAKE, None) == B.CR_EINVAL
     assert L.cr_kvq_fork(c, FAKE, 1, 4, FAKE, FAKE, 1, FAKE + 64, 4, FAKE, 1 << 20, FAKE, None) == B.CR_EINVAL
     assert L.cr_kvq_free(c, FAKE, 4, FAKE, 1, FAKE, None) == B.CR_EINVAL
     assert L.cr_kvq_compact(c, FAKE, FAKE, 1, 4, FAKE, FAKE, FAKE, 1 << 20, FAKE, None) == B.CR_EINVAL
     assert L.cr_kvq_copy(c, FAKE, FAKE, 1, FAKE, None) == B.CR_EINVAL
-    assert L.cr_kvq_append(c, 0, r, r, 1, FAKE, FAKE, 1, FAKE, 4, FAKE, None) == B.CR_EINVAL
-    assert L.cr_kvq_read(c, 0, r, r, 1, FAKE, FAKE, 1, FAKE, 4, FAKE, None) == B.CR_EINVAL
+    assert L.cr_kvq_append(c, ctypes.byref(_tokens()), FAKE, None) == B.CR_EINVAL
+    assert L.cr_kvq_read(c, ctypes.byref(_tokens()), FAKE, None) == B.CR_EINVAL
     assert L.cr_kvq_attn(c, ctypes.byref(_shared()), FAKE, 1 << 40, FAKE, None) == B.CR_EINVAL
 
 
@@ -56,25 +56,30 @@ def test_page_calls_refuse(L):  # noqa: F811
     assert L.cr_kvq_copy(c, None, None, 0, FAKE, None) == B.CR_OK
 
 
+def _tokens(**kw):
+    f = dict(layer=0, total=1, n=1, width=4, k=_rows(), v=_rows(), off=FAKE, length=FAKE, table=FAKE)
+    f.update(kw)
+    return B.CrKvqTokens(**f)
+
+
+BAD_TOKENS = [dict(layer=2), dict(k=_rows(token=100)), dict(v=_rows(FAKE + 2)), dict(v=_rows(head=-8)), dict(off=None), dict(length=None), dict(n=0),
+              dict(table=None), dict(total=1 << 31), dict(n=(1 << 24) + 1), dict(width=(1 << 28) + 1)]
+
+
 @pytest.mark.parametrize("call", ["cr_kvq_append", "cr_kvq_read"])
-def test_rows_of_tokens_refuse(L, call):  # noqa: F811
-    f, c = getattr(L, call), ctypes.byref(_cache())
-    r, off = ctypes.byref(_rows()), ctypes.byref(_rows(token=100))
-    assert f(c, 2, r, r, 1, FAKE, FAKE, 1, FAKE, 4, FAKE, None) == B.CR_EINVAL
-    assert f(c, 0, off, r, 1, FAKE, FAKE, 1, FAKE, 4, FAKE, None) == B.CR_EINVAL
-    assert f(c, 0, r, ctypes.byref(_rows(FAKE + 2)), 1, FAKE, FAKE, 1, FAKE, 4, FAKE, None) == B.CR_EINVAL
-    assert f(c, 0, r, r, 1, None, FAKE, 1, FAKE, 4, FAKE, None) == B.CR_EINVAL
-    assert f(c, 0, r, r, 1, FAKE, None, 1, FAKE, 4, FAKE, None) == B.CR_EINVAL
-    assert f(c, 0, r, r, 1, FAKE, FAKE, 1, None, 4, FAKE, None) == B.CR_EINVAL
-    assert f(c, 0, r, r, 1, FAKE, FAKE, 0, FAKE, 4, FAKE, None) == B.CR_EINVAL
-    assert f(c, 0, r, r, 1, FAKE, FAKE, 1, FAKE, 4, None, None) == B.CR_EINVAL
-    assert f(c, 0, r, r, 1 << 31, FAKE, FAKE, 1, FAKE, 4, FAKE, None) == B.CR_EINVAL
-    assert f(c, 0, r, r, 1, FAKE, FAKE, (1 << 24) + 1, FAKE, 4, FAKE, None) == B.CR_EINVAL
-    assert f(c, 0, r, r, 1, FAKE, FAKE, 1, FAKE, (1 << 28) + 1, FAKE, None) == B.CR_EINVAL
-    assert f(c, 0, r, r, 0, None, None, 0, None, 0, FAKE, None) == B.CR_OK
-    if call == "cr_kvq_append":  # rows to read into may be left out, rows to write may not
-        assert f(c, 0, r, None, 1, FAKE, FAKE, 1, FAKE, 4, FAKE, None) == B.CR_EINVAL
-        assert f(c, 0, None, r, 1, FAKE, FAKE, 1, FAKE, 4, FAKE, None) == B.CR_EINVAL
+@pytest.mark.parametrize("kw", BAD_TOKENS, ids=[next(iter(k)) + str(i) for i, k in enumerate(BAD_TOKENS)])
+def test_tokens_refuse(L, call, kw):  # noqa: F811
+    assert getattr(L, call)(ctypes.byref(_cache()), ctypes.byref(_tokens(**kw)), FAKE, None) == B.CR_EINVAL
+
+
+def test_tokens_of_nothing(L):  # noqa: F811
+    c, none = ctypes.byref(_cache()), ctypes.byref(_tokens(total=0, n=0, width=0, k=_rows(None), v=_rows(None), off=None, length=None, table=None))
+    for f in (L.cr_kvq_append, L.cr_kvq_read):
+        assert f(c, none, FAKE, None) == B.CR_OK
+        assert f(c, none, None, None) == B.CR_EINVAL and f(c, None, FAKE, None) == B.CR_EINVAL
+    # rows to read into may be left out, rows to write may not
+    assert L.cr_kvq_append(c, ctypes.byref(_tokens(v=_rows(None))), FAKE, None) == B.CR_EINVAL
+    assert L.cr_kvq_append(c, ctypes.byref(_tokens(k=_rows(None))), FAKE, None) == B.CR_EINVAL
 
 
 @pytest.mark.parametrize("kw", BAD_SHARED, ids=[next(iter(k)) + str(i) for i, k in enumerate(BAD_SHARED)])
@@ -119,6 +124,8 @@ def test_rotary_of_nothing(L):  # noqa: F811
 def test_struct_layouts_match_header(L):  # noqa: F811
     assert ctypes.sizeof(B.CrKvqCache) == 8 * 4 + 2 * 8 + 4 * 8 + 2 * 8
     assert ctypes.sizeof(B.CrRotaryArgs) == 8 * 4 + 4 * 24 + 2 * 8
+    t = (1, 70, 5, 9, (11, 8, 16), (22, 24, 32), 3, 4, 5)
+    assert B.TOKENS_ARGS.pack(*t[:4], *t[4], *t[5], *t[6:]) == bytes(B.CrKvqTokens(*t))
     v = [(1, 8, 2, 128, 64, 1, 70, 0.25), [(11 * i, 8 * i, 16 * i) for i in range(1, 5)], (3, 4)]
     assert B.ROTARY_ARGS.pack(*v[0], *(x for r in v[1] for x in r), *v[2]) == bytes(B.CrRotaryArgs(*v[0], *v[1], *v[2]))
 
