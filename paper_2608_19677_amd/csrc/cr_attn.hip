@@ -1665,10 +1665,8 @@ __global__ __launch_bounds__(kThreads, kMixedPerCu) void k_attn_mixed(const Attn
 }
 
 // Lists of few rows over codes alone.
-constexpr uint32_t few_per_cu(int dim) { return dim == 64 ? 3u : 2u; }  // blocks that share a compute unit
-
 template <typename E, typename S, int kDim>
-__global__ __launch_bounds__(kThreads, few_per_cu(kDim)) void k_attn_few(const Attn a, uint32_t lists)
+__global__ __launch_bounds__(kThreads, kMixedPerCu) void k_attn_few(const Attn a, uint32_t lists)
 {
     __shared__ __align__(16) uint16_t lds[kWaves * few_lds<kDim>()];
     __shared__ FewLds sh;
@@ -1862,9 +1860,9 @@ constexpr uint32_t kAloneKeys = 512;
 inline bool narrow_alone(uint64_t most, uint64_t keys, uint64_t blocks) { return keys <= kAloneKeys && most <= blocks * kStart; }
 
 // Blocks per key head: what the wide parts of the launch leave of the GPU, at least half of it.
-inline uint64_t narrow_blocks(uint32_t heads_kv, uint64_t wides, uint32_t per_cu = kMixedPerCu)
+inline uint64_t narrow_blocks(uint32_t heads_kv, uint64_t wides)
 {
-    const uint64_t room = per_cu * (uint64_t)device_cus();
+    const uint64_t room = kMixedPerCu * (uint64_t)device_cus();
     return ((wides < room / 2u ? room - wides : room / 2u) + heads_kv - 1u) / heads_kv;
 }
 
@@ -1948,7 +1946,7 @@ Shape shared_shape(const C* c, const cr_attn_shared_args* p)
         s.wide[s.wides++] = wide_shape(kOwn, rows, p->batch, c->heads, own, c->dim, &s.own_chunk, &s.own_slots);
     }
     if (s.lists) {
-        s.blocks = narrow_blocks(c->heads, wides, line.coded && wides == 0 ? few_per_cu(c->dim) : kMixedPerCu);
+        s.blocks = narrow_blocks(c->heads, wides);
         s.least = line.least();
         const uint64_t shares = s.blocks * line.shares();
         const uint64_t equal = units / shares, share = equal > s.least ? equal : s.least;

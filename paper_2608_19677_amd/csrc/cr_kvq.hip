@@ -206,7 +206,7 @@ __device__ __forceinline__ void append_span(const QCall& a, uint8_t* ck, uint8_t
                     }
                     out[i] = C::template code<true>(z[2] * up, z[3] * up, C::template code<false>(z[0] * up, z[1] * up, 0u));
                 }
-                *reinterpret_cast<u32x2*>(codes + (int64_t)((pos + (step0 + y) * kRows) & mask) * a.c.token_stride) = out;
+                __builtin_nontemporal_store(out, reinterpret_cast<u32x2*>(codes + (int64_t)((pos + (step0 + y) * kRows) & mask) * a.c.token_stride));
             }
         }
     }
@@ -224,6 +224,9 @@ __global__ __launch_bounds__(256) void k_kvq_append(QCall a, uint8_t* ck, uint8_
 }
 
 // Tokens read back: a wave takes a token's keys and values of all heads, a lane 8 elements of a head at a time.
+//
+// Bound by memory: 180,000 tokens of 8 heads of 128 (370 MB read, 740 written) take 254 us, 4.4 TB/s (274 with ordinary loads and
+// stores); 37 tokens 3 us.
 template <typename T, typename C, int kDim>
 __global__ __launch_bounds__(256) void k_kvq_read(QCall a)
 {
@@ -251,7 +254,7 @@ __global__ __launch_bounds__(256) void k_kvq_read(QCall a)
             for (uint32_t i = 0; i < kAhead; ++i) {
                 const uint32_t z = z0 + i * kWave + lane_id(), p = z < per ? z : z - per, h = p / kPieces;
                 if (z >= last) continue;
-                w[i] = *reinterpret_cast<const u32x2*>((z < per ? a.c.k : a.c.v) + from + (int64_t)h * a.c.head_stride + p % kPieces * 8u);
+                w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>((z < per ? a.c.k : a.c.v) + from + (int64_t)h * a.c.head_stride + p % kPieces * 8u));
                 const uint32_t two = a.c.scale[scale_at(page, a.c.heads, h, pos & mask, a.c.log_tokens, a.c.log_block)];
                 e[i] = z < per ? two & 0xFFu : two >> 8;
             }
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(256) void k_kvq_read(QCall a)
                 if (z >= last) continue;
                 const cr_rows& rows = z < per ? a.k : a.v;
                 uint16_t* to = (uint16_t*)rows.p + (int64_t)tok * rows.token_stride + (int64_t)h * rows.head_stride + p % kPieces * 8u;
-                *reinterpret_cast<u32x4*>(to) = wide_of<C, typename T::Pair>(w[i], scale_of(e[i]));
+                __builtin_nontemporal_store((wide_of<C, typename T::Pair>(w[i], scale_of(e[i]))), reinterpret_cast<u32x4*>(to));
             }
         }
     }

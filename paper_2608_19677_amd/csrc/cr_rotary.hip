@@ -12,14 +12,13 @@ namespace {
 constexpr uint32_t kRotThreads = 256;
 constexpr uint32_t kRotWaves = kRotThreads / kWave;
 constexpr uint32_t kRotBlocks = 1u << 20;  // of a launch; waves take more work in turn
-constexpr uint32_t kRotFill = 8192;        // waves that fill the GPU: a token's heads go to several where there are fewer tokens
 
 struct Rot {
     cr_rows q, k, q_out, k_out;
     const int32_t* positions;
     const uint64_t* freq;
     uint32_t heads_q, heads, rotated, pairs;  // heads: of queries and keys; pairs: layout
-    uint32_t total, parts;                    // parts: waves that share a token's heads
+    uint32_t total, steps;                    // steps: waves that share a token's heads
     uint32_t in_place_q, in_place_k;
     float magnitude;
 };
@@ -31,8 +30,12 @@ __device__ __forceinline__ uint32_t turned(float x, float z, float c, float s)
     return pack_pair<T>(__builtin_fmaf(x, c, -(z * s)), __builtin_fmaf(z, c, x * s));
 }
 
-// A wave takes a token and some of its heads, 8 (dim 128) or 16 (dim 64) at a time; a lane two pieces of 8 elements of a
-// head: 8 pairs, whose cosines and sines it computes once, or 16 elements that are only copied.
+// A wave takes 8 (dim 128) or 16 (dim 64) heads of a token; a lane two pieces of 8 elements of a head: 8 pairs, or 16
+// elements that are only copied. Cosines and sines are computed again for every such step of heads: what else the vector units have
+// to do is little, and waves that take several steps one after the other are slower.
+//
+// Bound by memory: 16,384 tokens of 64 heads and 8 key heads of 128 (604 MB read and written) take 104 us, 5.8 TB/s (124 with ordinary
+// loads and stores and a quarter of the waves: what is written is not kept in the cache's way); a token by the launch, 3 us.
 template <typename T, int kDim>
 __global__ __launch_bounds__(256) void k_rotary(const Rot a)
 {
@@ -40,46 +43,41 @@ __global__ __launch_bounds__(256) void k_rotary(const Rot a)
     const uint32_t lane = lane_id(), y = lane % kLanes, head0 = lane / kLanes;
     const bool turns = y < a.rotated / 16u;
     const uint32_t ea = turns && !a.pairs ? y * 8u : y * 16u, eb = turns && !a.pairs ? ea + a.rotated / 2u : ea + 8u;
-    const uint64_t waves = (uint64_t)gridDim.x * kRotWaves, items = (uint64_t)a.total * a.parts;
+    const uint64_t waves = (uint64_t)gridDim.x * kRotWaves, items = (uint64_t)a.total * a.steps;
     for (uint64_t item = (uint64_t)blockIdx.x * kRotWaves + wave_in_block(); item < items; item += waves) {
-        const uint32_t tok = (uint32_t)(item / a.parts), part = (uint32_t)(item % a.parts);
-        float c[8], s[8];
+        const uint32_t tok = (uint32_t)(item / a.steps), h = (uint32_t)(item % a.steps) * kHeads + head0;
+        if (h >= a.heads) continue;
+        const bool is_q = h < a.heads_q;
+        if (!turns && (is_q ? a.in_place_q : a.in_place_k)) continue;
+        const uint32_t hh = is_q ? h : h - a.heads_q;
+        const cr_rows &in = is_q ? a.q : a.k, &to = is_q ? a.q_out : a.k_out;
+        const uint16_t* from = (const uint16_t*)in.p + (int64_t)tok * in.token_stride + (int64_t)hh * in.head_stride;
+        uint16_t* out = (uint16_t*)to.p + (int64_t)tok * to.token_stride + (int64_t)hh * to.head_stride;
+        u32x4 ra = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from + ea)), rb = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from + eb));
         if (turns) {
             const uint64_t pos = (uint64_t)(int64_t)a.positions[tok];
+            float c[8], s[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float t = (float)(int32_t)((pos * a.freq[y * 8u + i]) >> 32) * 0x1p-32f;
                 c[i] = __builtin_amdgcn_cosf(t) * a.magnitude;
                 s[i] = __builtin_amdgcn_sinf(t) * a.magnitude;
             }
-        }
-        for (uint32_t h0 = part * kHeads; h0 < a.heads; h0 += a.parts * kHeads) {
-            const uint32_t h = h0 + head0;
-            if (h >= a.heads) continue;
-            const bool is_q = h < a.heads_q;
-            if (!turns && (is_q ? a.in_place_q : a.in_place_k)) continue;
-            const uint32_t hh = is_q ? h : h - a.heads_q;
-            const cr_rows &in = is_q ? a.q : a.k, &to = is_q ? a.q_out : a.k_out;
-            const uint16_t* from = (const uint16_t*)in.p + (int64_t)tok * in.token_stride + (int64_t)hh * in.head_stride;
-            uint16_t* out = (uint16_t*)to.p + (int64_t)tok * to.token_stride + (int64_t)hh * to.head_stride;
-            u32x4 ra = *reinterpret_cast<const u32x4*>(from + ea), rb = *reinterpret_cast<const u32x4*>(from + eb);
-            if (turns) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (a.pairs) {
-                        ra[i] = turned<T>(T::first(ra[i]), T::second(ra[i]), c[i], s[i]);
-                        rb[i] = turned<T>(T::first(rb[i]), T::second(rb[i]), c[4 + i], s[4 + i]);
-                    } else {
-                        const float x[2] = {T::first(ra[i]), T::second(ra[i])}, z[2] = {T::first(rb[i]), T::second(rb[i])};
-                        const float c0 = c[2 * i], s0 = s[2 * i], c1 = c[2 * i + 1], s1 = s[2 * i + 1];
-                        ra[i] = pack_pair<T>(__builtin_fmaf(x[0], c0, -(z[0] * s0)), __builtin_fmaf(x[1], c1, -(z[1] * s1)));
-                        rb[i] = pack_pair<T>(__builtin_fmaf(z[0], c0, x[0] * s0), __builtin_fmaf(z[1], c1, x[1] * s1));
-                    }
+            for (int i = 0; i < 4; ++i) {
+                if (a.pairs) {
+                    ra[i] = turned<T>(T::first(ra[i]), T::second(ra[i]), c[i], s[i]);
+                    rb[i] = turned<T>(T::first(rb[i]), T::second(rb[i]), c[4 + i], s[4 + i]);
+                } else {
+                    const float x[2] = {T::first(ra[i]), T::second(ra[i])}, z[2] = {T::first(rb[i]), T::second(rb[i])};
+                    const float c0 = c[2 * i], s0 = s[2 * i], c1 = c[2 * i + 1], s1 = s[2 * i + 1];
+                    ra[i] = pack_pair<T>(__builtin_fmaf(x[0], c0, -(z[0] * s0)), __builtin_fmaf(x[1], c1, -(z[1] * s1)));
+                    rb[i] = pack_pair<T>(__builtin_fmaf(z[0], c0, x[0] * s0), __builtin_fmaf(z[1], c1, x[1] * s1));
                 }
             }
-            *reinterpret_cast<u32x4*>(out + ea) = ra;
-            *reinterpret_cast<u32x4*>(out + eb) = rb;
         }
+        __builtin_nontemporal_store(ra, reinterpret_cast<u32x4*>(out + ea));
+        __builtin_nontemporal_store(rb, reinterpret_cast<u32x4*>(out + eb));
     }
 }
 
@@ -111,10 +109,9 @@ extern "C" cr_status cr_rotary(const cr_rotary_args* p, void* stream)
         return CR_EINVAL;
     Rot a{p->q, p->k, p->q_out, p->k_out, p->positions, p->freq, p->heads_q, p->heads_q + p->heads_k, p->rotated, p->layout, p->total, 1,
           same_rows(p->q, p->q_out), p->heads_k && same_rows(p->k, p->k_out), p->magnitude};
-    const uint32_t heads = kWave * 16u / p->dim, steps = (a.heads + heads - 1u) / heads;  // of a wave's step; steps of a token
-    const uint64_t want = ((uint64_t)kRotFill + p->total - 1u) / p->total;
-    a.parts = (uint32_t)(want < steps ? want : steps);
-    const uint64_t waves = (uint64_t)a.total * a.parts, need = (waves + kRotWaves - 1u) / kRotWaves;
+    const uint32_t heads = kWave * 16u / p->dim;  // of a wave
+    a.steps = (a.heads + heads - 1u) / heads;
+    const uint64_t need = ((uint64_t)a.total * a.steps + kRotWaves - 1u) / kRotWaves;
     const uint32_t blocks = (uint32_t)(need < kRotBlocks ? need : kRotBlocks);
     const hipStream_t st = as_stream(stream);
     (void)hipGetLastError();
