@@ -1256,18 +1256,29 @@ struct FewLoader {
 #pragma unroll
         for (uint32_t p = 0; p < kPer; ++p) page[p] = table[min(k0 + p * kStep + row, end - 1u) >> a.pg.log_tokens];
     }
-    __device__ __forceinline__ void load(const Attn& a, uint32_t k0, uint32_t end)
+    // once: nobody else reads the tile, which then need not stay in the caches (128 requests' own tokens, 270 MB, 85 -> 75 us). Where a
+    // row is less than a line, the head beside it reads the line too.
+    __device__ __forceinline__ void load(const Attn& a, uint32_t k0, uint32_t end, bool once)
+    {
+        if (kDim == 128 && once) load_as<true>(a, k0, end);
+        else load_as<false>(a, k0, end);
+    }
+    template <bool kOnce>
+    __device__ __forceinline__ void load_as(const Attn& a, uint32_t k0, uint32_t end)
     {
         const uint32_t mask = (1u << a.pg.log_tokens) - 1u, page_scales = a.pg.heads << (a.pg.log_tokens - a.log_block);
+        if (kOnce) asm volatile("");  // the compiler would join the two forms, and drop the hint
 #pragma unroll
         for (uint32_t p = 0; p < kPer; ++p) {
             const uint32_t tok = min(k0 + p * kStep + row, end - 1u) & mask, g = min(page[p], a.pg.num_pages - 1u);
             bad |= page[p] >= a.pg.num_pages;
             const uint64_t at = (uint64_t)g * (uint32_t)a.pg.page_stride + (uint64_t)tok * (uint32_t)a.pg.token_stride;
-            rk[p] = *reinterpret_cast<const u32x4*>(kb + at);
-            rv[p] = *reinterpret_cast<const u32x4*>(vb + at);
+            const u32x4 *k = reinterpret_cast<const u32x4*>(kb + at), *v = reinterpret_cast<const u32x4*>(vb + at);
+            rk[p] = kOnce ? __builtin_nontemporal_load(k) : *k;
+            rv[p] = kOnce ? __builtin_nontemporal_load(v) : *v;
             rs[p] = sb[(uint64_t)g * page_scales + (tok >> a.log_block)];
         }
+        if (kOnce) asm volatile("");
     }
     __device__ __forceinline__ void store(uint16_t* lk, uint16_t* lv) const
     {
@@ -1289,12 +1300,12 @@ struct FewLoader {
 template <typename E, typename S, int kDim>
 __device__ CR_INLINE void few_block(const Attn& a, uint32_t lists, uint32_t block, uint32_t blocks, uint16_t* lds, FewLds& sh)
 {
-    // All heads of a share on one XCD, side by side: where heads lie next to each other in a token a head's row may be less than a line of
-    // the L2.
+    // All heads of a share side by side, on one XCD: where heads lie next to each other in a token a head's row may be less than a line of
+    // the caches.
     if (blocks % kXcds == 0u) block = xcd_tile(block, blocks);
     constexpr uint32_t kKeyRun = key_run(kNarrowKeys), kValRun = val_run(kNarrowKeys);
     const uint32_t lane = lane_id(), wv = wave_in_block(), half = lane >> 5, col = lane & 31u;
-    const uint32_t head_kv = block % a.heads_kv;
+    const uint32_t wave = block * kWaves + wv, head_kv = wave % a.heads_kv;
     uint16_t* lk = lds + wv * few_lds<kDim>();
     uint16_t* lv = lk + key_tile(kNarrowKeys, kDim);
 
@@ -1325,7 +1336,7 @@ __device__ CR_INLINE void few_block(const Attn& a, uint32_t lists, uint32_t bloc
             sh.seq[i + j] = u32x4{before + (j ? r.v[0] : 0u), r.tok0[j], r.nq[j], r.n[j]};
         }
     };
-    const uint32_t index = block / a.heads_kv * kWaves + wv, of = blocks / a.heads_kv * kWaves;
+    const uint32_t index = wave / a.heads_kv, of = blocks * kWaves / a.heads_kv;
     uint32_t all, base = 0, x0 = 0, here, share;
     auto window = [&](uint32_t x) CR_INLINE {  // a wavefront's own
         const Pair r = pair_at(x + lane * 2u);
@@ -1478,6 +1489,7 @@ __device__ CR_INLINE void few_block(const Attn& a, uint32_t lists, uint32_t bloc
     auto table_of = [&](const Stretch& st) CR_INLINE {
         return st.own ? a.own_table + (uint64_t)st.y * a.own_width : a.prefix_table + (uint64_t)st.y * a.prefix_width;
     };
+    auto once_of = [&](const Stretch& st) CR_INLINE { return st.own && st.nq * a.group <= kFewRowTile; };
     auto load_rows = [&](const Stretch& st, auto& q) CR_INLINE {
         const uint32_t x = st.row0 + min(col, rows_of(st) - 1u);
         const uint16_t* qp = (const uint16_t*)a.q.p + (int64_t)(st.tok0 + x / a.group) * a.q.token_stride +
@@ -1556,7 +1568,7 @@ __device__ CR_INLINE void few_block(const Attn& a, uint32_t lists, uint32_t bloc
             for (; pk + kNarrowKeys < ps.key_end; pk += kNarrowKeys) {
                 ld.store(lk, lv);
                 wave_lds_fence();
-                ld.load(a, pk, ps.key_end);
+                ld.load(a, pk, ps.key_end, once_of(ps));
                 ld.pages(a, table, pk + kNarrowKeys, ps.key_end);
                 work(pk - kNarrowKeys);
             }
@@ -1581,7 +1593,7 @@ __device__ CR_INLINE void few_block(const Attn& a, uint32_t lists, uint32_t bloc
         lk0 = pk;
         if (ls.valid) {
             if (kAhead && lk0 == ls.key_begin) load_rows(ls, q_next);
-            if (lk0 < ls.key_end) ld.load(a, lk0, ls.key_end);
+            if (lk0 < ls.key_end) ld.load(a, lk0, ls.key_end, once_of(ls));
         }
         pk += kNarrowKeys;
         if (pk >= ps.key_end || !ps.valid) {
