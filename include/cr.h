@@ -576,7 +576,8 @@ cr_status cr_attn_shared(const cr_kv_cache* c, const cr_attn_shared_args* a, voi
  * anything). Finite elements beyond the largest one that both types have (1.875 * 2^127 for CR_BF16,
  * 1.875 * 2^15 for CR_F16 with CR_E4M3; 1.75 instead of 1.875 with CR_E5M2) are held as that one. A value
  * that is not finite is held as NaN with CR_E4M3 and as itself with CR_E5M2.
- * Powers of two, so that a code stands for an element of 16 bits exactly (CR_F16: but for those below 2^-24).
+ * Powers of two, so that a code stands for an element of 16 bits exactly (but for those below the type's smallest,
+ * which are rounded to it when they are read).
  * ------------------------------------------------------------------------------------- */
 #define CR_E4M3 0u
 #define CR_E5M2 1u
@@ -630,7 +631,7 @@ typedef struct {
 /* cr_kv_append for this cache: the rows are rounded into the tokens, with scales as above; tokens from before are those of the
  * sequence's first length[i] - (off[i+1] - off[i]). Errors as there (offsets out of order set CR_ERR_SEQ, and any
  * sequence may then be skipped); sequences must not name the same page for the tokens they write, nor one that
- * another table's row goes on reading. */
+ * another table's row goes on reading. Heads times min(total, total / max(block_tokens, 512 / dim) + 2 n) < 2^32. */
 cr_status cr_kvq_append(const cr_kvq_cache* c, const cr_kvq_tokens* t, uint32_t* err, void* stream);
 
 /* The reverse: the tokens into the rows. k.p or v.p (or both) may be NULL. Errors as cr_kvq_append; rows of
@@ -650,7 +651,8 @@ cr_status cr_kvq_attn(const cr_kvq_cache* c, const cr_attn_shared_args* a, void*
  * m = magnitude; the pair is elements i and i + rotated / 2 (CR_ROTARY_HALF) or 2 i and 2 i + 1
  * (CR_ROTARY_PAIRS). Other elements are copied. Computed in fp32 and rounded once; cosines and sines are
  * within 2^-22. Positions are i32; negative ones turn back. freq u64 [rotated / 2], 8-byte aligned: radians per position / (2 pi)
- * * 2^64, rounded. q_out and k_out are q and k (same pointer and strides), or do not overlap any input.
+ * * 2^64, rounded. q_out and k_out are q and k (same pointer and strides; CR_EINVAL for other
+ * strides), or do not overlap any input.
  * heads_k may be 0. total * (heads_q + heads_k) < 2^31. */
 #define CR_ROTARY_HALF 0u
 #define CR_ROTARY_PAIRS 1u

@@ -48,7 +48,7 @@ struct QCall {
     const uint32_t* table;
     uint32_t total, n, width;
     uint32_t log_span;     // append: tokens of a wave's piece of work
-    uint64_t items;        // append: spans x heads
+    uint32_t items;        // append: spans x heads
     uint32_t* err;
 };
 
@@ -84,15 +84,14 @@ __host__ __device__ __forceinline__ uint64_t span_start(uint32_t first, uint32_t
 // Bound by memory: 20,000 new tokens of 8 heads of 128 (104 MB) take 20 us, 5.2 TB/s; by the chain of dependent loads where there are
 // few: a token for each of 256 requests 6 us.
 template <typename T, typename C, int kDim>
-__device__ __forceinline__ void append_span(const QCall& a, uint8_t* ck, uint8_t* cv, uint64_t item)
+__device__ __forceinline__ void append_span(const QCall& a, uint8_t* ck, uint8_t* cv, uint32_t item)
 {
     constexpr uint32_t kPieces = kDim / 8, kRows = kWave / kPieces;  // lanes of a row, rows of a wave
     constexpr uint32_t kHold = 4;                                    // steps of rows held in registers
     constexpr uint32_t kMostBits = most_bits<T, C>();
     const uint32_t lane = lane_id(), piece = lane % kPieces, row = lane / kPieces;
     const uint32_t bl = a.c.log_block, mask = (1u << a.c.log_tokens) - 1u;
-    const uint32_t head = (uint32_t)(item % a.c.heads);
-    const uint64_t u = item / a.c.heads;
+    const uint32_t u = item / a.c.heads, head = item % a.c.heads;
     auto start = [&](uint32_t x) { return span_start(a.off[x], x, a.log_span); };
     const uint32_t x = wave_find(a.n, u, start);
     uint32_t o0, o1, len;
@@ -216,10 +215,10 @@ __device__ __forceinline__ void append_span(const QCall& a, uint8_t* ck, uint8_t
 template <typename T, typename C, int kDim>
 __global__ __launch_bounds__(256) void k_kvq_append(QCall a, uint8_t* ck, uint8_t* cv)
 {
-    const uint64_t waves = (uint64_t)gridDim.x * kQWaves, end = a.items > a.n ? a.items : a.n;
-    for (uint64_t item = (uint64_t)blockIdx.x * kQWaves + wave_in_block(); item < end; item += waves) {
+    const uint32_t waves = gridDim.x * kQWaves, end = max(a.items, a.n);
+    for (uint64_t item = blockIdx.x * kQWaves + wave_in_block(); item < end; item += waves) {
         q_check(a, item);
-        if (item < a.items) append_span<T, C, kDim>(a, ck, cv, item);
+        if (item < a.items) append_span<T, C, kDim>(a, ck, cv, (uint32_t)item);
     }
 }
 
@@ -324,7 +323,9 @@ extern "C" cr_status cr_kvq_append(const cr_kvq_cache* c, const cr_kvq_tokens* t
     if (rc != CR_OK || a.total == 0) return rc;
     const uint32_t rows = kWave * 8u / c->dim;  // of a wave
     a.log_span = log2_of(c->block_tokens > rows ? c->block_tokens : rows);
-    a.items = span_start(a.total, a.n, a.log_span) * c->heads;
+    const uint64_t items = span_start(a.total, a.n, a.log_span) * c->heads;
+    if (items >= (1ull << 32)) return CR_EINVAL;
+    a.items = (uint32_t)items;
     const hipStream_t st = as_stream(stream);
     const uint32_t blocks = q_blocks(a.items > a.n ? a.items : a.n);
     (void)hipGetLastError();

@@ -88,9 +88,9 @@ void rotary_launch(const Rot& a, uint32_t dim, uint32_t blocks, hipStream_t st)
     else hipLaunchKernelGGL((k_rotary<T, 64>), dim3(blocks), dim3(kRotThreads), 0, st, a);
 }
 
-inline bool same_rows(const cr_rows& x, const cr_rows& y)
+inline bool same_rows(const cr_rows& x, const cr_rows& y, uint32_t tokens, uint32_t heads)
 {
-    return x.p == y.p && x.token_stride == y.token_stride && x.head_stride == y.head_stride;
+    return x.p == y.p && (tokens == 1 || x.token_stride == y.token_stride) && (heads == 1 || x.head_stride == y.head_stride);
 }
 
 }  // namespace
@@ -108,7 +108,8 @@ extern "C" cr_status cr_rotary(const cr_rotary_args* p, void* stream)
         !aligned4(p->positions) || !p->freq || ((uintptr_t)p->freq & 7u) != 0)
         return CR_EINVAL;
     Rot a{p->q, p->k, p->q_out, p->k_out, p->positions, p->freq, p->heads_q, p->heads_q + p->heads_k, p->rotated, p->layout, p->total, 1,
-          same_rows(p->q, p->q_out), p->heads_k && same_rows(p->k, p->k_out), p->magnitude};
+          same_rows(p->q, p->q_out, p->total, p->heads_q), p->heads_k && same_rows(p->k, p->k_out, p->total, p->heads_k), p->magnitude};
+    if ((p->q.p == p->q_out.p && !a.in_place_q) || (p->heads_k && p->k.p == p->k_out.p && !a.in_place_k)) return CR_EINVAL;  // over itself
     const uint32_t heads = kWave * 16u / p->dim;  // of a wave
     a.steps = (a.heads + heads - 1u) / heads;
     const uint64_t need = ((uint64_t)a.total * a.steps + kRotWaves - 1u) / kRotWaves;

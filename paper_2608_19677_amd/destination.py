@@ -11,10 +11,13 @@ A batch of requests in arrival order:
   decode one token;
 * the requests' own pages are freed again.
 
+The cache holds 16-bit elements, or 8-bit floats (``codes``: twice the prefixes in the same memory); with ``rotary``
+queries and keys are turned by their positions, a request's following its prefix's.
+
 Keys and values come from ``project`` (a model's layer; here a seeded stand-in). The hits and
 prefill tokens counted on the way are the replay's statistics of that destination.
 
-  python -m paper_2608_19677_amd.destination [--requests N] [--batch B]
+  python -m paper_2608_19677_amd.destination [--requests N] [--batch B] [--codes e4m3] [--rotary]
 """
 from __future__ import annotations
 
@@ -23,7 +26,7 @@ import math
 import time
 from collections import OrderedDict
 from dataclasses import dataclass
-from typing import List
+from typing import List, Optional
 
 import numpy as np
 import torch
@@ -63,14 +66,18 @@ class Destination:
 
     def __init__(self, W: int, max_prefix: int, max_suffix: int, batch: int, *, layers: int = 1, heads_q: int = 64,
                  heads_kv: int = 8, dim: int = 128, page_tokens: int = 16, samples: int = 0, dtype=torch.bfloat16,
-                 device="cuda", project=None):
+                 device="cuda", project=None, codes: Optional[torch.dtype] = None, rotary: Optional[serve.Rotary] = None):
         self.W, self.batch, self.layers, self.samples, self.device = W, batch, layers, samples, device
         self.scale = 1.0 / math.sqrt(dim)
         up = lambda n: -(-n // page_tokens)  # noqa: E731
         self.width, self.own_width = up(max_prefix), up(max_suffix + 1)
         rows = W + batch  # prefixes of a batch stay until it is done
         pages = rows * self.width + batch * (1 + samples) * self.own_width
-        self.pool = serve.PagePool.empty(layers, pages, heads_kv, page_tokens, dim, dtype, device)
+        self.rotary = rotary
+        if codes is None:
+            self.pool = serve.PagePool.empty(layers, pages, heads_kv, page_tokens, dim, dtype, device)
+        else:
+            self.pool = serve.QuantPagePool.empty(layers, pages, heads_kv, page_tokens, dim, dtype, device, codes=codes)
         self.table = torch.full((rows, self.width), -1, dtype=torch.int32, device=device)
         self.rows: List[int] = list(range(rows))       # free rows of the table
         self.length = np.zeros(rows, dtype=np.int64)   # tokens of each row's prefix
@@ -124,6 +131,18 @@ class Destination:
         self._check()
         return hit, order, out
 
+    def _positions(self, first, lengths):
+        """Positions of packed tokens, lengths[i] of them from first[i] on; None without rotary."""
+        if self.rotary is None:
+            return None
+        return self._i32(np.concatenate([np.arange(n) + a for a, n in zip(first, lengths)]))
+
+    def _project(self, layer, ids, lengths, positions):
+        q, k, v = self.project(layer, ids, lengths)
+        if positions is not None:
+            q, k = self.rotary.apply(q, k, positions)
+        return q, k, v
+
     def _check(self):
         bits = int(self.pool.err.item())
         if bits:
@@ -135,9 +154,9 @@ class Destination:
         table = torch.full((len(missed), self.width), -1, dtype=torch.int32, device=self.device)
         n, off = self._i32(lengths), self._i32(self._off(lengths))
         self.pool.extend(table, None, n)
-        out = None
+        out, pos = None, self._positions(np.zeros(len(lengths), dtype=np.int64), lengths)
         for layer in range(self.layers):
-            q, k, v = self.project(layer, [key for key, _ in missed], lengths)
+            q, k, v = self._project(layer, [key for key, _ in missed], lengths, pos)
             out = serve.attend_prompt(q, k, v, off, off, self.scale, err=self.pool.err)
             self.pool.append(layer, k, v, off, n, table)
         self.table[rows] = table
@@ -151,17 +170,19 @@ class Destination:
         n, off = self._i32(suffix), self._i32(self._off(suffix))
         self.pool.extend(own, None, n)
         out = decoded = None
+        before = self.length[row]  # tokens of each request's prefix
+        pos = self._positions(before, suffix)
         for layer in range(self.layers):
-            q, k, v = self.project(layer, [1 << 40 | int(i) for i in ids], suffix)
+            q, k, v = self._project(layer, [1 << 40 | int(i) for i in ids], suffix, pos)
             self.pool.append(layer, k, v, off, n, own)
             out = serve.attend_shared(q, self.pool, layer, off, groups, prefixes, plen, own, n, self.scale)
         if self.samples:
-            decoded = self._decode(starts, prefixes, plen, own, n, suffix, ids)
+            decoded = self._decode(starts, prefixes, plen, own, n, suffix, ids, before + suffix)
         self.pool.free(own, n)
         return out, off, decoded
 
-    def _decode(self, starts, prefixes, plen, own, n, suffix, ids):
-        """One token of ``samples`` continuations of every request."""
+    def _decode(self, starts, prefixes, plen, own, n, suffix, ids, at):
+        """One token of ``samples`` continuations of every request, at position at[r]."""
         s = self.samples
         parent, length = self._i32(np.repeat(np.arange(len(suffix)), s)), self._i32(np.repeat(suffix, s))
         child = torch.empty((len(suffix) * s, self.own_width), dtype=torch.int32, device=self.device)
@@ -169,9 +190,10 @@ class Destination:
         self.pool.extend(child, length, length + 1)
         ones = self._i32(np.arange(len(suffix) * s + 1))
         groups = self._i32(np.concatenate([starts, [len(suffix)]]) * s)
-        out = None
+        one = np.ones(len(suffix) * s, dtype=np.int64)
+        out, pos = None, self._positions(np.repeat(at, s), one)
         for layer in range(self.layers):
-            q, k, v = self.project(layer, [2 << 40 | int(i) * s + j for i in ids for j in range(s)], np.ones(len(suffix) * s, dtype=np.int64))
+            q, k, v = self._project(layer, [2 << 40 | int(i) * s + j for i in ids for j in range(s)], one, pos)
             self.pool.append(layer, k, v, ones, length + 1, child)
             out = serve.attend_shared(q, self.pool, layer, ones, groups, prefixes, plen, child, length + 1, self.scale)
         self.pool.free(child, length + 1)
@@ -193,6 +215,8 @@ def main():
     ap = argparse.ArgumentParser(description="serve one destination's share of the tiny workload")
     ap.add_argument("--requests", type=int, default=256, help="requests of the destination to serve")
     ap.add_argument("--batch", type=int, default=32)
+    ap.add_argument("--codes", choices=("e4m3", "e5m2"), help="hold the cache in these 8-bit floats")
+    ap.add_argument("--rotary", action="store_true", help="turn queries and keys by their positions")
     a = ap.parse_args()
     wl = workload.tiny(n=20_000)
     pipe = Pipeline(wl)
@@ -201,7 +225,9 @@ def main():
     mine = np.flatnonzero(dest == 0)[:a.requests]
     keys, suffix = wl.keys[mine], wl.suffix[mine].astype(np.int64)
     plen = wl.prefix_len[keys].astype(np.int64)
-    d = Destination(wl.candidates[0].W, int(plen.max()), int(suffix.max()), a.batch, samples=2)
+    codes = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2, None: None}[a.codes]
+    d = Destination(wl.candidates[0].W, int(plen.max()), int(suffix.max()), a.batch, samples=2, codes=codes,
+                    rotary=serve.Rotary(128) if a.rotary else None)
     t0 = time.perf_counter()
     for b in range(0, len(mine), a.batch):
         e = min(len(mine), b + a.batch)

@@ -72,6 +72,12 @@ def test_tokens_refuse(L, call, kw):  # noqa: F811
     assert getattr(L, call)(ctypes.byref(_cache()), ctypes.byref(_tokens(**kw)), FAKE, None) == B.CR_EINVAL
 
 
+def test_more_spans_than_are_counted(L):  # noqa: F811
+    """Spans of 8 tokens (blocks of 8, rows of 128 elements) times 2 heads: 2^32 of them and more are refused."""
+    c = _cache(heads=1024)
+    assert L.cr_kvq_append(ctypes.byref(c), ctypes.byref(_tokens(total=(1 << 31) - 1)), FAKE, None) == B.CR_EINVAL
+
+
 def test_tokens_of_nothing(L):  # noqa: F811
     c, none = ctypes.byref(_cache()), ctypes.byref(_tokens(total=0, n=0, width=0, k=_rows(None), v=_rows(None), off=None, length=None, table=None))
     for f in (L.cr_kvq_append, L.cr_kvq_read):
@@ -114,6 +120,12 @@ BAD_ROTARY = [dict(dtype=2), dict(heads_q=0), dict(heads_q=1025), dict(heads_k=1
 @pytest.mark.parametrize("kw", BAD_ROTARY, ids=[next(iter(k)) + str(i) for i, k in enumerate(BAD_ROTARY)])
 def test_rotary_refuses(L, kw):  # noqa: F811
     assert L.cr_rotary(ctypes.byref(_rotary(**kw)), None) == B.CR_EINVAL
+
+
+def test_rotary_over_itself_with_other_strides(L):  # noqa: F811
+    other = _rows(FAKE + 4096)
+    for kw in (dict(q_out=_rows(head=256), k_out=other), dict(q_out=other, k_out=_rows(token=2048))):
+        assert L.cr_rotary(ctypes.byref(_rotary(**kw)), None) == B.CR_EINVAL
 
 
 def test_rotary_of_nothing(L):  # noqa: F811
