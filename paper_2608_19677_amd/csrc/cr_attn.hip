@@ -1206,10 +1206,13 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
 constexpr uint32_t kFewRowTile = 32, kFewWindow = 512, kFewPart = kFewWindow / kWaves, kFewEntries = 256;
 constexpr uint32_t kFewStart = 3;  // tiles that a stretch's start and end cost
 
+// Runs of keys shifted so that the eight lanes that write at once, two rows of 64 elements or one of 128, fall on different banks.
+constexpr uint32_t few_key_run(uint32_t dim) { return kNarrowKeys * 8u + (dim == 64u ? 16u : 8u); }
+
 template <int kDim>
 constexpr uint32_t few_lds()  // elements per wavefront
 {
-    return key_tile(kNarrowKeys, kDim) + val_tile(kNarrowKeys, kDim);
+    return kDim / 8u * few_key_run(kDim) + val_tile(kNarrowKeys, kDim);
 }
 
 // Sequences that the block looks at: up to kFewWindow of them all wavefronts together, of more each a part of its own; and
@@ -1280,6 +1283,16 @@ struct FewLoader {
         }
         if (kOnce) asm volatile("");
     }
+    __device__ __forceinline__ void take(const FewLoader& other)  // its tile
+    {
+        bad |= other.bad;
+#pragma unroll
+        for (uint32_t p = 0; p < kPer; ++p) {
+            rk[p] = other.rk[p];
+            rv[p] = other.rv[p];
+            rs[p] = other.rs[p];
+        }
+    }
     __device__ __forceinline__ void store(uint16_t* lk, uint16_t* lv) const
     {
 #pragma unroll
@@ -1289,7 +1302,7 @@ struct FewLoader {
 #pragma unroll
             for (uint32_t i = 0; i < 2; ++i) {
                 const uint32_t at = piece + i * kLanes;
-                *reinterpret_cast<u32x4*>(lk + at * key_run(kNarrowKeys) + r * 8u) = S::template wide<E>(u32x2{rk[p][2 * i], rk[p][2 * i + 1]}, ks);
+                *reinterpret_cast<u32x4*>(lk + at * few_key_run(kDim) + r * 8u) = S::template wide<E>(u32x2{rk[p][2 * i], rk[p][2 * i + 1]}, ks);
                 *reinterpret_cast<u32x4*>(lv + (at >> 2) * val_run(kNarrowKeys) + r * 32u + (at & 3u) * 8u) =
                     S::template wide<E>(u32x2{rv[p][2 * i], rv[p][2 * i + 1]}, vs);
             }
@@ -1303,11 +1316,11 @@ __device__ CR_INLINE void few_block(const Attn& a, uint32_t lists, uint32_t bloc
     // All heads of a share side by side, on one XCD: where heads lie next to each other in a token a head's row may be less than a line of
     // the caches.
     if (blocks % kXcds == 0u) block = xcd_tile(block, blocks);
-    constexpr uint32_t kKeyRun = key_run(kNarrowKeys), kValRun = val_run(kNarrowKeys);
+    constexpr uint32_t kKeyRun = few_key_run(kDim), kValRun = val_run(kNarrowKeys);
     const uint32_t lane = lane_id(), wv = wave_in_block(), half = lane >> 5, col = lane & 31u;
     const uint32_t wave = block * kWaves + wv, head_kv = wave % a.heads_kv;
     uint16_t* lk = lds + wv * few_lds<kDim>();
-    uint16_t* lv = lk + key_tile(kNarrowKeys, kDim);
+    uint16_t* lv = lk + kDim / 8u * kKeyRun;
 
     const uint32_t first_n = (lists & 1u) ? a.groups : 0u, all_n = first_n + ((lists & 2u) ? a.batch : 0u);
     const bool together = all_n <= kFewWindow;
@@ -1471,6 +1484,7 @@ __device__ CR_INLINE void few_block(const Attn& a, uint32_t lists, uint32_t bloc
         return st;
     };
     constexpr bool kAhead = kDim == 64;  // a stretch's queries are read a tile ahead; of 128 elements there is no room for them
+    constexpr bool kDeep = kDim == 64;  // of 128 elements one tile a wavefront is as many bytes, and as many registers
     FewLoader<E, S, kDim> ld;
     ld.init(a, head_kv);
     const uint32_t k_lane = half * kKeyRun + col * 8u;
@@ -1565,6 +1579,31 @@ __device__ CR_INLINE void few_block(const Attn& a, uint32_t lists, uint32_t bloc
         if (ls.valid && ps.valid && lk0 != ls.key_begin && pk != ps.key_begin) {
             // Inside a stretch: the tile loaded and the one whose page ids are here are of the stretch that is worked on.
             const uint32_t* table = table_of(ps);
+            if (kDeep && pk + 3u * kNarrowKeys < ps.key_end) {
+                // Two tiles of codes on their way, in two sets of registers. Loads come back in their order, so the page ids of a tile are asked for
+                // before the codes of the tile before it: waiting for them leaves those on their way.
+                FewLoader<E, S, kDim> ld2 = ld;  // with the page ids of the tile at pk
+                const bool once = once_of(ps);
+                ld.pages(a, table, pk + kNarrowKeys, ps.key_end);
+                ld2.load(a, pk, ps.key_end, once);
+                for (; pk + 3u * kNarrowKeys < ps.key_end; pk += 2u * kNarrowKeys) {
+                    ld.store(lk, lv);
+                    wave_lds_fence();
+                    ld2.pages(a, table, pk + 2u * kNarrowKeys, ps.key_end);
+                    ld.load(a, pk + kNarrowKeys, ps.key_end, once);
+                    work(pk - kNarrowKeys);
+                    ld2.store(lk, lv);
+                    wave_lds_fence();
+                    ld.pages(a, table, pk + 3u * kNarrowKeys, ps.key_end);
+                    ld2.load(a, pk + 2u * kNarrowKeys, ps.key_end, once);
+                    work(pk);
+                }
+                ld.store(lk, lv);
+                wave_lds_fence();
+                work(pk - kNarrowKeys);
+                pk += kNarrowKeys;
+                ld.take(ld2);
+            }
             for (; pk + kNarrowKeys < ps.key_end; pk += kNarrowKeys) {
                 ld.store(lk, lv);
                 wave_lds_fence();
