@@ -131,6 +131,17 @@ class _Memory:
             self._seen.add(handle)
 
 
+def _on_device(self, stream) -> Optional[int]:
+    """As _Memory's _on, for memory of one device: the call's launches go to the current one."""
+    device = _device()
+    if device != self._device:
+        raise B.CrError(f"made on cuda:{self._device}, the current device is cuda:{device}")
+    handle = _raw_stream(device) if stream is None and _raw_stream else B._stream(stream)
+    if handle not in self._seen:
+        self._see(handle, stream)
+    return handle
+
+
 class Workspace(_Memory):
     """Device scratch of an attention call and its error word."""
 
@@ -278,7 +289,7 @@ class QuantPagePool(PagePool):
         self._device = k.device.index
         self._ready("cr_kvq_", "cr_kvq_append", "cr_kvq_attn", scale)
         self._read = B.load().cr_kvq_read
-        self._head = [self.heads, self.dim]
+        self._head = torch.Size((self.heads, self.dim))
 
     @classmethod
     def empty(cls, layers: int, num_pages: int, heads: int, page_tokens: int, dim: int, dtype=torch.bfloat16, device="cuda",
@@ -292,15 +303,12 @@ class QuantPagePool(PagePool):
         scale = torch.full((layers, num_pages, heads, page_tokens // block, 2), 127, dtype=torch.uint8, device=device)
         return cls(k, v, scale, torch.zeros(num_pages, dtype=torch.int32, device=device), dtype, order)
 
-    def _on(self, stream):
-        if _device() != self._device:
-            raise B.CrError(f"the cache is on cuda:{self._device}, the current device is cuda:{_device()}")
-        return super()._on(stream)
+    _on = _on_device
 
     def _tokens(self, layer, k, v, off, length, table):
         """A cr_kvq_tokens of rows [total, heads, dim] of both."""
         shape, sk, sv, dtype = k.shape, k.stride(), v.stride(), self.dtype
-        if k.dtype is not dtype or v.dtype is not dtype or shape != v.shape or [*shape[1:]] != self._head or sk[2] != 1 or sv[2] != 1:
+        if k.dtype is not dtype or v.dtype is not dtype or shape != v.shape or shape[1:] != self._head or sk[2] != 1 or sv[2] != 1:
             raise B.CrError("rows of keys and values have the cache's heads, dim and type, with dim contiguous")
         if not (k.is_cuda and v.is_cuda):
             raise B.CrError("libcr takes device tensors")
@@ -403,6 +411,8 @@ class Rotary(_Memory):
         self._freq, self._call = self.freq.data_ptr(), B.load().cr_rotary
         super().__init__(self.freq)
 
+    _on = _on_device
+
     def apply(self, q, k, positions, q_out=None, k_out=None, stream=None):
         """q [tokens, heads, dim] and k [tokens, key heads, dim] (or None) turned by ``positions`` (int32 [tokens]; negative ones
         turn back) into q_out and k_out, new tensors if not given; q and k themselves may be given, other tensors must not overlap
@@ -441,8 +451,6 @@ class Rotary(_Memory):
                              *(queries if q_out is q else _rows(q_out)), *keys_out, _index(positions, shape[0]), self._freq)
         except _RANGE as e:
             raise B.CrError(f"an argument is out of range: {e}") from None
-        if _device() != self._device:
-            raise B.CrError(f"the frequencies are on cuda:{self._device}, the current device is cuda:{_device()}")
         rc = self._call(a, self._on(stream))
         if rc:
             B._check(rc, "cr_rotary")
