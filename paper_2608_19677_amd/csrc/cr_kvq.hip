@@ -81,8 +81,9 @@ __host__ __device__ __forceinline__ uint64_t span_start(uint32_t first, uint32_t
 // 128 elements, 8 of 64; a lane has 8 elements of a row). The magnitudes' maximum goes over the lanes of a block; rows from before that
 // share a block are rounded again only where its exponent grows.
 //
-// Bound by memory: 20,000 new tokens of 8 heads of 128 (104 MB) take 20 us, 5.2 TB/s; by the chain of dependent loads where there are
-// few: a token for each of 256 requests 6 us.
+// Bound by memory: 17,221 new tokens of 8 heads of 128 (106 MB read and written) take 19.4 us, 5.5 TB/s (24 in its
+// first form, with ordinary stores); by the chain of dependent loads where there are few: a token for each of 256 requests
+// 5.9 us (8.2 in its first form, with a wave for keys and one for values).
 template <typename T, typename C, int kDim>
 __device__ __forceinline__ void append_span(const QCall& a, uint8_t* ck, uint8_t* cv, uint32_t item)
 {
@@ -224,8 +225,8 @@ __global__ __launch_bounds__(256) void k_kvq_append(QCall a, uint8_t* ck, uint8_
 
 // Tokens read back: a wave takes a token's keys and values of all heads, a lane 8 elements of a head at a time.
 //
-// Bound by memory: 180,000 tokens of 8 heads of 128 (370 MB read, 740 written) take 254 us, 4.4 TB/s (274 with ordinary loads and
-// stores); 37 tokens 3 us.
+// Bound by memory: 180,167 tokens of 8 heads of 128 (370 MB read, 738 written) take 253 us, 4.4 TB/s (274 with ordinary loads and
+// stores); 37 tokens 3 us, the launch.
 template <typename T, typename C, int kDim>
 __global__ __launch_bounds__(256) void k_kvq_read(QCall a)
 {
