@@ -1263,7 +1263,7 @@ struct FewLoader {
 #pragma unroll
         for (uint32_t p = 0; p < kPer; ++p) page[p] = table[min(k0 + p * kStep + row, end - 1u) >> a.pg.log_tokens];
     }
-    // once: nobody else reads the tile, which then need not stay in the caches (128 requests' own tokens, 270 MB, 85 -> 75 us). Where a
+    // once: nobody else reads the tile, which then need not stay in the caches (128 requests' own tokens, 85 -> 75 us). Where a
     // row is less than a line, the head beside it reads the line too.
     __device__ __forceinline__ void load(const Attn& a, uint32_t k0, uint32_t end, bool once)
     {
