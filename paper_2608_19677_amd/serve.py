@@ -366,7 +366,12 @@ def rotary_frequencies(rotated: int, base: float = 10000.0, scaling: Optional[st
     if scaling == "base":
         if rotated == 2:
             raise B.CrError("one pair alone has no other base")
-        base *= factor ** (rotated / (rotated - 2))
+        try:
+            base *= factor ** (rotated / (rotated - 2))
+        except OverflowError:
+            base = math.inf
+        if not 0.0 < base < math.inf:
+            raise B.CrError("base and factor pass a float's range")
     f = [base ** (-2.0 * i / rotated) for i in range(rotated // 2)]
     if scaling == "linear":
         return [x / factor for x in f]
@@ -403,6 +408,8 @@ class Rotary(_Memory):
         self.frequencies = [float(f) for f in frequencies]
         if len(self.frequencies) != self.rotated // 2 or not all(math.isfinite(f) for f in self.frequencies):
             raise B.CrError(f"{self.rotated // 2} finite frequencies wanted")
+        if any(abs(f) >= 2.0 ** 900 for f in self.frequencies):
+            raise B.CrError("frequencies pass a float's range as fractions of a turn")
         turns = [int(round(f / (2.0 * math.pi) * 2.0 ** 64)) % (1 << 64) for f in self.frequencies]  # of 2^64 a turn
         self.freq = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64).to(device)
         if not self.freq.is_cuda:

@@ -201,3 +201,10 @@ def test_frequencies():
     for factor in (1.0, 1):
         for s in ("linear", "base", "turns", "index"):
             assert all(math.isclose(x, y, rel_tol=1e-12) for x, y in zip(serve.rotary_frequencies(r, base, s, factor, 4096), plain))
+
+
+@pytest.mark.parametrize("kw", [dict(frequencies=[1e300] * 32), dict(base=1e300, scaling="base", factor=1e300)])
+def test_frequencies_beyond_floats(kw):
+    """Finite arguments whose turns or base pass a float's range are refused as any other argument."""
+    with pytest.raises(B.CrError):
+        serve.Rotary(64, **kw, device="cpu")
