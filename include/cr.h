@@ -586,7 +586,7 @@ cr_status cr_attn_shared(const cr_kv_cache* c, const cr_attn_shared_args* a, voi
 /* As cr_kv_cache but for the codes (k, v: 1 byte each, 16-byte aligned), whose strides count
  * bytes (multiples of 16, not negative, below 2^31 but for layer_stride), and the scales: u8
  * [layers][num_pages][heads][page_tokens / block_tokens][2], the block's e + 127 of the keys and of the
- * values (at least 1; those of blocks without tokens may be anything). */
+ * values (1 to 254; those of blocks without tokens may be anything). */
 typedef struct {
     uint32_t dtype;        /* CR_BF16 or CR_F16: queries, new keys and values, outputs   */
     uint32_t code;         /* CR_E4M3 or CR_E5M2                                         */

@@ -189,7 +189,8 @@ __device__ __forceinline__ void append_span(const QCall& a, uint8_t* ck, uint8_t
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             uint8_t* codes = (j ? cv : ck) + (int64_t)head * a.c.head_stride + (int64_t)page * a.c.page_stride + piece * 8u;
-            const float up = scale_of(254u - e[j]);  // 2^-(e - 127); e is at most 247
+            // 2^-(e - 127). Elements alone need 247 at most; a block's e from before goes up to 254, and 2^-127 is subnormal.
+            const float up = e[j] < 254u ? scale_of(254u - e[j]) : 0x1p-127f;
 #pragma unroll
             for (uint32_t y = 0; y < kHold; ++y) {
                 if (!is_new(step0 + y)) continue;

@@ -267,7 +267,7 @@ class PagePool(_Memory):
 class QuantPagePool(PagePool):
     """Handle of a paged cache in 8 bits. ``k``, ``v``: as a PagePool's, float8_e4m3fn or float8_e5m2; ``scale``: uint8
     [layers, pages, heads, page tokens / block tokens, 2], of each block of tokens the exponent + 127 of the power of two
-    that its keys' codes, and its values', are multiplied with (a scale of 127 is 1); ``dtype``: the type of queries, new keys and values and outputs.
+    that its keys' codes, and its values', are multiplied with (1 to 254; a scale of 127 is 1); ``dtype``: the type of queries, new keys and values and outputs.
     All of PagePool's calls and ``attend_shared`` work on it: ``append`` rounds into it, with a block's scale chosen by
     its largest element."""
 
