@@ -359,10 +359,27 @@ def rotary_frequencies(rotated: int, base: float = 10000.0, scaling: Optional[st
         raise ValueError(f"unknown scaling {scaling!r}")
     if rotated < 2 or rotated % 2:
         raise B.CrError(f"pairs of elements turn, not {rotated}")
-    if not (base > 1.0 and factor > 0.0 and math.isfinite(base) and math.isfinite(factor)):
-        raise B.CrError("base is above 1 and factor above 0")
-    if scaling in ("turns", "index") and not (length is not None and length > 0 and 0.0 < low < high):
-        raise B.CrError("this scaling goes by the turns over `length` tokens, 0 < low < high")
+    by_turns = scaling in ("turns", "index")
+    try:
+        base, factor = float(base), float(factor)
+        if by_turns and length is not None:
+            length, low, high = float(length), float(low), float(high)
+    except OverflowError:
+        raise B.CrError("an argument passes a float's range") from None
+    if not (1.0 < base < math.inf and 0.0 < factor < math.inf):
+        raise B.CrError("base is above 1 and factor above 0, both finite")
+    if by_turns and not (length is not None and 0.0 < length < math.inf and 0.0 < low < high < math.inf):
+        raise B.CrError("this scaling goes by the turns over `length` tokens, 0 < low < high, all finite")
+    try:
+        f = _frequencies(rotated, base, scaling, factor, length, low, high)
+    except OverflowError:
+        f = [math.inf]
+    if not all(math.isfinite(x) for x in f):
+        raise B.CrError("frequencies pass a float's range")
+    return f
+
+
+def _frequencies(rotated, base, scaling, factor, length, low, high):
     if scaling == "base":
         if rotated == 2:
             raise B.CrError("one pair alone has no other base")
@@ -380,11 +397,23 @@ def rotary_frequencies(rotated: int, base: float = 10000.0, scaling: Optional[st
     if scaling == "turns":
         stay = [(length * x / (2.0 * math.pi) - low) / (high - low) for x in f]
     else:
-        pair = lambda turns: rotated * math.log(length / (2.0 * math.pi * turns)) / (2.0 * math.log(base))  # noqa: E731
+        def pair(turns):
+            over = length / (2.0 * math.pi * turns)
+            log = math.log(over) if 0.0 < over < math.inf else math.log(length) - math.log(2.0 * math.pi) - math.log(turns)
+            return rotated * log / (2.0 * math.log(base))
+
         a, b = max(math.floor(pair(high)), 0), min(math.ceil(pair(low)), rotated - 1)
         stay = [1.0 - (i - a) / max(b - a, 0.001) for i in range(len(f))]
     stay = [min(1.0, max(0.0, s)) for s in stay]
     return [x * ((1.0 - s) / factor + s) for x, s in zip(f, stay)]
+
+
+def _float(x) -> float:
+    """x, or infinity where it is a whole number beyond a float's range."""
+    try:
+        return float(x)
+    except OverflowError:
+        return math.inf
 
 
 class Rotary(_Memory):
@@ -398,14 +427,14 @@ class Rotary(_Memory):
                  frequencies: Optional[Sequence[float]] = None, device="cuda"):
         if layout not in _LAYOUTS:
             raise ValueError(f"unknown layout {layout!r}")
-        self.dim, self.rotated, self.layout, self.magnitude = dim, dim if rotated is None else rotated, layout, float(magnitude)
+        self.dim, self.rotated, self.layout, self.magnitude = dim, dim if rotated is None else rotated, layout, _float(magnitude)
         if dim not in (64, 128) or self.rotated not in range(16, dim + 1, 16):
             raise B.CrError("heads are of 64 or 128 elements, of which a multiple of 16 turns")
         if not abs(self.magnitude) <= 3.4e38:
             raise B.CrError("magnitude is finite")
         if frequencies is None:
             frequencies = rotary_frequencies(self.rotated, base, scaling, factor, length, low, high)
-        self.frequencies = [float(f) for f in frequencies]
+        self.frequencies = [_float(f) for f in frequencies]
         if len(self.frequencies) != self.rotated // 2 or not all(math.isfinite(f) for f in self.frequencies):
             raise B.CrError(f"{self.rotated // 2} finite frequencies wanted")
         if any(abs(f) >= 2.0 ** 900 for f in self.frequencies):
