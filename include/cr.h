@@ -652,7 +652,8 @@ cr_status cr_kvq_attn(const cr_kvq_cache* c, const cr_attn_shared_args* a, void*
  * (CR_ROTARY_PAIRS). Other elements are copied. Computed in fp32 and rounded once; cosines and sines are
  * within 2^-22. Positions are i32; negative ones turn back. freq u64 [rotated / 2], 8-byte aligned: radians per position / (2 pi)
  * * 2^64, rounded. q_out and k_out are q and k (same pointer and strides; CR_EINVAL for other
- * strides), or do not overlap any input.
+ * strides), or do not overlap any input; neither overlaps the other or the other's input (CR_EINVAL
+ * for the same pointer).
  * heads_k may be 0. total * (heads_q + heads_k) < 2^31. */
 #define CR_ROTARY_HALF 0u
 #define CR_ROTARY_PAIRS 1u

@@ -110,6 +110,7 @@ extern "C" cr_status cr_rotary(const cr_rotary_args* p, void* stream)
     Rot a{p->q, p->k, p->q_out, p->k_out, p->positions, p->freq, p->heads_q, p->heads_q + p->heads_k, p->rotated, p->layout, p->total, 1,
           same_rows(p->q, p->q_out, p->total, p->heads_q), p->heads_k && same_rows(p->k, p->k_out, p->total, p->heads_k), p->magnitude};
     if ((p->q.p == p->q_out.p && !a.in_place_q) || (p->heads_k && p->k.p == p->k_out.p && !a.in_place_k)) return CR_EINVAL;  // over itself
+    if (p->heads_k && (p->q_out.p == p->k_out.p || p->q_out.p == p->k.p || p->k_out.p == p->q.p)) return CR_EINVAL;  // over the other
     const uint32_t heads = kWave * 16u / p->dim;  // of a wave
     a.steps = (a.heads + heads - 1u) / heads;
     const uint64_t need = ((uint64_t)a.total * a.steps + kRotWaves - 1u) / kRotWaves;

@@ -452,7 +452,7 @@ class Rotary(_Memory):
     def apply(self, q, k, positions, q_out=None, k_out=None, stream=None):
         """q [tokens, heads, dim] and k [tokens, key heads, dim] (or None) turned by ``positions`` (int32 [tokens]; negative ones
         turn back) into q_out and k_out, new tensors if not given; q and k themselves may be given, other tensors must not overlap
-        q or k. Returns both."""
+        q or k, nor the two each other (one tensor as q and as k is not turned in place). Returns both."""
         shape, dtype, dim = q.shape, q.dtype, self.dim
         code = _DTYPES.get(dtype)
         if code is None:
