@@ -634,7 +634,7 @@ typedef struct {
  * another table's row goes on reading. Heads times min(total, total / max(block_tokens, 512 / dim) + 2 n) < 2^32. */
 cr_status cr_kvq_append(const cr_kvq_cache* c, const cr_kvq_tokens* t, uint32_t* err, void* stream);
 
-/* The reverse: the tokens into the rows. k.p or v.p (or both) may be NULL. Errors as cr_kvq_append; rows of
+/* The reverse: the tokens into the rows, which do not overlap each other (CR_EINVAL for the same pointer). k.p or v.p (or both) may be NULL. Errors as cr_kvq_append; rows of
  * tokens that are skipped stay as they are. */
 cr_status cr_kvq_read(const cr_kvq_cache* c, const cr_kvq_tokens* t, uint32_t* err, void* stream);
 

@@ -344,6 +344,7 @@ extern "C" cr_status cr_kvq_read(const cr_kvq_cache* c, const cr_kvq_tokens* t, 
     QCall a;
     const cr_status rc = q_call(c, t, true, err, &a);
     if (rc != CR_OK || a.total == 0) return rc;
+    if (a.k.p && a.k.p == a.v.p) return CR_EINVAL;  // one place for both
     const hipStream_t st = as_stream(stream);
     const uint32_t blocks = q_blocks(a.total > a.n ? a.total : a.n);
     (void)hipGetLastError();

@@ -330,7 +330,7 @@ class QuantPagePool(PagePool):
 
     def read(self, layer: int, k, v, off, length, table, stream=None):
         """The reverse of ``append``: the last tokens of the length[i] of sequence i into rows off[i]..off[i+1] of k and
-        v ([total, heads, dim], the cache's dtype; either may be None)."""
+        v ([total, heads, dim], the cache's dtype, apart from each other; either may be None)."""
         if k is None and v is None:
             raise B.CrError("rows of keys or of values are wanted")
         t = self._tokens(layer, v if k is None else k, k if v is None else v, off, length, table)
