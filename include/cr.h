@@ -638,8 +638,9 @@ cr_status cr_kvq_append(const cr_kvq_cache* c, const cr_kvq_tokens* t, uint32_t*
  * tokens that are skipped stay as they are. */
 cr_status cr_kvq_read(const cr_kvq_cache* c, const cr_kvq_tokens* t, uint32_t* err, void* stream);
 
-/* cr_attn_shared over this cache: keys and values are what the codes stand for, everything else is as
- * there, the workspace included. */
+/* cr_attn_shared over this cache: keys and values are what the codes stand for, as elements of the cache's type, everything else is as
+ * there, the workspace included; and so are tables much wider than their longest rows (the 64 requests there: attention
+ * takes 34 us, 72 with tables for 4,096 tokens, 269 with tables for 32,768). */
 size_t cr_kvq_attn_workspace_bytes(const cr_kvq_cache* c, const cr_attn_shared_args* a);
 cr_status cr_kvq_attn(const cr_kvq_cache* c, const cr_attn_shared_args* a, void* ws, size_t ws_bytes, uint32_t* err,
                       void* stream);

@@ -1198,15 +1198,19 @@ __device__ CR_INLINE void narrow_block(const Attn& a, uint32_t lists, uint32_t b
 
 // Few rows over codes. Every wavefront works by itself: it takes an equal share of its key head's line of units, where a
 // sequence has kFewStart units and one for each tile of 32 keys for every 32 of its rows, keeps its rows' sums
-// in registers to the end of a stretch and writes them to a slot. No barrier, no sums through LDS; page ids are read two tiles ahead and
-// codes one, past the end of a stretch into the next one's.
+// in registers to the end of a stretch and writes them to a slot. No barrier, no sums through LDS. While a tile is worked on the codes of the next
+// one are on their way, of heads of 64 those of the next two where a stretch has more than five tiles, and the page ids of the tile behind
+// them; at a stretch's end they are the next stretch's.
 //
 // With half the bytes of 16-bit elements a block's start and join (8 us a stretch where four wavefronts share one) were most of
-// the time of many short sequences: 256 requests and 48 prefixes (211 MB, heads of 64) took 84 us so, and take 64.
+// the time of many short sequences: 256 requests on 48 prefixes, heads of 64, pages with tokens before heads (251 MB read). Attention with
+// its join takes 72 us undisturbed, 95 in blocks of four wavefronts like the 16-bit cache's, 94 with three blocks to a compute unit instead of two.
 //
-// Bound by memory where heads have 128 elements: own tokens of 128 requests on 8 key heads, 293 MB read in 62 us, 4.7 TB/s. With 64
-// by latency and by what a tile costs beside its bytes: 251 MB in 64 us, 3.9 TB/s, vector units 47 % busy (the step 79 -> 74 us
-// with two tiles on their way). Three blocks to a compute unit were slower there than two, 65 against 57 us.
+// Bound by memory where heads have 128 elements: own tokens of 128 requests on 8 key heads, 293 MB read in 61 us of this kernel in a
+// trace, 4.8 TB/s. With 64 by latency and by what a tile costs beside its bytes: the 251 MB in 64 us of the 72, 3.9 TB/s, vector units 47 % busy.
+// Two tiles on their way gain where pages have heads before tokens (attention of the same requests so 70.5 -> 65.7 us, of prefixes of 5,000
+// tokens 98 -> 92, of one request on 60,000 34.5 -> 32.1) and cost up to 5 % where they have tokens before heads (71.1 -> 72.0; eight requests
+// on 25,000 tokens 53.8 -> 56.6).
 constexpr uint32_t kFewRowTile = 32, kFewWindow = 512, kFewPart = kFewWindow / kWaves, kFewEntries = 256;
 constexpr uint32_t kFewStart = 3;  // tiles that a stretch's start and end cost
 
@@ -1263,8 +1267,8 @@ struct FewLoader {
 #pragma unroll
         for (uint32_t p = 0; p < kPer; ++p) page[p] = table[min(k0 + p * kStep + row, end - 1u) >> a.pg.log_tokens];
     }
-    // once: nobody else reads the tile, which then need not stay in the caches (128 requests' own tokens, 85 -> 75 us). Where a
-    // row is less than a line, the head beside it reads the line too.
+    // once: nobody else reads the tile, which then need not stay in the caches (128 requests' own tokens, 70 -> 61 us in a trace). Where a
+    // row is less than a line, the head beside it reads the line too (256 requests on 48 prefixes, heads of 64, 64 -> 68 us).
     __device__ __forceinline__ void load(const Attn& a, uint32_t k0, uint32_t end, bool once)
     {
         if (kDim == 128 && once) load_as<true>(a, k0, end);
@@ -1488,7 +1492,7 @@ __device__ CR_INLINE void few_block(const Attn& a, uint32_t lists, uint32_t bloc
         return st;
     };
     constexpr bool kAhead = kDim == 64;  // a stretch's queries are read a tile ahead; of 128 elements there is no room for them
-    constexpr bool kDeep = kDim == 64;  // of 128 elements one tile a wavefront is as many bytes, and as many registers
+    constexpr bool kDeep = kDim == 64;  // of 128 elements one tile is as many bytes, and as many registers, as two of 64
     FewLoader<E, S, kDim> ld;
     ld.init(a, head_kv);
     const uint32_t k_lane = half * kKeyRun + col * 8u;

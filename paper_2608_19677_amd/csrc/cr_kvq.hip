@@ -83,7 +83,9 @@ __host__ __device__ __forceinline__ uint64_t span_start(uint32_t first, uint32_t
 //
 // Bound by memory: 17,221 new tokens of 8 heads of 128 (106 MB read and written) take 19.4 us, 5.5 TB/s (24 in its
 // first form, with ordinary stores); by the chain of dependent loads where there are few: a token for each of 256 requests
-// 5.9 us (8.2 in its first form, with a wave for keys and one for values).
+// 5.9 us (8.2 in its first form, with a wave for keys and one for values). A block of more than kHold steps of rows (16 of 128 elements,
+// 32 of 64) is read twice, for its largest magnitude and for its codes, and a wave has nothing beside it: the 17,221 tokens take 32 us
+// with blocks of 64 tokens and 40 with blocks of 128, the 256 requests' 10 and 15.
 template <typename T, typename C, int kDim>
 __device__ __forceinline__ void append_span(const QCall& a, uint8_t* ck, uint8_t* cv, uint32_t item)
 {

@@ -2,8 +2,8 @@
 //
 // Mathematics: pair (x1, x2) turns by the fraction t of a turn, x1' = m (x1 cos 2 pi t - x2 sin 2 pi t), x2' = m (x2 cos 2 pi t +
 // x1 sin 2 pi t). t is positions[token] * freq / 2^64 modulo 1: an integer product modulo 2^64, exact for every position, of
-// which the upper 32 bits are taken as a signed fraction (rounded to fp32: within 2^-26 of a turn). The hardware's sine and
-// cosine take turns; on all multiples of 2^-24 they are within 1.26e-7.
+// which the upper 32 bits are taken as a signed fraction (rounded to fp32: within 2^-26 of a turn, 0.94e-7 of a cosine). The hardware's sine and
+// cosine take turns; on all multiples of 2^-24 they are within 1.26e-7: 2.2e-7 together, below 2^-22.
 #include "cr_codes.h"
 
 namespace cr {
