@@ -505,7 +505,8 @@ cr_status cr_kv_append(const cr_kv_cache* c, uint32_t layer, const cr_rows* k, c
  * m the largest s_j. causal = 1: row i sees keys j <= i + nk - nq (the last query sees all
  * keys, so nk > nq continues earlier context); causal = 0: all keys. A row that sees no key
  * gives out 0 and lse -inf. Keys and values that a row does not see never reach it, whatever
- * bits they hold, those of its own sequence included. */
+ * bits they hold, those of its own sequence included. Values that are not finite make what they reach
+ * so: NaN, or an infinity that may have become NaN. */
 typedef struct {
     uint32_t dtype, heads_q, heads_kv, dim; /* dim 64 or 128; heads_q a multiple of heads_kv */
     uint32_t batch, causal;
@@ -539,7 +540,7 @@ cr_status cr_attn_prompt(const cr_attn_prompt_args* a, void* ws, size_t ws_bytes
  * own_len may be 0, and a table of width 0 may be NULL. */
 typedef struct {
     uint32_t heads_q, layer;
-    uint32_t batch, groups, total_q;
+    uint32_t batch, groups, total_q;        /* groups <= batch; some may be empty            */
     uint32_t prefix_width, own_width;       /* entries per table row                        */
     float scale;
     cr_rows q, out;                         /* [total_q][heads_q][dim], the cache's type    */
